@@ -295,6 +295,198 @@ gd_status gd_compress_static(const uint64_t* tensor_offsets, uint32_t num_tensor
                              const float* base, float* residual, double drop_ratio, gd_threshold mode,
                              gd_quant quant, const gd_sparse* out, void* stream);
 
+/*
+ * ---- Operators around the compressor ----
+ *
+ * A worker's layers, which write their weights' gradients straight into the
+ * flat gradient that gd_compress takes, and the optimiser step that a server
+ * takes with the summed gradient.  No passage of the paper: it leaves model
+ * and optimiser to the training system.  Conventions above hold, with these
+ * differences: sums and statistics are held in 32 bits or more and may be
+ * formed with fused multiply-adds and matrix instructions; results are the
+ * same on every run.  A handle holds a plan and device scratch, never a
+ * caller's data, so layers of one shape may share one; one call at a time per
+ * handle.  Nothing is allocated after create, so every call may be captured
+ * into a graph (the numbers in the argument struct are captured by value).
+ * Strides count elements between the starts of consecutive rows; within a row
+ * elements are contiguous.  Pointers need the alignment of their element only.
+ * An output may be the same buffer as an input of its own type and stride
+ * where stated, and must otherwise not overlap inputs or other outputs.
+ */
+typedef enum {
+    GD_F32 = 0,  /* IEEE binary32 */
+    GD_BF16 = 1, /* bfloat16 */
+    GD_F16 = 2   /* IEEE binary16 */
+} gd_dtype;
+
+/*
+ * gd_norm - root-mean-square norm of rows with the residual's addition.
+ *   h = x + residual (or x);  y = h * weight / sqrt(mean(h^2) + eps)
+ * The row's mean square is summed in 64 bits, so y does not depend on how the
+ * sum is split; h is rounded where it is written, and y is formed from the
+ * sum as it was before that rounding.
+ * gd_norm_create plans rows of `dim` elements (1..32768) in `type` on the
+ * current device and allocates the scratch of the backward pass (at most
+ * 2 KB per element of dim).
+ */
+typedef struct gd_norm gd_norm;
+gd_status gd_norm_create(gd_norm** out, uint32_t dim, gd_dtype type);
+void gd_norm_destroy(gd_norm* norm);
+
+typedef struct {
+    uint64_t rows;            /* 0: nothing is done */
+    const void* x;            /* [rows][dim] */
+    const void* residual;     /* [rows][dim], or NULL */
+    const void* weight;       /* [dim] */
+    void* sum;                /* [rows][dim] receives h, or NULL; may be x or residual */
+    void* y;                  /* [rows][dim] in the type, or int8 when y_scale is given; in the type it may be x */
+    float* y_scale;           /* [rows], or NULL: y[i][j] * y_scale[i] is then the value, y_scale[i] =
+                                 max_j |value| / 127, y rounded to nearest even.  A row of zeros has scale
+                                 0; one with an infinity or NaN has a scale that is not finite. */
+    uint64_t x_stride, residual_stride, sum_stride, y_stride; /* at least dim */
+    float eps;                /* 0 or more */
+} gd_norm_io;
+
+/* GD_ERR_ARG for a NULL pointer, a stride below dim (0 is no stride) or a bad eps. */
+gd_status gd_norm_forward(gd_norm* norm, const gd_norm_io* io, void* stream);
+
+typedef struct {
+    uint64_t rows;            /* 0: dweight becomes 0 (accumulate: stays) */
+    const void* dy;           /* [rows][dim] gradient of y */
+    const void* x;            /* [rows][dim] what was normalised: sum of the forward call, or its x */
+    const void* weight;       /* [dim] */
+    const void* dsum;         /* [rows][dim] further gradient of the sum (down the residual stream), or NULL */
+    void* dx;                 /* [rows][dim] gradient of x and of residual; may be dy or dsum */
+    float* dweight;           /* [dim] in binary32, or NULL */
+    uint64_t dy_stride, x_stride, dsum_stride, dx_stride;
+    float eps;
+    int accumulate;           /* not 0: dweight += instead of = */
+} gd_norm_grad;
+
+gd_status gd_norm_backward(gd_norm* norm, const gd_norm_grad* io, void* stream);
+
+/*
+ * gd_adamw - an AdamW step (Adam with decoupled weight decay; Kingma and Ba
+ * 2015, Loshchilov and Hutter 2019) over all tensors of a layout at once.
+ *   g' = s g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr weight_decay decay[t])
+ *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * s is grad_scale, or with max_norm > 0 grad_scale * min(1, max_norm / norm),
+ * norm the 2-norm of grad_scale * g over all tensors (summed in 64 bits); a
+ * norm that is not finite skips the step: nothing but *norm is written.
+ *
+ * The moments are the caller's, in 32 bits (m and v, N floats each) or in 8
+ * (N bytes each and a unit per block).  A block is 256 consecutive elements
+ * of one tensor (its last block may be shorter); blocks are numbered tensor
+ * by tensor, gd_adamw_blocks() of them.  In 8 bits a code q of m (signed)
+ * stands for m_unit * q * |q|, with m_unit = max(max |m|, 2^-100) / 127^2
+ * over the block; a code q of v (unsigned) stands for (v_unit * q^2)^2, with
+ * v_unit = max(max sqrt(v), 2^-100) / 255^2: both roots are rounded to the
+ * nearest whole number, except that a v above 0 keeps at least code 1, so
+ * that no moment is divided by eps alone.  All-zero state is zeros, units too.
+ * A block that meets a value that is not finite decodes to such values.
+ */
+typedef struct gd_adamw gd_adamw;
+typedef enum { GD_STATE_F32 = 0, GD_STATE_8BIT = 1 } gd_state;
+
+/* offsets (host, num_tensors + 1 entries): as gd_create, but up to 2^40
+ * elements.  decay (host, num_tensors finite floats of 0 or more, or NULL for
+ * all 1).  Allocates about 16 bytes per 1,024 elements and 20 per tensor on
+ * the current device. */
+gd_status gd_adamw_create(gd_adamw** out, const uint64_t* tensor_offsets, uint32_t num_tensors, gd_state state,
+                          const float* decay);
+void gd_adamw_destroy(gd_adamw* opt);
+uint64_t gd_adamw_blocks(const gd_adamw* opt); /* units per moment; 0 for NULL */
+
+typedef struct {
+    float* params;      /* [N] in/out */
+    const void* grad;   /* [N] in grad_type */
+    void* m;            /* [N] float or int8, in/out */
+    void* v;            /* [N] float or uint8, in/out */
+    float* m_unit;      /* [blocks] in/out; 8-bit state only */
+    float* v_unit;      /* [blocks] */
+    void* copy;         /* [N] receives params rounded to copy_type, or NULL */
+    float* norm;        /* receives the norm when max_norm > 0; or NULL */
+    gd_dtype grad_type, copy_type; /* copy_type: GD_BF16 or GD_F16 when copy is given */
+    uint64_t step;      /* 1 for the first step */
+    double lr, beta1, beta2, eps, weight_decay; /* lr, weight_decay >= 0; 0 <= beta < 1; eps >= 2^-126 */
+    double max_norm;    /* 0: no norm is taken; infinity: taken, and clips nothing */
+    double grad_scale;  /* finite */
+} gd_adamw_io;
+
+gd_status gd_adamw_step(gd_adamw* opt, const gd_adamw_io* io, void* stream);
+
+/* The values that 8-bit moments stand for, as m and v in binary32 (to look at
+ * a state, or to go on from it in 32 bits).  GD_ERR_ARG for a 32-bit state. */
+gd_status gd_adamw_decode(gd_adamw* opt, const void* m, const void* v, const float* m_unit, const float* v_unit,
+                          float* m_out, float* v_out, void* stream);
+
+/*
+ * gd_linear - a layer y = act(x weight^T + bias) + residual, x [rows][in],
+ * weight [out][in], and its backward.
+ * gd_linear_create plans layers of this shape in `type` on the current device
+ * and allocates their scratch (32 MB for partial products, and 1 KB per
+ * output for the bias's gradient).  in and out are 1 to 2^22, max_rows at
+ * most 2^31 - 1.  The handle holds no weights.
+ */
+typedef struct gd_linear gd_linear;
+typedef enum {
+    GD_ACT_NONE = 0,
+    GD_ACT_RELU = 1, /* max(z, 0) */
+    GD_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2 */
+    GD_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} gd_act;
+
+gd_status gd_linear_create(gd_linear** out, uint32_t in, uint32_t out_features, gd_dtype type, gd_act act,
+                           uint64_t max_rows);
+void gd_linear_destroy(gd_linear* layer);
+
+typedef struct {
+    uint64_t rows;            /* 0: nothing is done */
+    const void* x;            /* [rows][in] in the type, or int8 with both scales */
+    const void* weight;       /* [out][in] likewise */
+    const float* x_scale;     /* [rows] and [out], or both NULL: x[i][k] * x_scale[i] and weight[j][k] * */
+    const float* weight_scale; /* weight_scale[j] are the values; the 8-bit products are summed exactly */
+    const void* bias;         /* [out] in the type, or NULL */
+    const void* residual;     /* [rows][out] in the type, or NULL */
+    void* y;                  /* [rows][out] in the type; may be residual */
+    void* pre;                /* [rows][out] in the type receives x weight^T + bias for the backward, or NULL */
+    uint64_t x_stride, weight_stride; /* at least in */
+    uint64_t residual_stride, y_stride, pre_stride; /* at least out; every stride at most 2^22 */
+} gd_linear_io;
+
+/* GD_ERR_ARG for a NULL pointer, rows above max_rows, a bad stride, one scale
+ * without the other; GD_ERR_LAYOUT when in is above 131,072 with scales (the
+ * exact sums are held in 32 bits). */
+gd_status gd_linear_forward(gd_linear* layer, const gd_linear_io* io, void* stream);
+
+typedef struct {
+    uint64_t rows;            /* 0: dweight and dbias become 0 (accumulate: stay) */
+    const void* dy;           /* [rows][out] gradient of y (and of residual) */
+    const void* x;            /* [rows][in]; needed for dweight */
+    const void* weight;       /* [out][in]; needed for dx */
+    const void* pre;          /* [rows][out] pre of the forward call; not read for GD_ACT_NONE */
+    void* dz;                 /* [rows][out] receives dy act'(pre), rounded to the type, the gradient at the
+                                 activation's input that the products below are taken with; may be dy or pre.
+                                 Not written for GD_ACT_NONE, where it is dy. */
+    void* dx;                 /* [rows][in] receives dz weight, or NULL */
+    float* dweight;           /* [out][in] in binary32, rows at dweight_stride: dz^T x, or NULL */
+    float* dbias;             /* [out] in binary32: sum over rows of dz, or NULL */
+    uint64_t dy_stride, x_stride, weight_stride, pre_stride, dz_stride, dx_stride, dweight_stride;
+    int accumulate;           /* not 0: dweight and dbias += instead of = */
+} gd_linear_grad;
+
+gd_status gd_linear_backward(gd_linear* layer, const gd_linear_grad* io, void* stream);
+
+/*
+ * Rows in 8 bits, as the 8-bit products take them: scale[i] = max_j |x[i][j]|
+ * / 127 and q = x / scale rounded to nearest even (a row of zeros has scale 0,
+ * one with an infinity or NaN a scale that is not finite; a row below 2^-119
+ * is stored as zeros).  columns at least 1; x_stride, q_stride >= columns.
+ */
+gd_status gd_quantise_rows(const void* x, gd_dtype type, uint64_t rows, uint64_t columns, uint64_t x_stride, int8_t* q,
+                           uint64_t q_stride, float* scale, void* stream);
+
 /* Infrastructure, no passage of the paper: a static, NUL-terminated
  * description of a status code ("unknown status" for other values). */
 const char* gd_status_string(gd_status status);

@@ -9,41 +9,19 @@
 #include <vector>
 
 #include "gd.h"
+#include "gd_host.hpp"
 #include "gd_internal.h"
 #include "gd_kernels.h"
 
 namespace {
 
+using gd::DeviceGuard;
+using gd::enum_int;
 using gd::kMaxUnits;
 using gd::kUnit;
 
-// Restores the caller's current device on scope exit.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) return;
-        ok = prev == dev || hipSetDevice(dev) == hipSuccess;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
-    }
-};
-
 uint64_t keep_ppm_of(double drop_ratio) { return (uint64_t)std::llround((1.0 - drop_ratio) * 1e6); }
 
-// The integer a C caller passed for an enum parameter.  A C caller may pass
-// any int; in C++ reading an enum object that holds a value outside the
-// enumeration is undefined, so the bytes are copied out instead and checked
-// as an int.
-template <typename E>
-int enum_int(const E* e) {
-    static_assert(sizeof(E) == sizeof(int), "C enums are int-sized");
-    int v;
-    std::memcpy(&v, e, sizeof v);
-    return v;
-}
 bool valid_mode(int m) { return m == GD_GLOBAL || m == GD_PER_TENSOR; }
 bool valid_quant(int q) { return q >= GD_QUANT_NONE && q <= GD_QUANT_COLUMN_MEAN; }
 

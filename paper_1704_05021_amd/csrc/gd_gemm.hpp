@@ -1,0 +1,511 @@
+// The matrix products of the linear layers: out[j][i] = sum_k P(i, k) Q(j, k),
+// with bias, activation and residual in the epilogue.
+//
+// Each operand lies either along k (row i or j holds consecutive k) or across
+// it (row k holds consecutive i or j): forward, P is the weight and Q the
+// input, both along k; for the input's gradient the weight lies across; for
+// the weight's gradient both operands do.  P's rows are the result's
+// contiguous direction, so that a lane's four consecutive accumulators are
+// neighbours in memory.
+//
+// A tile of BI x BJ results takes one block.  Each step of 128 bytes of k is
+// loaded into registers while the step before is multiplied, then stored to
+// the other half of LDS: rows of eight 16-byte chunks, the chunk's place
+// exclusive-ored with bits of the row, so that neither the stores nor the
+// matrix fragments' reads of 32 rows pile onto a bank.  Operands that lie
+// across k are transposed in registers on their way (16-bit elements: one
+// byte permutation per two elements; 32-bit ones: none).  A matrix
+// instruction's lanes each take 16 bytes along k from one row; which k they
+// are does not matter as long as both operands agree.
+#pragma once
+
+#include "gd.h"
+#include "gd_ops.hpp"
+
+namespace gd {
+
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef int i4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef int i16v __attribute__((ext_vector_type(16)));
+typedef bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef f16 h8 __attribute__((ext_vector_type(8)));
+
+template <typename A, typename B>
+__device__ __forceinline__ A bits_as(const B& b) {
+    static_assert(sizeof(A) == sizeof(B));
+    A a;
+    __builtin_memcpy(&a, &b, sizeof a);
+    return a;
+}
+
+// Matrix instructions on 16-byte fragments.  big: 32 x 32 results, lane l
+// holds rows l % 32 and half l / 32 of the fragment pair; result r of a lane
+// is P row 8 (r / 4) + 4 (l / 32) + r % 4, Q row l % 32.  small: 16 x 16, four
+// fragments; result r is P row 4 (l / 16) + r, Q row l % 16.
+template <typename E>
+struct Mma;
+template <>
+struct Mma<bf16> {
+    typedef f16v Big;
+    typedef f4 Small;
+    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bits_as<bf8>(a), bits_as<bf8>(b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<bf8>(a), bits_as<bf8>(b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<f16> {
+    typedef f16v Big;
+    typedef f4 Small;
+    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(bits_as<h8>(a), bits_as<h8>(b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<h8>(a), bits_as<h8>(b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<float> {
+    typedef f16v Big;
+    typedef f4 Small;
+    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
+        const f4 x = bits_as<f4>(a), y = bits_as<f4>(b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], y[j], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+        const f4 x = bits_as<f4>(a), y = bits_as<f4>(b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+        return c;
+    }
+};
+template <>
+struct Mma<int8_t> {
+    typedef i16v Big;
+    typedef i4 Small;
+    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(bits_as<i4>(a), bits_as<i4>(b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(bits_as<i4>(a), bits_as<i4>(b), c, 0, 0, 0);
+    }
+};
+
+// What becomes of a sum.
+struct Finish {
+    void* out;              // [J][I] of O
+    uint64_t out_stride;
+    const void* bias;       // [I] of O, or null
+    const void* residual;   // [J][I] of O, or null
+    uint64_t residual_stride;
+    void* pre;              // [J][I] of O, or null
+    uint64_t pre_stride;
+    const float* p_scale;   // [I] and [J]: 8-bit operands
+    const float* q_scale;
+    int act;
+    int accumulate;         // O float: out += instead of =
+};
+
+struct GemmArgs {
+    const void* p;
+    const void* q;
+    uint64_t p_stride, q_stride;
+    uint32_t I, J, K;
+    uint32_t tiles_i, tiles_j;
+    uint32_t steps;         // k steps of one split
+    float* part;            // [splits][J][I] sums in place of results (int bits for 8-bit operands), or null
+    Finish fin;
+};
+
+__device__ __forceinline__ float activate(int act, float z) {
+    switch (act) {
+        case GD_ACT_RELU: return fmaxf(z, 0.0f) + (z != z ? z : 0.0f);
+        case GD_ACT_GELU: return z * (0.5f * (1.0f + erff(z * 0.70710678118654752f)));
+        case GD_ACT_SILU: return z / (1.0f + expf(-z));
+    }
+    return z;
+}
+
+// Results (j, i) to (j, i + N - 1), n of which exist, from their sums.
+template <typename O, int N>
+__device__ __forceinline__ void finish(const Finish& f, uint64_t j, uint32_t i, float (&s)[N], int n) {
+    if (f.p_scale) {
+        const Pack<float, N> ps = load_some<N>(f.p_scale + i, n);
+        const float qs = f.q_scale[j];
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] *= qs * ps.v[c];
+    }
+    if (f.bias) {
+        const Pack<O, N> b = load_some<N>((const O*)f.bias + i, n);
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] += (float)b.v[c];
+    }
+    if (f.pre) {
+        Pack<O, N> z;
+#pragma unroll
+        for (int c = 0; c < N; ++c) z.v[c] = (O)s[c];
+        store_some<N>((O*)f.pre + j * f.pre_stride + i, z, n);
+    }
+    if (f.act != GD_ACT_NONE)
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = activate(f.act, s[c]);
+    if (f.residual) {
+        const Pack<O, N> r = load_some<N>((const O*)f.residual + j * f.residual_stride + i, n);
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] += (float)r.v[c];
+    }
+    O* out = (O*)f.out + j * f.out_stride + i;
+    if (f.accumulate) {
+        const Pack<O, N> r = load_some<N>(out, n);
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] += (float)r.v[c];
+    }
+    Pack<O, N> y;
+#pragma unroll
+    for (int c = 0; c < N; ++c) y.v[c] = (O)s[c];
+    store_some<N>(out, y, n);
+}
+
+constexpr int kStepBytes = 128;  // of k in a step
+constexpr int kRowChunks = kStepBytes / 16;
+
+// Byte of chunk c of a tile's row in LDS.
+__device__ __forceinline__ uint32_t chunk_at(uint32_t row, uint32_t c) {
+    return row * kStepBytes + ((c ^ (row & 7u) ^ ((row >> 3) & 3u)) << 4);
+}
+
+// A step's R rows of one operand on their way from memory to LDS, the
+// block's THREADS threads sharing them.
+template <typename E, bool ACROSS, int R, int THREADS>
+struct TileLoad;
+
+template <typename E, int R, int THREADS>
+struct TileLoad<E, false, R, THREADS> {
+    static constexpr int CE = 16 / sizeof(E), N = R * kRowChunks / THREADS;
+    static_assert(R * kRowChunks % THREADS == 0, "every thread carries whole chunks");
+    const E* base;       // the tile's first row at the step's k
+    uint32_t off[N];     // elements
+    u4 r[N];
+
+    __device__ void start(const void* p, uint64_t stride, uint32_t row0, uint32_t rows, uint32_t k0) {
+        base = (const E*)p + (uint64_t)row0 * stride + k0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {  // rows past the end repeat the last one; their results are dropped
+            const uint32_t id = n * THREADS + threadIdx.x;
+            off[n] = min(id / kRowChunks, rows - row0 - 1) * (uint32_t)stride + id % kRowChunks * CE;
+        }
+    }
+    __device__ __forceinline__ void load(uint32_t k_left) {
+        if (k_left >= kStepBytes / sizeof(E)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) r[n] = bits_as<u4>(load_pack<CE>(base + off[n]));
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int have = (int)k_left - (int)((n * THREADS + threadIdx.x) % kRowChunks * CE);
+                r[n] = bits_as<u4>(load_some<CE>(base + off[n], have));
+            }
+        }
+        base += kStepBytes / sizeof(E);
+    }
+    __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t id = n * THREADS + threadIdx.x;
+            *(u4*)(lds + chunk_at(id / kRowChunks, id % kRowChunks)) = r[n];
+        }
+    }
+};
+
+template <typename E, int R, int THREADS>
+struct TileLoad<E, true, R, THREADS> {
+    // an item: one chunk of k of four neighbouring rows of the tile
+    static constexpr int CE = 16 / sizeof(E), ITEMS = R / 4 * kRowChunks, N = (ITEMS + THREADS - 1) / THREADS;
+    const E* base;
+    uint64_t stride;
+    int cols[N];         // how many of the item's four rows exist
+    Pack<E, 4> r[N][CE];
+
+    static __device__ __forceinline__ uint32_t group(int n) { return (n * THREADS + threadIdx.x) % (R / 4); }
+    static __device__ __forceinline__ uint32_t chunk(int n) { return (n * THREADS + threadIdx.x) / (R / 4); }
+
+    __device__ void start(const void* p, uint64_t st, uint32_t row0, uint32_t rows, uint32_t k0) {
+        stride = st;
+        base = (const E*)p + (uint64_t)k0 * st + row0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) cols[n] = (int)(rows - row0) - (int)(group(n) * 4);
+    }
+    __device__ __forceinline__ void load(uint32_t k_left) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
+            const uint32_t off = chunk(n) * CE * (uint32_t)stride + group(n) * 4;
+            if (k_left >= kStepBytes / sizeof(E) && cols[n] >= 4) {
+#pragma unroll
+                for (int e = 0; e < CE; ++e) r[n][e] = load_pack<4>(base + (uint64_t)e * stride + off);
+            } else {
+#pragma unroll
+                for (int e = 0; e < CE; ++e)
+                    r[n][e] = load_some<4>(base + (uint64_t)e * stride + off,
+                                           chunk(n) * CE + e < k_left ? cols[n] : 0);
+            }
+        }
+        base += kStepBytes / sizeof(E) * stride;
+    }
+    __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                Pack<E, CE> c;
+#pragma unroll
+                for (int e = 0; e < CE; ++e) c.v[e] = r[n][e].v[m];
+                *(u4*)(lds + chunk_at(group(n) * 4 + m, chunk(n))) = bits_as<u4>(c);
+            }
+        }
+    }
+};
+
+// WI x WJ waves of NI x NJ 32 x 32 results each.
+template <int WI_, int WJ_, int NI_, int NJ_>
+struct Tile {
+    static constexpr int WI = WI_, WJ = WJ_, NI = NI_, NJ = NJ_;
+    static constexpr int BI = WI * NI * 32, BJ = WJ * NJ * 32, kThreads = WI * WJ * kWave;
+    static constexpr int kStage = (BI + BJ) * kStepBytes;           // bytes of LDS of one step
+    static constexpr int kLds = 2 * kStage;
+    static_assert(WI * WJ * NI * 32 * 32 * 4 <= kLds, "the epilogue's rows fit where the operands were");
+};
+typedef Tile<2, 4, 4, 2> TileBig;
+typedef Tile<2, 2, 2, 2> TileMid;
+typedef Tile<2, 2, 1, 1> TileSmall;
+
+// The tile of block b: blocks go to the eight dies in turn, so each die is
+// given a run of neighbouring tiles, and a run goes through 8 tiles along j
+// before the next along i, so that the operands' rows are shared in its L2.
+__device__ __forceinline__ void tile_of(const GemmArgs& a, uint32_t b, uint32_t& ti, uint32_t& tj) {
+    const uint32_t n = a.tiles_i * a.tiles_j, x = b % 8, per = n / 8, rest = n % 8;
+    const uint32_t t = x * per + min(x, rest) + b / 8;
+    constexpr uint32_t kRun = 8;
+    const uint32_t g = t / (kRun * a.tiles_i), wide = min(kRun, a.tiles_j - g * kRun), in = t - g * kRun * a.tiles_i;
+    ti = in / wide;
+    tj = g * kRun + in % wide;
+}
+
+template <typename E, typename O, bool PA, bool QA, typename TL>
+__global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
+    using M = Mma<E>;
+    __shared__ __align__(16) char lds[TL::kLds];
+    constexpr uint32_t KE = kStepBytes / sizeof(E);
+    uint32_t ti, tj;
+    tile_of(a, blockIdx.x, ti, tj);
+    const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
+    const uint32_t k0 = blockIdx.y * a.steps * KE;
+    const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * KE);
+    const uint32_t steps = k_end > k0 ? (k_end - k0 + KE - 1) / KE : 0;
+
+    TileLoad<E, PA, TL::BI, TL::kThreads> lp;
+    TileLoad<E, QA, TL::BJ, TL::kThreads> lq;
+    lp.start(a.p, a.p_stride, i0, a.I, k0);
+    lq.start(a.q, a.q_stride, j0, a.J, k0);
+    typename M::Big acc[TL::NI][TL::NJ];
+#pragma unroll
+    for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+        for (int j = 0; j < TL::NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+
+    const uint32_t wave = wave_index(), lane = lane_id();
+    const uint32_t wi = wave % TL::WI, wj = wave / TL::WI;
+    // this lane's fragment of row r, chunk pair s: the row's bits 0..4 set the chunk's place
+    const uint32_t at = chunk_at(lane & 31, lane >> 5);
+    const uint32_t p_at = wi * TL::NI * 32 * kStepBytes + at;
+    const uint32_t q_at = TL::BI * kStepBytes + wj * TL::NJ * 32 * kStepBytes + at;
+
+    if (steps) {
+        lp.load(k_end - k0);
+        lq.load(k_end - k0);
+        lp.store(lds);
+        lq.store(lds + TL::BI * kStepBytes);
+    }
+    __syncthreads();
+    for (uint32_t s = 0; s < steps; ++s) {
+        const char* now = lds + (s & 1) * TL::kStage;
+        if (s + 1 < steps) {
+            lp.load(k_end - k0 - (s + 1) * KE);
+            lq.load(k_end - k0 - (s + 1) * KE);
+        }
+#pragma unroll
+        for (int c = 0; c < kRowChunks / 2; ++c) {
+            u4 p[TL::NI], q[TL::NJ];
+#pragma unroll
+            for (int i = 0; i < TL::NI; ++i) p[i] = *(const u4*)(now + ((p_at ^ (c << 5)) + i * 32 * kStepBytes));
+#pragma unroll
+            for (int j = 0; j < TL::NJ; ++j) q[j] = *(const u4*)(now + ((q_at ^ (c << 5)) + j * 32 * kStepBytes));
+#pragma unroll
+            for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+                for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::big(p[i], q[j], acc[i][j]);
+        }
+        if (s + 1 < steps) {
+            char* next = lds + ((s + 1) & 1) * TL::kStage;
+            lp.store(next);
+            lq.store(next + TL::BI * kStepBytes);
+        }
+        __syncthreads();
+    }
+
+    // Epilogue: the wave's results go through LDS, 32 rows j of all its i at a
+    // time, so that it reads and writes whole runs of memory.
+    constexpr int W = TL::NI * 32;  // results of a row
+    float* rows = (float*)(lds + wave * (W * 32 * 4));
+    constexpr int kPer = 8, kLanes = W / kPer, kAtOnce = kWave / kLanes;
+#pragma unroll
+    for (int j = 0; j < TL::NJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                f4 v;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = bits_as<float>(acc[i][j][r * 4 + c]);
+                const uint32_t col = i * 32 + r * 8 + (lane >> 5) * 4;
+                *(f4*)(rows + (lane & 31) * W + (col ^ ((lane & 7) << 2))) = v;
+            }
+        wave_lds_sync();
+        const uint32_t col = lane % kLanes * kPer, i = i0 + wi * W + col;
+#pragma unroll 1
+        for (uint32_t r = lane / kLanes; r < 32; r += kAtOnce) {
+            const uint32_t row = j0 + (wj * TL::NJ + j) * 32 + r;
+            float s[kPer];
+            const f4 lo = *(const f4*)(rows + r * W + (col ^ ((r & 7) << 2)));
+            const f4 hi = *(const f4*)(rows + r * W + ((col + 4) ^ ((r & 7) << 2)));
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[c] = lo[c], s[c + 4] = hi[c];
+            if (row < a.J && i < a.I) {
+                const int n = (int)min(a.I - i, (uint32_t)kPer);
+                if (a.part) {
+                    Pack<float, kPer> v;
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c) v.v[c] = s[c];
+                    store_some<kPer>(a.part + ((uint64_t)blockIdx.y * a.J + row) * a.I + i, v, n);
+                } else {
+                    if constexpr (sizeof(E) == 1)
+#pragma unroll
+                        for (int c = 0; c < kPer; ++c) s[c] = (float)bits_as<int>(s[c]);
+                    finish<O>(a.fin, row, i, s, n);
+                }
+            }
+        }
+        wave_lds_sync();
+    }
+}
+
+// Joins the splits' sums, four results a thread.
+template <typename E, typename O>
+__global__ __launch_bounds__(kBlock) void k_join(GemmArgs a, uint32_t splits) {
+    const uint32_t per_row = (a.I + 3) / 4;
+    const uint64_t all = (uint64_t)per_row * a.J;
+    for (uint64_t t = (uint64_t)blockIdx.x * kBlock + threadIdx.x; t < all; t += (uint64_t)gridDim.x * kBlock) {
+        const uint64_t j = t / per_row;
+        const uint32_t i = (uint32_t)(t - j * per_row) * 4;
+        const int n = (int)min(a.I - i, 4u);
+        const float* p = a.part + j * a.I + i;
+        float s[4];
+        if constexpr (sizeof(E) == 1) {
+            int v[4] = {0, 0, 0, 0};
+            for (uint32_t k = 0; k < splits; ++k) {
+                const Pack<float, 4> x = load_some<4>(p + (uint64_t)k * a.J * a.I, n);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] += bits_as<int>(x.v[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[c] = (float)v[c];
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[c] = 0.0f;
+#pragma unroll 4
+            for (uint32_t k = 0; k < splits; ++k) {
+                const Pack<float, 4> x = load_some<4>(p + (uint64_t)k * a.J * a.I, n);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[c] += x.v[c];
+            }
+        }
+        finish<O>(a.fin, j, i, s, n);
+    }
+}
+
+// At most 16 rows of Q (single tokens): a block takes 16 rows of P, its eight
+// waves a share of k each, straight from memory, and joins their sums.  Bound
+// by reading P once.
+constexpr int kThinRows = 16, kThinWaves = 8, kThinDeep = 8;
+template <typename E, typename O>
+__global__ __launch_bounds__(kThinWaves* kWave) void k_thin(GemmArgs a) {
+    using M = Mma<E>;
+    __shared__ f4 lds[kThinWaves][kWave];
+    constexpr uint32_t CE = 16 / sizeof(E), KE = 4 * CE;  // k of one instruction
+    const uint32_t wave = wave_index(), lane = lane_id();
+    const uint32_t i0 = blockIdx.x * kThinRows;
+    const E* p = (const E*)a.p + (uint64_t)min(i0 + lane % 16, a.I - 1) * a.p_stride + lane / 16 * CE;
+    const E* q = (const E*)a.q + (uint64_t)min(lane % 16, a.J - 1) * a.q_stride + lane / 16 * CE;
+    const uint32_t whole = a.K / KE, share = (whole + kThinWaves - 1) / kThinWaves;
+    uint32_t s = min(wave * share, whole);
+    const uint32_t end = min(s + share, whole);
+    typename M::Small acc = {0, 0, 0, 0};
+    for (; s + kThinDeep <= end; s += kThinDeep) {
+        u4 x[kThinDeep], y[kThinDeep];
+#pragma unroll
+        for (int d = 0; d < kThinDeep; ++d) x[d] = bits_as<u4>(load_pack<CE>(p + (uint64_t)(s + d) * KE));
+#pragma unroll
+        for (int d = 0; d < kThinDeep; ++d) y[d] = bits_as<u4>(load_pack<CE>(q + (uint64_t)(s + d) * KE));
+#pragma unroll
+        for (int d = 0; d < kThinDeep; ++d) acc = M::small(x[d], y[d], acc);
+    }
+    for (; s < end; ++s)
+        acc = M::small(bits_as<u4>(load_pack<CE>(p + (uint64_t)s * KE)), bits_as<u4>(load_pack<CE>(q + (uint64_t)s * KE)),
+                       acc);
+    if (wave == kThinWaves - 1 && whole * KE < a.K) {  // what is left of k
+        const int have = (int)(a.K - whole * KE) - (int)(lane / 16 * CE);
+        acc = M::small(bits_as<u4>(load_some<CE>(p + (uint64_t)whole * KE, have)),
+                       bits_as<u4>(load_some<CE>(q + (uint64_t)whole * KE, have)), acc);
+    }
+    lds[wave][lane] = bits_as<f4>(acc);
+    __syncthreads();
+    if (wave != 0) return;
+    const uint32_t i = i0 + lane / 16 * 4, j = lane % 16;
+    if (i >= a.I || j >= a.J) return;
+    float v[4];
+    if constexpr (sizeof(E) == 1) {
+        int t[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kThinWaves; ++w)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) t[c] += bits_as<int>(lds[w][lane][c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = (float)t[c];
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kThinWaves; ++w)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] += lds[w][lane][c];
+    }
+    finish<O>(a.fin, j, i, v, (int)min(a.I - i, 4u));
+}
+
+// Which operands lie across k.
+enum GemmForm { kAlong = 0, kPAcross = 1, kBothAcross = 2 };
+
+// One product, its sums in `room` floats at a.part where k is split.  Operand
+// types: E is O's type, or int8 with kAlong.
+template <typename E, typename O, int FORM>
+hipError_t launch_gemm(GemmArgs a, uint64_t room, hipStream_t st);
+
+}  // namespace gd

@@ -1,0 +1,11 @@
+// The matrix products of layers in bf16.
+#include <algorithm>
+
+#include "gd_gemm_launch.hpp"
+
+namespace gd {
+template hipError_t launch_gemm<bf16, bf16, kAlong>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<bf16, bf16, kPAcross>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<bf16, float, kBothAcross>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<int8_t, bf16, kAlong>(GemmArgs, uint64_t, hipStream_t);
+}  // namespace gd

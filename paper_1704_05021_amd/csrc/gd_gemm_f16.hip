@@ -1,0 +1,11 @@
+// The matrix products of layers in f16.
+#include <algorithm>
+
+#include "gd_gemm_launch.hpp"
+
+namespace gd {
+template hipError_t launch_gemm<f16, f16, kAlong>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<f16, f16, kPAcross>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<f16, float, kBothAcross>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<int8_t, f16, kAlong>(GemmArgs, uint64_t, hipStream_t);
+}  // namespace gd

@@ -48,6 +48,20 @@ EXPORTS = [
     "gd_debug_apply_form",
     "gd_debug_state",
     "gd_compress_static",
+    "gd_norm_create",
+    "gd_norm_destroy",
+    "gd_norm_forward",
+    "gd_norm_backward",
+    "gd_adamw_create",
+    "gd_adamw_destroy",
+    "gd_adamw_blocks",
+    "gd_adamw_step",
+    "gd_adamw_decode",
+    "gd_linear_create",
+    "gd_linear_destroy",
+    "gd_linear_forward",
+    "gd_linear_backward",
+    "gd_quantise_rows",
 ]
 
 
@@ -67,6 +81,25 @@ class _Sparse(ctypes.Structure):
         ("capacity", ctypes.c_uint64),
     ]
 
+
+def _struct(name, **fields):
+    """A ctypes structure from (C type, space-separated field names) pairs in order."""
+    return type(name, (ctypes.Structure,), {"_fields_": [(f, t) for t, names in fields["of"] for f in names.split()]})
+
+
+_vp, _u64, _dbl, _int, _flt = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_double, ctypes.c_int, ctypes.c_float
+_NormIO = _struct("_NormIO", of=[(_u64, "rows"), (_vp, "x residual weight sum y y_scale"),
+                                 (_u64, "x_stride residual_stride sum_stride y_stride"), (_flt, "eps")])
+_NormGrad = _struct("_NormGrad", of=[(_u64, "rows"), (_vp, "dy x weight dsum dx dweight"),
+                                     (_u64, "dy_stride x_stride dsum_stride dx_stride"), (_flt, "eps"),
+                                     (_int, "accumulate")])
+_AdamWIO = _struct("_AdamWIO", of=[(_vp, "params grad m v m_unit v_unit copy norm"), (_int, "grad_type copy_type"),
+                                   (_u64, "step"), (_dbl, "lr beta1 beta2 eps weight_decay max_norm grad_scale")])
+_LinearIO = _struct("_LinearIO", of=[(_u64, "rows"), (_vp, "x weight x_scale weight_scale bias residual y pre"),
+                                     (_u64, "x_stride weight_stride residual_stride y_stride pre_stride")])
+_LinearGrad = _struct("_LinearGrad", of=[(_u64, "rows"), (_vp, "dy x weight pre dz dx dweight dbias"),
+                                         (_u64, "dy_stride x_stride weight_stride pre_stride dz_stride dx_stride "
+                                                "dweight_stride"), (_int, "accumulate")])
 
 _LIB = None
 
@@ -116,6 +149,17 @@ def _lib() -> ctypes.CDLL:
     lib.gd_debug_state.restype = i32
     lib.gd_compress_static.argtypes = [vp, u32, vp, vp, vp, dbl, i32, i32, ctypes.POINTER(_Sparse), vp]
     lib.gd_compress_static.restype = i32
+    for what, args in (("norm", [ctypes.POINTER(vp), u32, i32]), ("linear", [ctypes.POINTER(vp), u32, u32, i32, i32, u64]),
+                       ("adamw", [ctypes.POINTER(vp), vp, u32, i32, vp])):
+        create, destroy = getattr(lib, f"gd_{what}_create"), getattr(lib, f"gd_{what}_destroy")
+        create.argtypes, create.restype = args, i32
+        destroy.argtypes, destroy.restype = [vp], None
+    for name, io in (("gd_norm_forward", _NormIO), ("gd_norm_backward", _NormGrad), ("gd_adamw_step", _AdamWIO),
+                     ("gd_linear_forward", _LinearIO), ("gd_linear_backward", _LinearGrad)):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = [vp, ctypes.POINTER(io), vp], i32
+    lib.gd_adamw_blocks.argtypes, lib.gd_adamw_blocks.restype = [vp], u64
+    lib.gd_adamw_decode.argtypes, lib.gd_adamw_decode.restype = [vp] * 8, i32
+    lib.gd_quantise_rows.argtypes, lib.gd_quantise_rows.restype = [vp, i32, u64, u64, u64, vp, u64, vp, vp], i32
     _LIB = lib
     return lib
 
@@ -437,3 +481,371 @@ def compress_static(offsets: Sequence[int], grad: torch.Tensor, residual: torch.
     else:
         out.k = keep_count(n, drop_ratio)
     return out
+
+
+# ---- operators around the compressor ----
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _dtype_code(dtype: torch.dtype) -> int:
+    if dtype not in _DTYPES:
+        raise TypeError(f"dtype must be float32, bfloat16 or float16, not {dtype}")
+    return _DTYPES[dtype]
+
+
+class _Handle:
+    """A library handle on one device, freed with the object."""
+
+    _what = ""
+
+    def _create(self, device, *args) -> None:
+        lib = _lib()
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self._h = None
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            st = getattr(lib, f"gd_{self._what}_create")(ctypes.byref(h), *args)
+        if st != 0:
+            raise GDError(st, f"gd_{self._what}_create")
+        self._h = h
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            getattr(_lib(), f"gd_{self._what}_destroy")(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _tensor(self, t: torch.Tensor, name: str, dtype: torch.dtype, n: int) -> int:
+        """Address of a contiguous tensor of n elements."""
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous {dtype} tensor on {self.device}")
+        if t.numel() != n:
+            raise ValueError(f"{name} has {t.numel()} elements, not {n}")
+        return t.data_ptr()
+
+    def _matrix(self, t: torch.Tensor, name: str, dtype: torch.dtype, columns: int, rows: Optional[int] = None):
+        """(rows, address, row stride) of a tensor [..., columns] whose rows are contiguous and evenly spaced."""
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device:
+            raise TypeError(f"{name} must be a {dtype} tensor on {self.device}")
+        if t.dim() == 0 or t.shape[-1] != columns:
+            raise ValueError(f"{name} must have rows of {columns} elements, not shape {tuple(t.shape)}")
+        if t.dim() != 2:
+            t = t.view(-1, columns)
+        n = t.shape[0]
+        if rows is not None and n != rows:
+            raise ValueError(f"{name} has {n} rows, not {rows}")
+        if columns > 1 and t.stride(1) != 1 and n > 0:
+            raise ValueError(f"{name} must be contiguous within its rows")
+        return n, t.data_ptr(), t.stride(0) if n > 1 else columns
+
+    def _stream(self, stream: Optional[torch.cuda.Stream], *tensors) -> Optional[int]:
+        """The stream's handle.  Tensors used on a stream that is not the current one are kept from reuse until
+        its work so far is done; that the work before them is done is the caller's to see to."""
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.device.index) or None
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+        return stream.cuda_stream or None
+
+
+class RMSNorm(_Handle):
+    """Root-mean-square norm of rows of ``dim`` elements with the residual's addition (gd_norm_*).
+
+    y = h * weight / sqrt(mean(h^2) + eps), h = x + residual.  Tensors are [..., dim] in ``dtype``; one object
+    serves every layer of its shape on a stream.
+    """
+
+    _what = "norm"
+
+    def __init__(self, dim: int, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-6, device=None):
+        self.dim, self.dtype, self.eps = int(dim), dtype, float(eps)
+        if not 0 < self.dim < 1 << 32:
+            raise GDError(1, "RMSNorm")
+        self._create(device, self.dim, _dtype_code(dtype))
+
+    def forward(self, x, weight, residual=None, out=None, sum_out=None, stream=None):
+        """(y, h); h is x itself without a residual.  ``sum_out`` may be x or residual, ``out`` may be x."""
+        y = torch.empty(x.shape, dtype=self.dtype, device=self.device) if out is None else out
+        h = self._run(x, weight, residual, y, None, sum_out, stream)
+        return y, h
+
+    def forward_int8(self, x, weight, residual=None, out=None, scale=None, sum_out=None, stream=None):
+        """(q, scale, h): rows of y in 8 bits, y = q * scale[row], scale[row] = max|y| / 127."""
+        q = torch.empty(x.shape, dtype=torch.int8, device=self.device) if out is None else out
+        if scale is None:
+            scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=self.device)
+        h = self._run(x, weight, residual, q, scale, sum_out, stream)
+        return q, scale, h
+
+    def _run(self, x, weight, residual, y, scale, sum_out, stream):
+        io = _NormIO(eps=self.eps)
+        rows, io.x, io.x_stride = self._matrix(x, "x", self.dtype, self.dim)
+        io.rows = rows
+        io.weight = self._tensor(weight, "weight", self.dtype, self.dim)
+        _, io.y, io.y_stride = self._matrix(y, "out", self.dtype if scale is None else torch.int8, self.dim, rows)
+        if scale is not None:
+            io.y_scale = self._tensor(scale, "scale", torch.float32, rows)
+        h = x
+        if residual is not None:
+            _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.dim, rows)
+            h = torch.empty(x.shape, dtype=self.dtype, device=self.device) if sum_out is None else sum_out
+        elif sum_out is not None:
+            h = sum_out
+        if h is not x or sum_out is not None:
+            _, io.sum, io.sum_stride = self._matrix(h, "sum_out", self.dtype, self.dim, rows)
+        st = _lib().gd_norm_forward(self._h, io, self._stream(stream, x, weight, residual, y, scale, h))
+        if st != 0:
+            raise GDError(st, "gd_norm_forward")
+        return h
+
+    def backward(self, dy, h, weight, dsum=None, dx=None, dweight=None, accumulate=False, stream=None):
+        """(dx, dweight): the gradient of x and of residual, and the weight's in float32 (a slice of a flat
+        gradient, say).  ``h`` is what forward returned, ``dsum`` a further gradient of h; dx may be dy or dsum."""
+        io = _NormGrad(eps=self.eps, accumulate=int(accumulate))
+        rows, io.dy, io.dy_stride = self._matrix(dy, "dy", self.dtype, self.dim)
+        io.rows = rows
+        _, io.x, io.x_stride = self._matrix(h, "h", self.dtype, self.dim, rows)
+        io.weight = self._tensor(weight, "weight", self.dtype, self.dim)
+        if dsum is not None:
+            _, io.dsum, io.dsum_stride = self._matrix(dsum, "dsum", self.dtype, self.dim, rows)
+        if dx is None:
+            dx = torch.empty(dy.shape, dtype=self.dtype, device=self.device)
+        _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.dim, rows)
+        dweight = _gradient(dweight, accumulate, (self.dim,), self.device)
+        io.dweight = self._tensor(dweight, "dweight", torch.float32, self.dim)
+        st = _lib().gd_norm_backward(self._h, io, self._stream(stream, dy, h, weight, dsum, dx, dweight))
+        if st != 0:
+            raise GDError(st, "gd_norm_backward")
+        return dx, dweight
+
+
+def _gradient(given, accumulate, shape, device):
+    if given is not None:
+        return given
+    if accumulate:
+        raise ValueError("accumulate needs the gradient to add to")
+    return torch.empty(shape, dtype=torch.float32, device=device)
+
+
+class Linear(_Handle):
+    """A layer y = act(x weight^T + bias) + residual (gd_linear_*), weight [out, in] in ``dtype``.
+
+    act: "none", "relu", "gelu" (by erf) or "silu".  The object holds the plan and scratch of calls of at most
+    ``max_rows`` rows, no weights; one object serves every layer of its shape on a stream.
+    """
+
+    _what = "linear"
+
+    def __init__(self, in_features: int, out_features: int, dtype: torch.dtype = torch.bfloat16, act: str = "none",
+                 max_rows: int = 65536, device=None):
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, not {act!r}")
+        self.inf, self.outf, self.dtype, self.act = int(in_features), int(out_features), dtype, act
+        if not (0 < self.inf < 1 << 32 and 0 < self.outf < 1 << 32 and 0 <= int(max_rows) < 1 << 64):
+            raise GDError(1, "Linear")
+        self._create(device, self.inf, self.outf, _dtype_code(dtype), ACTIVATIONS[act], int(max_rows))
+
+    def forward(self, x, weight, bias=None, residual=None, out=None, keep_pre=False, stream=None):
+        """y, or (y, pre) with ``keep_pre`` (True, or a tensor to write): x weight^T + bias for the backward.
+        ``out`` may be residual."""
+        return self._run(x, weight, None, None, bias, residual, out, keep_pre, stream)
+
+    def forward_int8(self, q, scale, weight_q, weight_scale, bias=None, residual=None, out=None, stream=None):
+        """y in ``dtype`` from 8-bit operands: rows of x are q * scale[row], rows of weight weight_q *
+        weight_scale[row], codes in -127..127 (see quantise_rows and RMSNorm.forward_int8)."""
+        return self._run(q, weight_q, scale, weight_scale, bias, residual, out, False, stream)
+
+    def _run(self, x, weight, xs, ws, bias, residual, out, keep_pre, stream):
+        kind = self.dtype if xs is None else torch.int8
+        io = _LinearIO()
+        rows, io.x, io.x_stride = self._matrix(x, "x", kind, self.inf)
+        io.rows = rows
+        _, io.weight, io.weight_stride = self._matrix(weight, "weight", kind, self.inf, self.outf)
+        if xs is not None:
+            io.x_scale = self._tensor(xs, "scale", torch.float32, rows)
+            io.weight_scale = self._tensor(ws, "weight_scale", torch.float32, self.outf)
+        if bias is not None:
+            io.bias = self._tensor(bias, "bias", self.dtype, self.outf)
+        if residual is not None:
+            _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.outf, rows)
+        shape = (*x.shape[:-1], self.outf)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.outf, rows)
+        pre = None
+        if keep_pre is not False:
+            pre = torch.empty(shape, dtype=self.dtype, device=self.device) if keep_pre is True else keep_pre
+            _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, self.outf, rows)
+        st = _lib().gd_linear_forward(self._h, io, self._stream(stream, x, weight, xs, ws, bias, residual, out, pre))
+        if st != 0:
+            raise GDError(st, "gd_linear_forward")
+        return out if pre is None else (out, pre)
+
+    def backward(self, dy, x, weight, pre=None, dx=None, dweight=None, dbias=None, dz=None, need_dx=True,
+                 need_dweight=True, accumulate=False, stream=None):
+        """(dx, dweight, dbias, dz); dweight and dbias in float32 (slices of a flat gradient, say).
+
+        dbias: a tensor to write, True for a new one, or None for a layer without a bias.
+        dz = dy act'(pre) in ``dtype`` is the gradient that the products take (dy itself without an
+        activation).  None for what is not needed; the gradient of the residual is dy.
+        """
+        io = _LinearGrad(accumulate=int(accumulate))
+        rows, io.dy, io.dy_stride = self._matrix(dy, "dy", self.dtype, self.outf)
+        io.rows = rows
+        if self.act != "none":
+            if pre is None:
+                raise ValueError(f"the backward of {self.act} needs pre")
+            _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, self.outf, rows)
+            if dz is None:
+                dz = torch.empty(dy.shape, dtype=self.dtype, device=self.device)
+            _, io.dz, io.dz_stride = self._matrix(dz, "dz", self.dtype, self.outf, rows)
+        else:
+            pre, dz = None, dy
+        if need_dx:
+            _, io.weight, io.weight_stride = self._matrix(weight, "weight", self.dtype, self.inf, self.outf)
+            if dx is None:
+                dx = torch.empty((*dy.shape[:-1], self.inf), dtype=self.dtype, device=self.device)
+            _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.inf, rows)
+        else:
+            dx = None
+        if need_dweight:
+            _, io.x, io.x_stride = self._matrix(x, "x", self.dtype, self.inf, rows)
+            dweight = _gradient(dweight, accumulate, (self.outf, self.inf), self.device)
+            _, io.dweight, io.dweight_stride = self._matrix(dweight, "dweight", torch.float32, self.inf, self.outf)
+        else:
+            dweight = None
+        if dbias is not None:
+            dbias = _gradient(None if dbias is True else dbias, accumulate, (self.outf,), self.device)
+            io.dbias = self._tensor(dbias, "dbias", torch.float32, self.outf)
+        st = _lib().gd_linear_backward(self._h, io, self._stream(stream, dy, x, weight, pre, dz, dx, dweight, dbias))
+        if st != 0:
+            raise GDError(st, "gd_linear_backward")
+        return dx, dweight, dbias, dz
+
+
+def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.cuda.Stream] = None):
+    """(q, scale): rows of x in 8 bits, x = q * scale[row], scale[row] = max|x| / 127 (gd_quantise_rows)."""
+    code = _dtype_code(x.dtype)
+    if not x.is_cuda or x.dim() == 0 or x.shape[-1] == 0:
+        raise ValueError("x must be a GPU tensor of rows of at least one element")
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device) if out is None else out
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
+    on = _Handle()
+    on.device, on._h = x.device, None
+    rows, xp, xs = on._matrix(x, "x", x.dtype, x.shape[-1])
+    _, qp, qs = on._matrix(q, "out", torch.int8, x.shape[-1], rows)
+    sp = on._tensor(scale, "scale", torch.float32, rows)
+    with torch.cuda.device(x.device):
+        st = _lib().gd_quantise_rows(xp, code, rows, x.shape[-1], xs, qp, qs, sp, on._stream(stream, x, q, scale))
+    if st != 0:
+        raise GDError(st, "gd_quantise_rows")
+    return q, scale
+
+
+@dataclass
+class AdamWState:
+    """The moments of an AdamW, the caller's like every other state: in float32, or int8 and uint8 codes with a
+    float32 unit per block of 256 elements of a tensor."""
+
+    m: torch.Tensor
+    v: torch.Tensor
+    m_unit: Optional[torch.Tensor] = None
+    v_unit: Optional[torch.Tensor] = None
+
+
+class AdamW(_Handle):
+    """An AdamW step over all tensors of a layout at once (gd_adamw_*), moments in ``bits`` = 32 or 8 bits.
+
+    ``decay``: a factor per tensor on the step's weight decay (0 for biases and norms, say); all 1 by default.
+    """
+
+    _what = "adamw"
+
+    def __init__(self, offsets: Sequence[int], bits: int = 32, decay: Optional[Sequence[float]] = None, device=None):
+        if bits not in (32, 8):
+            raise ValueError("bits must be 32 or 8")
+        self.offsets = [int(o) for o in offsets]
+        self.T, self.bits = len(self.offsets) - 1, bits
+        if self.T < 1 or min(self.offsets) < 0:
+            raise GDError(2, "AdamW")
+        self.N = self.offsets[-1]
+        if decay is not None and len(decay) != self.T:
+            raise ValueError(f"need {self.T} decay factors, got {len(decay)}")
+        d = None if decay is None else (ctypes.c_float * self.T)(*[float(x) for x in decay])
+        self._create(device, (ctypes.c_uint64 * (self.T + 1))(*self.offsets), self.T, 1 if bits == 8 else 0, d)
+        self.blocks = int(_lib().gd_adamw_blocks(self._h))
+
+    def init_state(self) -> AdamWState:
+        """Moments before the first step: zeros."""
+        kinds = (torch.int8, torch.uint8) if self.bits == 8 else (torch.float32, torch.float32)
+        m, v = (torch.zeros(self.N, dtype=k, device=self.device) for k in kinds)
+        if self.bits == 32:
+            return AdamWState(m, v)
+        return AdamWState(m, v, *(torch.zeros(self.blocks, device=self.device) for _ in range(2)))
+
+    def step(self, params, grad, state: AdamWState, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+             weight_decay: float = 0.01, max_norm: Optional[float] = None, grad_scale: float = 1.0, copy=None,
+             stream=None):
+        """One step, numbered from 1: params (float32) and state change in place; ``copy`` (bfloat16 or float16)
+        receives the new params rounded.  grad is float32, bfloat16 or float16.
+
+        With ``max_norm`` the scaled gradient is clipped to that 2-norm over all tensors, and its norm is
+        returned (one float32 on the device); when it is not finite, nothing else changes.
+        """
+        if not 1 <= int(step) < 1 << 63:
+            raise ValueError("steps are numbered from 1")
+        io = _AdamWIO(step=int(step), lr=lr, beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay,
+                      grad_scale=grad_scale, max_norm=0.0, copy_type=1)
+        io.params = self._tensor(params, "params", torch.float32, self.N)
+        io.grad_type = _dtype_code(grad.dtype)
+        io.grad = self._tensor(grad, "grad", grad.dtype, self.N)
+        self._state(state, io)
+        if copy is not None:
+            if copy.dtype not in (torch.bfloat16, torch.float16):
+                raise TypeError("copy must be bfloat16 or float16")
+            io.copy_type = _DTYPES[copy.dtype]
+            io.copy = self._tensor(copy, "copy", copy.dtype, self.N)
+        norm = None
+        if max_norm is not None:
+            if not max_norm > 0:
+                raise ValueError("max_norm must be above 0")
+            norm = torch.empty(1, dtype=torch.float32, device=self.device)
+            io.max_norm, io.norm = max_norm, norm.data_ptr()
+        st = _lib().gd_adamw_step(self._h, io, self._stream(stream, params, grad, state.m, state.v, state.m_unit,
+                                                            state.v_unit, copy, norm))
+        if st != 0:
+            raise GDError(st, "gd_adamw_step")
+        return norm
+
+    def _state(self, state, io) -> None:
+        if self.bits == 8:
+            io.m = self._tensor(state.m, "state.m", torch.int8, self.N)
+            io.v = self._tensor(state.v, "state.v", torch.uint8, self.N)
+            io.m_unit = self._tensor(state.m_unit, "state.m_unit", torch.float32, self.blocks)
+            io.v_unit = self._tensor(state.v_unit, "state.v_unit", torch.float32, self.blocks)
+        else:
+            io.m = self._tensor(state.m, "state.m", torch.float32, self.N)
+            io.v = self._tensor(state.v, "state.v", torch.float32, self.N)
+
+    def decode(self, state: AdamWState, stream=None):
+        """(m, v) in float32 that an 8-bit state stands for."""
+        if self.bits != 8:
+            raise ValueError("the state is in 32 bits already")
+        io = _AdamWIO()
+        self._state(state, io)
+        m, v = (torch.empty(self.N, dtype=torch.float32, device=self.device) for _ in range(2))
+        st = _lib().gd_adamw_decode(self._h, io.m, io.v, io.m_unit, io.v_unit, m.data_ptr(), v.data_ptr(),
+                                    self._stream(stream, state.m, state.v, state.m_unit, state.v_unit, m, v))
+        if st != 0:
+            raise GDError(st, "gd_adamw_decode")
+        return m, v
