@@ -188,9 +188,11 @@ template <typename E, int R, int THREADS>
 struct TileLoad<E, false, R, THREADS> {
     static constexpr int CE = 16 / sizeof(E), N = R * kRowChunks / THREADS;
     static_assert(R * kRowChunks % THREADS == 0, "every thread carries whole chunks");
-    const E* base;       // the tile's first row at the step's k
+    const E* base;       // the tile's first row at the first step's k
     uint32_t off[N];     // elements
-    u4 r[N];
+    struct Regs {
+        u4 r[N];
+    };
 
     __device__ void start(const void* p, uint64_t stride, uint32_t row0, uint32_t rows, uint32_t k0) {
         base = (const E*)p + (uint64_t)row0 * stride + k0;
@@ -200,24 +202,24 @@ struct TileLoad<E, false, R, THREADS> {
             off[n] = min(id / kRowChunks, rows - row0 - 1) * (uint32_t)stride + id % kRowChunks * CE;
         }
     }
-    __device__ __forceinline__ void load(uint32_t k_left) {
+    __device__ __forceinline__ void load(Regs& g, uint32_t step, uint32_t k_left) const {
+        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E));
         if (k_left >= kStepBytes / sizeof(E)) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) r[n] = bits_as<u4>(load_pack<CE>(base + off[n]));
+            for (int n = 0; n < N; ++n) g.r[n] = bits_as<u4>(load_pack<CE>(at + off[n]));
         } else {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int have = (int)k_left - (int)((n * THREADS + threadIdx.x) % kRowChunks * CE);
-                r[n] = bits_as<u4>(load_some<CE>(base + off[n], have));
+                g.r[n] = bits_as<u4>(load_some<CE>(at + off[n], have));
             }
         }
-        base += kStepBytes / sizeof(E);
     }
-    __device__ __forceinline__ void store(char* lds) const {
+    __device__ __forceinline__ void store(const Regs& g, char* lds) const {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const uint32_t id = n * THREADS + threadIdx.x;
-            *(u4*)(lds + chunk_at(id / kRowChunks, id % kRowChunks)) = r[n];
+            *(u4*)(lds + chunk_at(id / kRowChunks, id % kRowChunks)) = g.r[n];
         }
     }
 };
@@ -229,7 +231,9 @@ struct TileLoad<E, true, R, THREADS> {
     const E* base;
     uint64_t stride;
     int cols[N];         // how many of the item's four rows exist
-    Pack<E, 4> r[N][CE];
+    struct Regs {
+        Pack<E, 4> r[N][CE];
+    };
 
     static __device__ __forceinline__ uint32_t group(int n) { return (n * THREADS + threadIdx.x) % (R / 4); }
     static __device__ __forceinline__ uint32_t chunk(int n) { return (n * THREADS + threadIdx.x) / (R / 4); }
@@ -240,24 +244,24 @@ struct TileLoad<E, true, R, THREADS> {
 #pragma unroll
         for (int n = 0; n < N; ++n) cols[n] = (int)(rows - row0) - (int)(group(n) * 4);
     }
-    __device__ __forceinline__ void load(uint32_t k_left) {
+    __device__ __forceinline__ void load(Regs& g, uint32_t step, uint32_t k_left) const {
+        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E)) * stride;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
             const uint32_t off = chunk(n) * CE * (uint32_t)stride + group(n) * 4;
             if (k_left >= kStepBytes / sizeof(E) && cols[n] >= 4) {
 #pragma unroll
-                for (int e = 0; e < CE; ++e) r[n][e] = load_pack<4>(base + (uint64_t)e * stride + off);
+                for (int e = 0; e < CE; ++e) g.r[n][e] = load_pack<4>(at + (uint64_t)e * stride + off);
             } else {
 #pragma unroll
                 for (int e = 0; e < CE; ++e)
-                    r[n][e] = load_some<4>(base + (uint64_t)e * stride + off,
-                                           chunk(n) * CE + e < k_left ? cols[n] : 0);
+                    g.r[n][e] = load_some<4>(at + (uint64_t)e * stride + off,
+                                             chunk(n) * CE + e < k_left ? cols[n] : 0);
             }
         }
-        base += kStepBytes / sizeof(E) * stride;
     }
-    __device__ __forceinline__ void store(char* lds) const {
+    __device__ __forceinline__ void store(const Regs& g, char* lds) const {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
@@ -265,7 +269,7 @@ struct TileLoad<E, true, R, THREADS> {
             for (int m = 0; m < 4; ++m) {
                 Pack<E, CE> c;
 #pragma unroll
-                for (int e = 0; e < CE; ++e) c.v[e] = r[n][e].v[m];
+                for (int e = 0; e < CE; ++e) c.v[e] = g.r[n][e].v[m];
                 *(u4*)(lds + chunk_at(group(n) * 4 + m, chunk(n))) = bits_as<u4>(c);
             }
         }
@@ -297,72 +301,12 @@ __device__ __forceinline__ void tile_of(const GemmArgs& a, uint32_t b, uint32_t&
     tj = g * kRun + in % wide;
 }
 
-template <typename E, typename O, bool PA, bool QA, typename TL>
-__global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
-    using M = Mma<E>;
-    __shared__ __align__(16) char lds[TL::kLds];
-    constexpr uint32_t KE = kStepBytes / sizeof(E);
-    uint32_t ti, tj;
-    tile_of(a, blockIdx.x, ti, tj);
-    const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
-    const uint32_t k0 = blockIdx.y * a.steps * KE;
-    const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * KE);
-    const uint32_t steps = k_end > k0 ? (k_end - k0 + KE - 1) / KE : 0;
-
-    TileLoad<E, PA, TL::BI, TL::kThreads> lp;
-    TileLoad<E, QA, TL::BJ, TL::kThreads> lq;
-    lp.start(a.p, a.p_stride, i0, a.I, k0);
-    lq.start(a.q, a.q_stride, j0, a.J, k0);
-    typename M::Big acc[TL::NI][TL::NJ];
-#pragma unroll
-    for (int i = 0; i < TL::NI; ++i)
-#pragma unroll
-        for (int j = 0; j < TL::NJ; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-
-    const uint32_t wave = wave_index(), lane = lane_id();
-    const uint32_t wi = wave % TL::WI, wj = wave / TL::WI;
-    // this lane's fragment of row r, chunk pair s: the row's bits 0..4 set the chunk's place
-    const uint32_t at = chunk_at(lane & 31, lane >> 5);
-    const uint32_t p_at = wi * TL::NI * 32 * kStepBytes + at;
-    const uint32_t q_at = TL::BI * kStepBytes + wj * TL::NJ * 32 * kStepBytes + at;
-
-    if (steps) {
-        lp.load(k_end - k0);
-        lq.load(k_end - k0);
-        lp.store(lds);
-        lq.store(lds + TL::BI * kStepBytes);
-    }
-    __syncthreads();
-    for (uint32_t s = 0; s < steps; ++s) {
-        const char* now = lds + (s & 1) * TL::kStage;
-        if (s + 1 < steps) {
-            lp.load(k_end - k0 - (s + 1) * KE);
-            lq.load(k_end - k0 - (s + 1) * KE);
-        }
-#pragma unroll
-        for (int c = 0; c < kRowChunks / 2; ++c) {
-            u4 p[TL::NI], q[TL::NJ];
-#pragma unroll
-            for (int i = 0; i < TL::NI; ++i) p[i] = *(const u4*)(now + ((p_at ^ (c << 5)) + i * 32 * kStepBytes));
-#pragma unroll
-            for (int j = 0; j < TL::NJ; ++j) q[j] = *(const u4*)(now + ((q_at ^ (c << 5)) + j * 32 * kStepBytes));
-#pragma unroll
-            for (int i = 0; i < TL::NI; ++i)
-#pragma unroll
-                for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::big(p[i], q[j], acc[i][j]);
-        }
-        if (s + 1 < steps) {
-            char* next = lds + ((s + 1) & 1) * TL::kStage;
-            lp.store(next);
-            lq.store(next + TL::BI * kStepBytes);
-        }
-        __syncthreads();
-    }
-
-    // Epilogue: the wave's results go through LDS, 32 rows j of all its i at a
-    // time, so that it reads and writes whole runs of memory.
+// The block's sums to their results.  A wave's go through LDS, 32 rows j of
+// all its i at a time, so that it reads and writes whole runs of memory.
+template <typename E, typename O, typename TL>
+__device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::Big (&acc)[TL::NI][TL::NJ], char* lds,
+                                           uint32_t i0, uint32_t j0) {
+    const uint32_t wave = wave_index(), lane = lane_id(), wi = wave % TL::WI, wj = wave / TL::WI;
     constexpr int W = TL::NI * 32;  // results of a row
     float* rows = (float*)(lds + wave * (W * 32 * 4));
     constexpr int kPer = 8, kLanes = W / kPer, kAtOnce = kWave / kLanes;
@@ -405,6 +349,295 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
         }
         wave_lds_sync();
     }
+}
+
+template <typename E, typename O, bool PA, bool QA, typename TL, int SETS = 2>
+__global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
+    using M = Mma<E>;
+    __shared__ __align__(16) char lds[TL::kLds];
+    constexpr uint32_t KE = kStepBytes / sizeof(E);
+    uint32_t ti, tj;
+    tile_of(a, blockIdx.x, ti, tj);
+    const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
+    const uint32_t k0 = blockIdx.y * a.steps * KE;
+    const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * KE);
+    const uint32_t steps = k_end > k0 ? (k_end - k0 + KE - 1) / KE : 0;
+
+    TileLoad<E, PA, TL::BI, TL::kThreads> lp;
+    TileLoad<E, QA, TL::BJ, TL::kThreads> lq;
+    lp.start(a.p, a.p_stride, i0, a.I, k0);
+    lq.start(a.q, a.q_stride, j0, a.J, k0);
+    typename M::Big acc[TL::NI][TL::NJ];
+#pragma unroll
+    for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+        for (int j = 0; j < TL::NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+
+    const uint32_t wave = wave_index(), lane = lane_id();
+    const uint32_t wi = wave % TL::WI, wj = wave / TL::WI;
+    // this lane's fragment of row r, chunk pair s: the row's bits 0..4 set the chunk's place
+    const uint32_t at = chunk_at(lane & 31, lane >> 5);
+    const uint32_t p_at = wi * TL::NI * 32 * kStepBytes + at;
+    const uint32_t q_at = TL::BI * kStepBytes + wj * TL::NJ * 32 * kStepBytes + at;
+
+    typename decltype(lp)::Regs rp[SETS];
+    typename decltype(lq)::Regs rq[SETS];
+    const auto load = [&](int set, uint32_t s) {
+        if (s >= steps) return;
+        lp.load(rp[set], s, k_end - k0 - s * KE);
+        lq.load(rq[set], s, k_end - k0 - s * KE);
+    };
+    const auto store = [&](int set, uint32_t s) {
+        if (s >= steps) return;
+        char* to = lds + (s & 1) * TL::kStage;
+        lp.store(rp[set], to);
+        lq.store(rq[set], to + TL::BI * kStepBytes);
+    };
+    const auto multiply = [&](uint32_t s, int c) {
+        const char* now = lds + (s & 1) * TL::kStage;
+        u4 p[TL::NI], q[TL::NJ];
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i) p[i] = *(const u4*)(now + ((p_at ^ (c << 5)) + i * 32 * kStepBytes));
+#pragma unroll
+        for (int j = 0; j < TL::NJ; ++j) q[j] = *(const u4*)(now + ((q_at ^ (c << 5)) + j * 32 * kStepBytes));
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+            for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::big(p[i], q[j], acc[i][j]);
+    };
+    // step s multiplies what LDS holds, stores step s + 1, loaded SETS steps
+    // ago, to the other half, and loads into its registers anew
+    load(0, 0);
+    store(0, 0);
+#pragma unroll
+    for (int d = 0; d < SETS; ++d) load(d, d + 1);
+    __syncthreads();
+    for (uint32_t s0 = 0; s0 < steps; s0 += SETS)
+#pragma unroll
+        for (int d = 0; d < SETS; ++d) {
+            const uint32_t s = s0 + d;
+            if (SETS > 1 && s >= steps) break;
+            multiply(s, 0);
+            store(d, s + 1);
+            load(d, s + 1 + SETS);
+#pragma unroll
+            for (int c = 1; c < kRowChunks / 2; ++c) multiply(s, c);
+            __syncthreads();
+        }
+
+    store_tile<E, O, TL>(a, acc, lds, i0, j0);
+}
+
+// ---- The same product with operands that memory instructions place in LDS ----
+//
+// For 16- and 8-bit operands whose rows start and end at 16-byte boundaries.
+// A step is 64 bytes of k; four steps have room in LDS.  While step s is
+// multiplied, steps s + 2 to s + 4 are on their way from memory straight into
+// LDS, in no register, and step s + 1 is there: its first fragments are read
+// behind the last products of step s.  One barrier a step both shows that
+// step s + 1 has come for every wave and frees the room of step s.
+//
+// Along k a row's four 16-byte chunks change places by the row's bits 2 and 3.
+// Across k the tile lies in LDS as in memory, a row for each k, and the
+// transposing LDS read gives each lane four k of one row; pairs of 16-byte
+// chunks change places by the low bits of k.  A load puts its lanes' data
+// side by side, so the places are chosen by what each lane fetches.
+constexpr int kLineBytes = 64;  // of k in a step
+constexpr int kDeep = 4;        // steps in LDS
+
+static __device__ const u4 zero_chunk = {0, 0, 0, 0};  // what lanes past the end of k fetch
+
+// 16 bytes from base + off to each lane's place after lds_at (uniform).  The
+// instruction writes no register; load_wait says when its data is there.
+__device__ __forceinline__ void fetch(const void* base, uint32_t off, uint32_t lds_at) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds_at)
+                 : "memory");
+}
+__device__ __forceinline__ void fetch_far(const void* at, uint32_t lds_at) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds_at) : "memory");
+}
+// Until at most N fetches of this wave are under way and its LDS reads are done; then until all waves are here.
+template <int N>
+__device__ __forceinline__ void load_wait() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <typename E, bool ACROSS, int R, int THREADS>
+struct TileFetch {
+    static constexpr int kBytes = R * kLineBytes, N = kBytes / (THREADS * 16), KE = kLineBytes / sizeof(E);
+    static constexpr int CE = 16 / sizeof(E);
+    static constexpr int kRowBytes = ACROSS ? R * (int)sizeof(E) : kLineBytes;
+    static constexpr int kUnits = kRowBytes / 32;  // across: pairs of chunks of a k
+    static_assert(kBytes % (THREADS * 16) == 0 && (!ACROSS || sizeof(E) == 2));
+    const E* base;      // the tile's first row at the first step's k
+    uint64_t per_step;  // bytes
+    uint32_t stride;
+    uint32_t off[N];    // bytes
+
+    // k and row, in elements of the tile, of the chunk that this lane fetches with its n-th load
+    static __device__ __forceinline__ uint32_t at(int n) {
+        return (n * (THREADS / kWave) + wave_index()) * kWave * 16 + lane_id() * 16;
+    }
+    static __device__ __forceinline__ uint32_t place(uint32_t k) { return kUnits >= 8 ? (k & 3) << 1 : k & 3; }
+    static __device__ __forceinline__ uint32_t k_of(int n) {
+        if constexpr (ACROSS) return at(n) / kRowBytes;
+        const uint32_t row = at(n) / kLineBytes;
+        return ((at(n) / 16 % 4) ^ ((row >> 2) & 3)) * CE;
+    }
+    static __device__ __forceinline__ uint32_t row_of(int n) {
+        if constexpr (!ACROSS) return at(n) / kLineBytes;
+        const uint32_t chunk = at(n) % kRowBytes / 16;
+        return ((chunk >> 1) ^ place(k_of(n))) * 16 + (chunk & 1) * 8;
+    }
+    __device__ void start(const void* p, uint64_t st, uint32_t row0, uint32_t rows, uint32_t k0) {
+        stride = (uint32_t)st;
+        base = (const E*)p + (ACROSS ? (uint64_t)k0 * st + row0 : (uint64_t)row0 * st + k0);
+        per_step = (ACROSS ? KE * st : KE) * sizeof(E);
+        const uint32_t last = rows - row0 - (ACROSS ? 8 : 1);  // rows past the end repeat the last; their results are dropped
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t r = min(row_of(n), last);
+            off[n] = (ACROSS ? k_of(n) * stride + r : r * stride + k_of(n)) * (uint32_t)sizeof(E);
+        }
+    }
+    template <bool WHOLE>
+    __device__ __forceinline__ void issue(uint32_t step, uint32_t k_left, uint32_t lds_at) const {
+        const char* from = (const char*)base + step * per_step;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t to = lds_at + (n * (THREADS / kWave) + wave_index()) * kWave * 16;
+            if (WHOLE)
+                fetch(from, off[n], to);
+            else
+                fetch_far(k_of(n) < k_left ? (const void*)(from + off[n]) : &zero_chunk, to);
+        }
+    }
+    // This lane's part of the address of its fragment of 32 rows, 16 bytes of k each, number c of the step.
+    static __device__ __forceinline__ uint32_t lane_at(int c) {
+        const uint32_t l = lane_id();
+        if constexpr (ACROSS) {
+            const uint32_t k = c * 16 + (l >> 5) * 8 + l % 16 / 4, unit = (l >> 4) & 1;
+            return k * kRowBytes + ((unit ^ place(k)) << 5) + l % 4 * 8;
+        }
+        const uint32_t row = l & 31;
+        return row * kLineBytes + (((c * 2 + (l >> 5)) ^ ((row >> 2) & 3)) << 4);
+    }
+    // The fragment of rows row0 (a multiple of 32) on; lane is lane_at(c), the tile starts at `tile` in LDS.
+    static __device__ __forceinline__ u4 fragment(const char* tile, uint32_t row0, uint32_t lane) {
+        if constexpr (ACROSS) {
+            // rows 32 on are two units on; the place's exclusive-or does not carry into them beyond 8 units
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4 lds_s4;
+            const char* p = tile + (lane ^ (row0 / 16 << 5));
+            u4 v;
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p);
+            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * kRowBytes));
+            __builtin_memcpy(&v, &lo, 8);
+            __builtin_memcpy((char*)&v + 8, &hi, 8);
+            return v;
+        }
+        return *(const u4*)(tile + row0 * kLineBytes + lane);
+    }
+};
+
+template <typename E, typename O, bool PA, bool QA, typename TL>
+__global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
+    using M = Mma<E>;
+    using FP = TileFetch<E, PA, TL::BI, TL::kThreads>;
+    using FQ = TileFetch<E, QA, TL::BJ, TL::kThreads>;
+    constexpr int kStage = (TL::BI + TL::BJ) * kLineBytes, kLoads = FP::N + FQ::N;
+    __shared__ __align__(1024) char lds[kDeep * kStage];
+    static_assert(TL::kLds <= kDeep * kStage, "the epilogue's rows fit");
+    uint32_t ti, tj;
+    tile_of(a, blockIdx.x, ti, tj);
+    const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
+    const uint32_t k0 = blockIdx.y * a.steps * FP::KE;
+    const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * FP::KE);
+    const uint32_t steps = k_end > k0 ? (k_end - k0 + FP::KE - 1) / FP::KE : 0;
+    FP fp;
+    FQ fq;
+    fp.start(a.p, a.p_stride, i0, a.I, k0);
+    fq.start(a.q, a.q_stride, j0, a.J, k0);
+    typename M::Big acc[TL::NI][TL::NJ];
+#pragma unroll
+    for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+        for (int j = 0; j < TL::NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+
+    const uint32_t wave = wave_index(), wi = wave % TL::WI, wj = wave / TL::WI;
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    uint32_t p_at[2], q_at[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) p_at[c] = FP::lane_at(c), q_at[c] = FQ::lane_at(c);
+    const uint32_t whole = k_end > k0 ? (k_end - k0) / FP::KE : 0;
+    const auto issue_whole = [&](uint32_t s) {
+        const uint32_t to = lds_at + s % kDeep * kStage;
+        fp.template issue<true>(s, 0, to);
+        fq.template issue<true>(s, 0, to + FP::kBytes);
+    };
+    const auto issue = [&](uint32_t s) {
+        if (s < whole) return issue_whole(s);
+        const uint32_t to = lds_at + s % kDeep * kStage, left = k_end - k0 - s * FP::KE;
+        fp.template issue<false>(s, left, to);
+        fq.template issue<false>(s, left, to + FP::kBytes);
+    };
+    const auto read = [&](uint32_t s, int c, u4 (&p)[TL::NI], u4 (&q)[TL::NJ]) {
+        const char* now = lds + s % kDeep * kStage;
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i) p[i] = FP::fragment(now, (wi * TL::NI + i) * 32, p_at[c]);
+#pragma unroll
+        for (int j = 0; j < TL::NJ; ++j) q[j] = FQ::fragment(now + FP::kBytes, (wj * TL::NJ + j) * 32, q_at[c]);
+    };
+    const auto multiply = [&](const u4 (&p)[TL::NI], const u4 (&q)[TL::NJ]) {
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+            for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::big(p[i], q[j], acc[i][j]);
+    };
+    // steps s + 1 on may be under way up to the last that was issued
+    const auto wait_for = [&](uint32_t s) {
+        const uint32_t after = min(steps - 1 - s, 2u);
+        if (after == 2)
+            load_wait<2 * kLoads>();
+        else if (after == 1)
+            load_wait<kLoads>();
+        else
+            load_wait<0>();
+    };
+    u4 pa[TL::NI], qa[TL::NJ], pb[TL::NI], qb[TL::NJ];
+    if (steps) {
+#pragma unroll 1
+        for (uint32_t s = 0; s < min(steps, kDeep - 1u); ++s) issue(s);
+        wait_for(0);
+        if (kDeep - 1 < steps) issue(kDeep - 1);
+        read(0, 0, pa, qa);
+    }
+    uint32_t s = 0;
+    for (; s + kDeep < whole; ++s) {
+        read(s, 1, pb, qb);
+        multiply(pa, qa);
+        load_wait<2 * kLoads>();
+        issue_whole(s + kDeep);
+        read(s + 1, 0, pa, qa);
+        multiply(pb, qb);
+    }
+#pragma unroll 1
+    for (; s < steps; ++s) {
+        read(s, 1, pb, qb);
+        multiply(pa, qa);
+        if (s + 1 < steps) {
+            wait_for(s + 1);
+            if (s + kDeep < steps) issue(s + kDeep);
+            read(s + 1, 0, pa, qa);
+        }
+        multiply(pb, qb);
+    }
+    __syncthreads();
+    store_tile<E, O, TL>(a, acc, lds, i0, j0);
 }
 
 // Joins the splits' sums, four results a thread.

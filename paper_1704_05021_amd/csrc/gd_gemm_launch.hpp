@@ -5,9 +5,20 @@
 
 namespace gd {
 
+// Whether every row of both operands starts and ends at a 16-byte boundary.
+template <typename E, int FORM>
+bool whole_chunks(const GemmArgs& a) {
+    constexpr uint32_t CE = 16 / sizeof(E);
+    if (sizeof(E) > 2) return false;
+    const bool aligned = (((uintptr_t)a.p | (uintptr_t)a.q) & 15) == 0 && a.p_stride % CE == 0 && a.q_stride % CE == 0;
+    return aligned && (FORM == kBothAcross || a.K % CE == 0) && (FORM == kAlong || a.I % CE == 0) &&
+           (FORM != kBothAcross || a.J % CE == 0);
+}
+
 template <typename E, typename O, int FORM, typename TL>
 hipError_t launch_tiles(GemmArgs a, uint64_t room, hipStream_t st) {
-    constexpr uint32_t KE = kStepBytes / sizeof(E);
+    const bool direct = whole_chunks<E, FORM>(a);
+    const uint32_t KE = (direct ? kLineBytes : kStepBytes) / sizeof(E);
     a.tiles_i = (a.I + TL::BI - 1) / TL::BI;
     a.tiles_j = (a.J + TL::BJ - 1) / TL::BJ;
     const uint64_t tiles = (uint64_t)a.tiles_i * a.tiles_j, steps = ((uint64_t)a.K + KE - 1) / KE;
@@ -23,8 +34,11 @@ hipError_t launch_tiles(GemmArgs a, uint64_t room, hipStream_t st) {
     if (a.steps) splits = (steps + a.steps - 1) / a.steps;
     float* part = a.part;
     if (splits == 1) a.part = nullptr;
-    k_gemm<E, O, FORM >= kPAcross, FORM == kBothAcross, TL>
-        <<<dim3((uint32_t)tiles, (uint32_t)splits), dim3(TL::kThreads), 0, st>>>(a);
+    const dim3 grid((uint32_t)tiles, (uint32_t)splits);
+    if constexpr (sizeof(E) <= 2) {
+        if (direct) k_gemm_fetch<E, O, FORM >= kPAcross, FORM == kBothAcross, TL><<<grid, dim3(TL::kThreads), 0, st>>>(a);
+    }
+    if (!direct) k_gemm<E, O, FORM >= kPAcross, FORM == kBothAcross, TL><<<grid, dim3(TL::kThreads), 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     a.part = part;
