@@ -425,9 +425,13 @@ gd_status gd_adamw_decode(gd_adamw* opt, const void* m, const void* v, const flo
  * gd_linear - a layer y = act(x weight^T + bias) + residual, x [rows][in],
  * weight [out][in], and its backward.
  * gd_linear_create plans layers of this shape in `type` on the current device
- * and allocates their scratch (32 MB for partial products, and 1 KB per
- * output for the bias's gradient).  in and out are 1 to 2^22, max_rows at
- * most 2^31 - 1.  The handle holds no weights.
+ * and allocates their scratch: 32 MB for partial products, 1 KB per output for
+ * the bias's gradient, and in 16 bits, where in or out is no multiple of 8,
+ * room for padded copies of a product's operands, at most 512 MB (larger
+ * products then take a slower form).  in and out are 1 to 2^22, max_rows at
+ * most 2^31 - 1.  The handle holds no weights.  Products are fastest where in
+ * and out are multiples of 8 (16 for 8-bit operands) and operands start at
+ * 16-byte boundaries.
  */
 typedef struct gd_linear gd_linear;
 typedef enum {
@@ -446,7 +450,8 @@ typedef struct {
     const void* x;            /* [rows][in] in the type, or int8 with both scales */
     const void* weight;       /* [out][in] likewise */
     const float* x_scale;     /* [rows] and [out], or both NULL: x[i][k] * x_scale[i] and weight[j][k] * */
-    const float* weight_scale; /* weight_scale[j] are the values; the 8-bit products are summed exactly */
+    const float* weight_scale; /* weight_scale[j] are the values, codes in -127..127; their products are summed
+                                  exactly */
     const void* bias;         /* [out] in the type, or NULL */
     const void* residual;     /* [rows][out] in the type, or NULL */
     void* y;                  /* [rows][out] in the type; may be residual */

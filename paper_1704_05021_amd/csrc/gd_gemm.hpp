@@ -26,8 +26,6 @@ namespace gd {
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
-typedef float f16v __attribute__((ext_vector_type(16)));
-typedef int i16v __attribute__((ext_vector_type(16)));
 typedef bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef f16 h8 __attribute__((ext_vector_type(8)));
 
@@ -39,45 +37,31 @@ __device__ __forceinline__ A bits_as(const B& b) {
     return a;
 }
 
-// Matrix instructions on 16-byte fragments.  big: 32 x 32 results, lane l
-// holds rows l % 32 and half l / 32 of the fragment pair; result r of a lane
-// is P row 8 (r / 4) + 4 (l / 32) + r % 4, Q row l % 32.  small: 16 x 16, four
-// fragments; result r is P row 4 (l / 16) + r, Q row l % 16.
+// 16 x 16 results from 16-byte fragments: lane l holds row l % 16 and chunk
+// l / 16 of a fragment's four; result r of a lane is P row 4 (l / 16) + r,
+// Q row l % 16.  (Results of 32 x 32 would need half as many instructions for
+// the same reads of LDS, but move more accumulator registers: the product of
+// 8192 x 4096 x 4096 took 220 us with them, 205 with these.)
 template <typename E>
 struct Mma;
 template <>
 struct Mma<bf16> {
-    typedef f16v Big;
-    typedef f4 Small;
-    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bits_as<bf8>(a), bits_as<bf8>(b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+    typedef f4 Sum;
+    static __device__ __forceinline__ Sum multiply(u4 a, u4 b, Sum c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<bf8>(a), bits_as<bf8>(b), c, 0, 0, 0);
     }
 };
 template <>
 struct Mma<f16> {
-    typedef f16v Big;
-    typedef f4 Small;
-    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(bits_as<h8>(a), bits_as<h8>(b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+    typedef f4 Sum;
+    static __device__ __forceinline__ Sum multiply(u4 a, u4 b, Sum c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<h8>(a), bits_as<h8>(b), c, 0, 0, 0);
     }
 };
 template <>
 struct Mma<float> {
-    typedef f16v Big;
-    typedef f4 Small;
-    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
-        const f4 x = bits_as<f4>(a), y = bits_as<f4>(b);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], y[j], c, 0, 0, 0);
-        return c;
-    }
-    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+    typedef f4 Sum;
+    static __device__ __forceinline__ Sum multiply(u4 a, u4 b, Sum c) {
         const f4 x = bits_as<f4>(a), y = bits_as<f4>(b);
 #pragma unroll
         for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
@@ -86,12 +70,8 @@ struct Mma<float> {
 };
 template <>
 struct Mma<int8_t> {
-    typedef i16v Big;
-    typedef i4 Small;
-    static __device__ __forceinline__ Big big(u4 a, u4 b, Big c) {
-        return __builtin_amdgcn_mfma_i32_32x32x32_i8(bits_as<i4>(a), bits_as<i4>(b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ Small small(u4 a, u4 b, Small c) {
+    typedef i4 Sum;
+    static __device__ __forceinline__ Sum multiply(u4 a, u4 b, Sum c) {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(bits_as<i4>(a), bits_as<i4>(b), c, 0, 0, 0);
     }
 };
@@ -202,17 +182,18 @@ struct TileLoad<E, false, R, THREADS> {
             off[n] = min(id / kRowChunks, rows - row0 - 1) * (uint32_t)stride + id % kRowChunks * CE;
         }
     }
-    __device__ __forceinline__ void load(Regs& g, uint32_t step, uint32_t k_left) const {
+    __device__ __forceinline__ void load_whole(Regs& g, uint32_t step) const {
         const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E));
-        if (k_left >= kStepBytes / sizeof(E)) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) g.r[n] = bits_as<u4>(load_pack<CE>(at + off[n]));
-        } else {
+        for (int n = 0; n < N; ++n) g.r[n] = bits_as<u4>(load_pack<CE>(at + off[n]));
+    }
+    __device__ __forceinline__ void load(Regs& g, uint32_t step, uint32_t k_left) const {
+        if (k_left >= kStepBytes / sizeof(E)) return load_whole(g, step);
+        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E));
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int have = (int)k_left - (int)((n * THREADS + threadIdx.x) % kRowChunks * CE);
-                g.r[n] = bits_as<u4>(load_some<CE>(at + off[n], have));
-            }
+        for (int n = 0; n < N; ++n) {
+            const int have = (int)k_left - (int)((n * THREADS + threadIdx.x) % kRowChunks * CE);
+            g.r[n] = bits_as<u4>(load_some<CE>(at + off[n], have));
         }
     }
     __device__ __forceinline__ void store(const Regs& g, char* lds) const {
@@ -244,21 +225,25 @@ struct TileLoad<E, true, R, THREADS> {
 #pragma unroll
         for (int n = 0; n < N; ++n) cols[n] = (int)(rows - row0) - (int)(group(n) * 4);
     }
+    __device__ __forceinline__ void load_whole(Regs& g, uint32_t step) const {
+        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E)) * stride;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
+            const uint32_t off = chunk(n) * CE * (uint32_t)stride + group(n) * 4;
+#pragma unroll
+            for (int e = 0; e < CE; ++e) g.r[n][e] = load_pack<4>(at + (uint64_t)e * stride + off);
+        }
+    }
     __device__ __forceinline__ void load(Regs& g, uint32_t step, uint32_t k_left) const {
         const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E)) * stride;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
             const uint32_t off = chunk(n) * CE * (uint32_t)stride + group(n) * 4;
-            if (k_left >= kStepBytes / sizeof(E) && cols[n] >= 4) {
 #pragma unroll
-                for (int e = 0; e < CE; ++e) g.r[n][e] = load_pack<4>(at + (uint64_t)e * stride + off);
-            } else {
-#pragma unroll
-                for (int e = 0; e < CE; ++e)
-                    g.r[n][e] = load_some<4>(at + (uint64_t)e * stride + off,
-                                             chunk(n) * CE + e < k_left ? cols[n] : 0);
-            }
+            for (int e = 0; e < CE; ++e)
+                g.r[n][e] = load_some<4>(at + (uint64_t)e * stride + off, chunk(n) * CE + e < k_left ? cols[n] : 0);
         }
     }
     __device__ __forceinline__ void store(const Regs& g, char* lds) const {
@@ -276,18 +261,18 @@ struct TileLoad<E, true, R, THREADS> {
     }
 };
 
-// WI x WJ waves of NI x NJ 32 x 32 results each.
+// WI x WJ waves of NI x NJ 16 x 16 results each.
 template <int WI_, int WJ_, int NI_, int NJ_>
 struct Tile {
     static constexpr int WI = WI_, WJ = WJ_, NI = NI_, NJ = NJ_;
-    static constexpr int BI = WI * NI * 32, BJ = WJ * NJ * 32, kThreads = WI * WJ * kWave;
+    static constexpr int BI = WI * NI * 16, BJ = WJ * NJ * 16, kThreads = WI * WJ * kWave;
     static constexpr int kStage = (BI + BJ) * kStepBytes;           // bytes of LDS of one step
     static constexpr int kLds = 2 * kStage;
-    static_assert(WI * WJ * NI * 32 * 32 * 4 <= kLds, "the epilogue's rows fit where the operands were");
+    static_assert(WI * WJ * NI * 16 * 32 * 4 <= kLds && NJ % 2 == 0, "the epilogue's rows fit where the operands were");
 };
-typedef Tile<2, 4, 4, 2> TileBig;
-typedef Tile<2, 2, 2, 2> TileMid;
-typedef Tile<2, 2, 1, 1> TileSmall;
+typedef Tile<2, 4, 8, 4> TileBig;
+typedef Tile<2, 2, 4, 4> TileMid;
+typedef Tile<2, 2, 2, 2> TileSmall;
 
 // The tile of block b: blocks go to the eight dies in turn, so each die is
 // given a run of neighbouring tiles, and a run goes through 8 tiles along j
@@ -304,29 +289,26 @@ __device__ __forceinline__ void tile_of(const GemmArgs& a, uint32_t b, uint32_t&
 // The block's sums to their results.  A wave's go through LDS, 32 rows j of
 // all its i at a time, so that it reads and writes whole runs of memory.
 template <typename E, typename O, typename TL>
-__device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::Big (&acc)[TL::NI][TL::NJ], char* lds,
+__device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::Sum (&acc)[TL::NI][TL::NJ], char* lds,
                                            uint32_t i0, uint32_t j0) {
     const uint32_t wave = wave_index(), lane = lane_id(), wi = wave % TL::WI, wj = wave / TL::WI;
-    constexpr int W = TL::NI * 32;  // results of a row
+    constexpr int W = TL::NI * 16;  // results of a row
     float* rows = (float*)(lds + wave * (W * 32 * 4));
     constexpr int kPer = 8, kLanes = W / kPer, kAtOnce = kWave / kLanes;
 #pragma unroll
-    for (int j = 0; j < TL::NJ; ++j) {
+    for (int j = 0; j < TL::NJ / 2; ++j) {
 #pragma unroll
         for (int i = 0; i < TL::NI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f4 v;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = bits_as<float>(acc[i][j][r * 4 + c]);
-                const uint32_t col = i * 32 + r * 8 + (lane >> 5) * 4;
-                *(f4*)(rows + (lane & 31) * W + (col ^ ((lane & 7) << 2))) = v;
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t col = i * 16 + (lane >> 4) * 4, row = h * 16 + (lane & 15);
+                *(f4*)(rows + row * W + (col ^ ((row & 7) << 2))) = bits_as<f4>(acc[i][j * 2 + h]);
             }
         wave_lds_sync();
         const uint32_t col = lane % kLanes * kPer, i = i0 + wi * W + col;
 #pragma unroll 1
         for (uint32_t r = lane / kLanes; r < 32; r += kAtOnce) {
-            const uint32_t row = j0 + (wj * TL::NJ + j) * 32 + r;
+            const uint32_t row = j0 + wj * TL::NJ * 16 + j * 32 + r;
             float s[kPer];
             const f4 lo = *(const f4*)(rows + r * W + (col ^ ((r & 7) << 2)));
             const f4 hi = *(const f4*)(rows + r * W + ((col + 4) ^ ((r & 7) << 2)));
@@ -352,7 +334,7 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::B
 }
 
 template <typename E, typename O, bool PA, bool QA, typename TL, int SETS = 2>
-__global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
+__global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
     using M = Mma<E>;
     __shared__ __align__(16) char lds[TL::kLds];
     constexpr uint32_t KE = kStepBytes / sizeof(E);
@@ -367,30 +349,33 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
     TileLoad<E, QA, TL::BJ, TL::kThreads> lq;
     lp.start(a.p, a.p_stride, i0, a.I, k0);
     lq.start(a.q, a.q_stride, j0, a.J, k0);
-    typename M::Big acc[TL::NI][TL::NJ];
+    typename M::Sum acc[TL::NI][TL::NJ];
 #pragma unroll
     for (int i = 0; i < TL::NI; ++i)
 #pragma unroll
         for (int j = 0; j < TL::NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = 0;
 
     const uint32_t wave = wave_index(), lane = lane_id();
     const uint32_t wi = wave % TL::WI, wj = wave / TL::WI;
     // this lane's fragment of row r, chunk pair s: the row's bits 0..4 set the chunk's place
-    const uint32_t at = chunk_at(lane & 31, lane >> 5);
-    const uint32_t p_at = wi * TL::NI * 32 * kStepBytes + at;
-    const uint32_t q_at = TL::BI * kStepBytes + wj * TL::NJ * 32 * kStepBytes + at;
+    const uint32_t at = chunk_at(lane & 15, lane >> 4);
+    const uint32_t p_at = wi * TL::NI * 16 * kStepBytes + at;
+    const uint32_t q_at = TL::BI * kStepBytes + wj * TL::NJ * 16 * kStepBytes + at;
 
     typename decltype(lp)::Regs rp[SETS];
     typename decltype(lq)::Regs rq[SETS];
+    const uint32_t left = k_end > k0 ? k_end - k0 : 0;
+    // steps whose every load is a whole vector: those of whole length, in tiles with no ragged edge across k
+    const bool edge = (PA && a.I - i0 < (uint32_t)TL::BI) || (QA && a.J - j0 < (uint32_t)TL::BJ);
+    const uint32_t whole = edge ? 0 : left / KE;
     const auto load = [&](int set, uint32_t s) {
         if (s >= steps) return;
-        lp.load(rp[set], s, k_end - k0 - s * KE);
-        lq.load(rq[set], s, k_end - k0 - s * KE);
+        lp.load(rp[set], s, left - s * KE);
+        lq.load(rq[set], s, left - s * KE);
     };
     const auto store = [&](int set, uint32_t s) {
-        if (s >= steps) return;
         char* to = lds + (s & 1) * TL::kStage;
         lp.store(rp[set], to);
         lq.store(rq[set], to + TL::BI * kStepBytes);
@@ -399,31 +384,45 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
         const char* now = lds + (s & 1) * TL::kStage;
         u4 p[TL::NI], q[TL::NJ];
 #pragma unroll
-        for (int i = 0; i < TL::NI; ++i) p[i] = *(const u4*)(now + ((p_at ^ (c << 5)) + i * 32 * kStepBytes));
+        for (int i = 0; i < TL::NI; ++i)
+            p[i] = *(const u4*)(now + (((p_at ^ (c << 6)) ^ ((i & 1) << 5)) + i * 16 * kStepBytes));
 #pragma unroll
-        for (int j = 0; j < TL::NJ; ++j) q[j] = *(const u4*)(now + ((q_at ^ (c << 5)) + j * 32 * kStepBytes));
+        for (int j = 0; j < TL::NJ; ++j)
+            q[j] = *(const u4*)(now + (((q_at ^ (c << 6)) ^ ((j & 1) << 5)) + j * 16 * kStepBytes));
 #pragma unroll
         for (int i = 0; i < TL::NI; ++i)
 #pragma unroll
-            for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::big(p[i], q[j], acc[i][j]);
+            for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::multiply(p[i], q[j], acc[i][j]);
     };
     // step s multiplies what LDS holds, stores step s + 1, loaded SETS steps
     // ago, to the other half, and loads into its registers anew
-    load(0, 0);
-    store(0, 0);
+    if (steps) {
+        load(0, 0);
+        store(0, 0);
 #pragma unroll
-    for (int d = 0; d < SETS; ++d) load(d, d + 1);
+        for (int d = 0; d < SETS; ++d) load(d, d + 1);
+    }
     __syncthreads();
-    for (uint32_t s0 = 0; s0 < steps; s0 += SETS)
+    uint32_t s = 0;
+    for (; s + 2 * SETS < whole; s += SETS)
 #pragma unroll
         for (int d = 0; d < SETS; ++d) {
-            const uint32_t s = s0 + d;
-            if (SETS > 1 && s >= steps) break;
-            multiply(s, 0);
-            store(d, s + 1);
-            load(d, s + 1 + SETS);
+            multiply(s + d, 0);
+            store(d, s + d + 1);
+            lp.load_whole(rp[d], s + d + 1 + SETS);
+            lq.load_whole(rq[d], s + d + 1 + SETS);
+            multiply(s + d, 1);
+            __syncthreads();
+        }
+#pragma unroll 1
+    for (; s < steps; s += SETS)
 #pragma unroll
-            for (int c = 1; c < kRowChunks / 2; ++c) multiply(s, c);
+        for (int d = 0; d < SETS; ++d) {
+            if (s + d >= steps) break;
+            multiply(s + d, 0);
+            if (s + d + 1 < steps) store(d, s + d + 1);
+            load(d, s + d + 1 + SETS);
+            multiply(s + d, 1);
             __syncthreads();
         }
 
@@ -432,21 +431,20 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm(GemmArgs a) {
 
 // ---- The same product with operands that memory instructions place in LDS ----
 //
-// For 16- and 8-bit operands whose rows start and end at 16-byte boundaries.
-// A step is 64 bytes of k; four steps have room in LDS.  While step s is
-// multiplied, steps s + 2 to s + 4 are on their way from memory straight into
-// LDS, in no register, and step s + 1 is there: its first fragments are read
-// behind the last products of step s.  One barrier a step both shows that
-// step s + 1 has come for every wave and frees the room of step s.
+// For 16- and 8-bit operands whose rows start at 16-byte boundaries and whose
+// last 16 bytes may be read whole (along k with zeros behind the end of k):
+// the caller's where their sizes are so, else copies made by k_pad.
+// LDS has room for two steps.  While step s is multiplied, step s + 1 is on
+// its way from memory straight into LDS, in no register; one barrier, behind
+// the last reads of step s, both shows that step s + 1 has come for every
+// wave and frees the room of step s for step s + 2.  Each fragment is read
+// right behind the last use of the one whose registers it takes.
 //
-// Along k a row's four 16-byte chunks change places by the row's bits 2 and 3.
+// Along k a row's eight 16-byte chunks change places by the row's low bits.
 // Across k the tile lies in LDS as in memory, a row for each k, and the
 // transposing LDS read gives each lane four k of one row; pairs of 16-byte
 // chunks change places by the low bits of k.  A load puts its lanes' data
 // side by side, so the places are chosen by what each lane fetches.
-constexpr int kLineBytes = 64;  // of k in a step
-constexpr int kDeep = 4;        // steps in LDS
-
 static __device__ const u4 zero_chunk = {0, 0, 0, 0};  // what lanes past the end of k fetch
 
 // 16 bytes from base + off to each lane's place after lds_at (uniform).  The
@@ -466,9 +464,9 @@ __device__ __forceinline__ void load_wait() {
 
 template <typename E, bool ACROSS, int R, int THREADS>
 struct TileFetch {
-    static constexpr int kBytes = R * kLineBytes, N = kBytes / (THREADS * 16), KE = kLineBytes / sizeof(E);
+    static constexpr int kBytes = R * kStepBytes, N = kBytes / (THREADS * 16), KE = kStepBytes / sizeof(E);
     static constexpr int CE = 16 / sizeof(E);
-    static constexpr int kRowBytes = ACROSS ? R * (int)sizeof(E) : kLineBytes;
+    static constexpr int kRowBytes = ACROSS ? R * (int)sizeof(E) : kStepBytes;
     static constexpr int kUnits = kRowBytes / 32;  // across: pairs of chunks of a k
     static_assert(kBytes % (THREADS * 16) == 0 && (!ACROSS || sizeof(E) == 2));
     const E* base;      // the tile's first row at the first step's k
@@ -481,13 +479,16 @@ struct TileFetch {
         return (n * (THREADS / kWave) + wave_index()) * kWave * 16 + lane_id() * 16;
     }
     static __device__ __forceinline__ uint32_t place(uint32_t k) { return kUnits >= 8 ? (k & 3) << 1 : k & 3; }
+    static __device__ __forceinline__ uint32_t row_place(uint32_t row) {
+        return (row & 7) ^ ((row >> 3) & 1);
+    }
     static __device__ __forceinline__ uint32_t k_of(int n) {
         if constexpr (ACROSS) return at(n) / kRowBytes;
-        const uint32_t row = at(n) / kLineBytes;
-        return ((at(n) / 16 % 4) ^ ((row >> 2) & 3)) * CE;
+        const uint32_t row = at(n) / kStepBytes;
+        return ((at(n) / 16 % (kStepBytes / 16)) ^ row_place(row)) * CE;
     }
     static __device__ __forceinline__ uint32_t row_of(int n) {
-        if constexpr (!ACROSS) return at(n) / kLineBytes;
+        if constexpr (!ACROSS) return at(n) / kStepBytes;
         const uint32_t chunk = at(n) % kRowBytes / 16;
         return ((chunk >> 1) ^ place(k_of(n))) * 16 + (chunk & 1) * 8;
     }
@@ -495,7 +496,8 @@ struct TileFetch {
         stride = (uint32_t)st;
         base = (const E*)p + (ACROSS ? (uint64_t)k0 * st + row0 : (uint64_t)row0 * st + k0);
         per_step = (ACROSS ? KE * st : KE) * sizeof(E);
-        const uint32_t last = rows - row0 - (ACROSS ? 8 : 1);  // rows past the end repeat the last; their results are dropped
+        // rows past the end repeat the last; their results are dropped
+        const uint32_t last = ACROSS ? (rows + CE - 1) / CE * CE - row0 - CE : rows - row0 - 1;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const uint32_t r = min(row_of(n), last);
@@ -518,11 +520,11 @@ struct TileFetch {
     static __device__ __forceinline__ uint32_t lane_at(int c) {
         const uint32_t l = lane_id();
         if constexpr (ACROSS) {
-            const uint32_t k = c * 16 + (l >> 5) * 8 + l % 16 / 4, unit = (l >> 4) & 1;
-            return k * kRowBytes + ((unit ^ place(k)) << 5) + l % 4 * 8;
+            const uint32_t k = c * 32 + (l >> 4) * 8 + l % 16 / 4;
+            return k * kRowBytes + (place(k) << 5) + l % 4 * 8;
         }
-        const uint32_t row = l & 31;
-        return row * kLineBytes + (((c * 2 + (l >> 5)) ^ ((row >> 2) & 3)) << 4);
+        const uint32_t row = l & 15;
+        return row * kStepBytes + (((c * 4 + (l >> 4)) ^ row_place(row)) << 4);
     }
     // The fragment of rows row0 (a multiple of 32) on; lane is lane_at(c), the tile starts at `tile` in LDS.
     static __device__ __forceinline__ u4 fragment(const char* tile, uint32_t row0, uint32_t lane) {
@@ -538,103 +540,139 @@ struct TileFetch {
             __builtin_memcpy((char*)&v + 8, &hi, 8);
             return v;
         }
-        return *(const u4*)(tile + row0 * kLineBytes + lane);
+        return *(const u4*)(tile + row0 * kStepBytes + lane);
     }
 };
+
+// A copy of an operand's rows at 16-byte boundaries, zeros behind their ends: 16 bytes a thread.
+template <typename E>
+__global__ __launch_bounds__(kBlock) void k_pad(const E* from, uint64_t stride, uint64_t rows, uint32_t columns, E* to) {
+    constexpr uint32_t CE = 16 / sizeof(E);
+    const uint32_t per_row = (columns + CE - 1) / CE;
+    const uint64_t all = rows * per_row;
+    for (uint64_t t = (uint64_t)blockIdx.x * kBlock + threadIdx.x; t < all; t += (uint64_t)gridDim.x * kBlock) {
+        const uint64_t row = t / per_row;
+        const uint32_t c = (uint32_t)(t - row * per_row) * CE;
+        store_pack<CE>(to + t * CE, load_some<CE>(from + row * stride + c, (int)(columns - c)));
+    }
+}
 
 template <typename E, typename O, bool PA, bool QA, typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
     using M = Mma<E>;
     using FP = TileFetch<E, PA, TL::BI, TL::kThreads>;
     using FQ = TileFetch<E, QA, TL::BJ, TL::kThreads>;
-    constexpr int kStage = (TL::BI + TL::BJ) * kLineBytes, kLoads = FP::N + FQ::N;
-    __shared__ __align__(1024) char lds[kDeep * kStage];
-    static_assert(TL::kLds <= kDeep * kStage, "the epilogue's rows fit");
+    static_assert(FP::kBytes + FQ::kBytes == TL::kStage);
+    __shared__ __align__(1024) char lds[TL::kLds];
     uint32_t ti, tj;
     tile_of(a, blockIdx.x, ti, tj);
     const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
     const uint32_t k0 = blockIdx.y * a.steps * FP::KE;
     const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * FP::KE);
-    const uint32_t steps = k_end > k0 ? (k_end - k0 + FP::KE - 1) / FP::KE : 0;
+    const uint32_t left = k_end > k0 ? k_end - k0 : 0, steps = (left + FP::KE - 1) / FP::KE, whole = left / FP::KE;
     FP fp;
     FQ fq;
     fp.start(a.p, a.p_stride, i0, a.I, k0);
     fq.start(a.q, a.q_stride, j0, a.J, k0);
-    typename M::Big acc[TL::NI][TL::NJ];
+    typename M::Sum acc[TL::NI][TL::NJ];
 #pragma unroll
     for (int i = 0; i < TL::NI; ++i)
 #pragma unroll
         for (int j = 0; j < TL::NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = 0;
 
     const uint32_t wave = wave_index(), wi = wave % TL::WI, wj = wave / TL::WI;
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     uint32_t p_at[2], q_at[2];
 #pragma unroll
     for (int c = 0; c < 2; ++c) p_at[c] = FP::lane_at(c), q_at[c] = FQ::lane_at(c);
-    const uint32_t whole = k_end > k0 ? (k_end - k0) / FP::KE : 0;
-    const auto issue_whole = [&](uint32_t s) {
-        const uint32_t to = lds_at + s % kDeep * kStage;
-        fp.template issue<true>(s, 0, to);
-        fq.template issue<true>(s, 0, to + FP::kBytes);
-    };
     const auto issue = [&](uint32_t s) {
-        if (s < whole) return issue_whole(s);
-        const uint32_t to = lds_at + s % kDeep * kStage, left = k_end - k0 - s * FP::KE;
-        fp.template issue<false>(s, left, to);
-        fq.template issue<false>(s, left, to + FP::kBytes);
+        if (s >= steps) return;
+        const uint32_t to = lds_at + (s & 1) * TL::kStage;
+        if (s < whole) {
+            fp.template issue<true>(s, 0, to);
+            fq.template issue<true>(s, 0, to + FP::kBytes);
+        } else {
+            fp.template issue<false>(s, left - s * FP::KE, to);
+            fq.template issue<false>(s, left - s * FP::KE, to + FP::kBytes);
+        }
     };
-    const auto read = [&](uint32_t s, int c, u4 (&p)[TL::NI], u4 (&q)[TL::NJ]) {
-        const char* now = lds + s % kDeep * kStage;
-#pragma unroll
-        for (int i = 0; i < TL::NI; ++i) p[i] = FP::fragment(now, (wi * TL::NI + i) * 32, p_at[c]);
-#pragma unroll
-        for (int j = 0; j < TL::NJ; ++j) q[j] = FQ::fragment(now + FP::kBytes, (wj * TL::NJ + j) * 32, q_at[c]);
+    u4 p[TL::NI], qa[TL::NJ], qb[TL::NJ];
+    const auto read_p = [&](uint32_t s, int c, int i) {
+        p[i] = FP::fragment(lds + (s & 1) * TL::kStage, (wi * TL::NI + i) * 16, p_at[c]);
     };
-    const auto multiply = [&](const u4 (&p)[TL::NI], const u4 (&q)[TL::NJ]) {
-#pragma unroll
-        for (int i = 0; i < TL::NI; ++i)
-#pragma unroll
-            for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::big(p[i], q[j], acc[i][j]);
+    const auto read_q = [&](uint32_t s, int c, int j) {
+        return FQ::fragment(lds + (s & 1) * TL::kStage + FP::kBytes, (wj * TL::NJ + j) * 16, q_at[c]);
     };
-    // steps s + 1 on may be under way up to the last that was issued
-    const auto wait_for = [&](uint32_t s) {
-        const uint32_t after = min(steps - 1 - s, 2u);
-        if (after == 2)
-            load_wait<2 * kLoads>();
-        else if (after == 1)
-            load_wait<kLoads>();
+    // The products of p and q; each fragment of group nc of step ns is read behind the last use of the one whose
+    // place it takes.  `before` comes before the first read, more(m) behind product m.
+    const auto group = [&](uint32_t ns, int nc, u4 (&nq)[TL::NJ], const u4 (&q)[TL::NJ], auto before, auto more) {
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i) {
+#pragma unroll
+            for (int j = 0; j < TL::NJ; ++j) {
+                acc[i][j] = M::multiply(p[i], q[j], acc[i][j]);
+                more(i * TL::NJ + j);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (i == 0) before();
+            read_p(ns, nc, i);
+#pragma unroll
+            for (int j = 0; j < TL::NJ; ++j)
+                if (min(j, TL::NI - 1) == i) nq[j] = read_q(ns, nc, j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const auto nothing = [] {};
+    const auto no_more = [](int) {};
+    if (steps) {
+        issue(0);
+        issue(1);
+        if (steps > 1)
+            load_wait<FP::N + FQ::N>();
         else
             load_wait<0>();
-    };
-    u4 pa[TL::NI], qa[TL::NJ], pb[TL::NI], qb[TL::NJ];
-    if (steps) {
-#pragma unroll 1
-        for (uint32_t s = 0; s < min(steps, kDeep - 1u); ++s) issue(s);
-        wait_for(0);
-        if (kDeep - 1 < steps) issue(kDeep - 1);
-        read(0, 0, pa, qa);
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i) read_p(0, 0, i);
+#pragma unroll
+        for (int j = 0; j < TL::NJ; ++j) qa[j] = read_q(0, 0, j);
     }
     uint32_t s = 0;
-    for (; s + kDeep < whole; ++s) {
-        read(s, 1, pb, qb);
-        multiply(pa, qa);
-        load_wait<2 * kLoads>();
-        issue_whole(s + kDeep);
-        read(s + 1, 0, pa, qa);
-        multiply(pb, qb);
+    for (; s + 2 < whole; ++s) {
+        group(s, 1, qb, qa, nothing, no_more);
+        const char* from_p = (const char*)fp.base + (s + 2) * fp.per_step;
+        const char* from_q = (const char*)fq.base + (s + 2) * fq.per_step;
+        const uint32_t to = lds_at + (s & 1) * TL::kStage;
+        // the loads are spread over the group: side by side they would hold up its reads of LDS
+        group(s + 1, 0, qa, qb, [] { load_wait<0>(); }, [&](int m) {
+            constexpr int kLoads = FP::N + FQ::N, kRoom = TL::NI * TL::NJ - TL::NJ;
+#pragma unroll
+            for (int d = 0; d < kLoads; ++d) {
+                if (TL::NJ + d * kRoom / kLoads != m) continue;
+                if (d < FP::N)
+                    fetch(from_p, fp.off[d], to + (d * (TL::kThreads / kWave) + wave) * kWave * 16);
+                else
+                    fetch(from_q, fq.off[d - FP::N],
+                          to + FP::kBytes + ((d - FP::N) * (TL::kThreads / kWave) + wave) * kWave * 16);
+            }
+        });
     }
 #pragma unroll 1
     for (; s < steps; ++s) {
-        read(s, 1, pb, qb);
-        multiply(pa, qa);
+        group(s, 1, qb, qa, nothing, no_more);
+#pragma unroll
+        for (int i = 0; i < TL::NI; ++i)
+#pragma unroll
+            for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::multiply(p[i], qb[j], acc[i][j]);
         if (s + 1 < steps) {
-            wait_for(s + 1);
-            if (s + kDeep < steps) issue(s + kDeep);
-            read(s + 1, 0, pa, qa);
+            load_wait<0>();
+            issue(s + 2);
+#pragma unroll
+            for (int i = 0; i < TL::NI; ++i) read_p(s + 1, 0, i);
+#pragma unroll
+            for (int j = 0; j < TL::NJ; ++j) qa[j] = read_q(s + 1, 0, j);
         }
-        multiply(pb, qb);
     }
     __syncthreads();
     store_tile<E, O, TL>(a, acc, lds, i0, j0);
@@ -690,7 +728,7 @@ __global__ __launch_bounds__(kThinWaves* kWave) void k_thin(GemmArgs a) {
     const uint32_t whole = a.K / KE, share = (whole + kThinWaves - 1) / kThinWaves;
     uint32_t s = min(wave * share, whole);
     const uint32_t end = min(s + share, whole);
-    typename M::Small acc = {0, 0, 0, 0};
+    typename M::Sum acc = {0, 0, 0, 0};
     for (; s + kThinDeep <= end; s += kThinDeep) {
         u4 x[kThinDeep], y[kThinDeep];
 #pragma unroll
@@ -698,14 +736,14 @@ __global__ __launch_bounds__(kThinWaves* kWave) void k_thin(GemmArgs a) {
 #pragma unroll
         for (int d = 0; d < kThinDeep; ++d) y[d] = bits_as<u4>(load_pack<CE>(q + (uint64_t)(s + d) * KE));
 #pragma unroll
-        for (int d = 0; d < kThinDeep; ++d) acc = M::small(x[d], y[d], acc);
+        for (int d = 0; d < kThinDeep; ++d) acc = M::multiply(x[d], y[d], acc);
     }
     for (; s < end; ++s)
-        acc = M::small(bits_as<u4>(load_pack<CE>(p + (uint64_t)s * KE)), bits_as<u4>(load_pack<CE>(q + (uint64_t)s * KE)),
+        acc = M::multiply(bits_as<u4>(load_pack<CE>(p + (uint64_t)s * KE)), bits_as<u4>(load_pack<CE>(q + (uint64_t)s * KE)),
                        acc);
     if (wave == kThinWaves - 1 && whole * KE < a.K) {  // what is left of k
         const int have = (int)(a.K - whole * KE) - (int)(lane / 16 * CE);
-        acc = M::small(bits_as<u4>(load_some<CE>(p + (uint64_t)whole * KE, have)),
+        acc = M::multiply(bits_as<u4>(load_some<CE>(p + (uint64_t)whole * KE, have)),
                        bits_as<u4>(load_some<CE>(q + (uint64_t)whole * KE, have)), acc);
     }
     lds[wave][lane] = bits_as<f4>(acc);
@@ -736,9 +774,16 @@ __global__ __launch_bounds__(kThinWaves* kWave) void k_thin(GemmArgs a) {
 // Which operands lie across k.
 enum GemmForm { kAlong = 0, kPAcross = 1, kBothAcross = 2 };
 
-// One product, its sums in `room` floats at a.part where k is split.  Operand
-// types: E is O's type, or int8 with kAlong.
+// Scratch of a product: `floats` for sums where k is split (at GemmArgs::part),
+// and room for padded copies of operands (none: null).
+struct GemmRoom {
+    uint64_t floats;
+    char* pad;
+    uint64_t pad_bytes;
+};
+
+// One product.  Operand types: E is O's type, or int8 with kAlong.
 template <typename E, typename O, int FORM>
-hipError_t launch_gemm(GemmArgs a, uint64_t room, hipStream_t st);
+hipError_t launch_gemm(GemmArgs a, const GemmRoom& room, hipStream_t st);
 
 }  // namespace gd

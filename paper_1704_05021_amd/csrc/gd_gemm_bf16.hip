@@ -4,8 +4,8 @@
 #include "gd_gemm_launch.hpp"
 
 namespace gd {
-template hipError_t launch_gemm<bf16, bf16, kAlong>(GemmArgs, uint64_t, hipStream_t);
-template hipError_t launch_gemm<bf16, bf16, kPAcross>(GemmArgs, uint64_t, hipStream_t);
-template hipError_t launch_gemm<bf16, float, kBothAcross>(GemmArgs, uint64_t, hipStream_t);
-template hipError_t launch_gemm<int8_t, bf16, kAlong>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<bf16, bf16, kAlong>(GemmArgs, const GemmRoom&, hipStream_t);
+template hipError_t launch_gemm<bf16, bf16, kPAcross>(GemmArgs, const GemmRoom&, hipStream_t);
+template hipError_t launch_gemm<bf16, float, kBothAcross>(GemmArgs, const GemmRoom&, hipStream_t);
+template hipError_t launch_gemm<int8_t, bf16, kAlong>(GemmArgs, const GemmRoom&, hipStream_t);
 }  // namespace gd

@@ -4,8 +4,8 @@
 #include "gd_gemm_launch.hpp"
 
 namespace gd {
-template hipError_t launch_gemm<float, float, kAlong>(GemmArgs, uint64_t, hipStream_t);
-template hipError_t launch_gemm<float, float, kPAcross>(GemmArgs, uint64_t, hipStream_t);
-template hipError_t launch_gemm<float, float, kBothAcross>(GemmArgs, uint64_t, hipStream_t);
-template hipError_t launch_gemm<int8_t, float, kAlong>(GemmArgs, uint64_t, hipStream_t);
+template hipError_t launch_gemm<float, float, kAlong>(GemmArgs, const GemmRoom&, hipStream_t);
+template hipError_t launch_gemm<float, float, kPAcross>(GemmArgs, const GemmRoom&, hipStream_t);
+template hipError_t launch_gemm<float, float, kBothAcross>(GemmArgs, const GemmRoom&, hipStream_t);
+template hipError_t launch_gemm<int8_t, float, kAlong>(GemmArgs, const GemmRoom&, hipStream_t);
 }  // namespace gd

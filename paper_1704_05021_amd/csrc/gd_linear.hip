@@ -11,6 +11,7 @@ namespace gd {
 
 constexpr uint64_t kLinearRoom = 8ull << 20;  // floats of partial sums of a product
 constexpr uint32_t kLinearMaxDim = 1u << 22, kLinearMaxInt8 = 1u << 17;
+constexpr uint64_t kLinearPad = 512ull << 20; // bytes of padded copies, at most
 constexpr uint32_t kBiasParts = 256;          // partial sums of the bias's gradient
 
 __device__ __forceinline__ float act_slope(int act, float z) {
@@ -80,15 +81,15 @@ hipError_t launch_slope(const gd_linear_grad& io, int type, uint32_t columns, in
 }
 
 template <typename T>
-hipError_t forward(const GemmArgs& a, bool int8, hipStream_t st) {
-    return int8 ? launch_gemm<int8_t, T, kAlong>(a, kLinearRoom, st) : launch_gemm<T, T, kAlong>(a, kLinearRoom, st);
+hipError_t forward(const GemmArgs& a, const GemmRoom& room, bool int8, hipStream_t st) {
+    return int8 ? launch_gemm<int8_t, T, kAlong>(a, room, st) : launch_gemm<T, T, kAlong>(a, room, st);
 }
 
 template <typename T>
-hipError_t backward(const GemmArgs* dx, const GemmArgs* dw, hipStream_t st) {
+hipError_t backward(const GemmArgs* dx, const GemmArgs* dw, const GemmRoom& room, hipStream_t st) {
     hipError_t e = hipSuccess;
-    if (dx) e = launch_gemm<T, T, kPAcross>(*dx, kLinearRoom, st);
-    if (dw && e == hipSuccess) e = launch_gemm<T, float, kBothAcross>(*dw, kLinearRoom, st);
+    if (dx) e = launch_gemm<T, T, kPAcross>(*dx, room, st);
+    if (dw && e == hipSuccess) e = launch_gemm<T, float, kBothAcross>(*dw, room, st);
     return e;
 }
 
@@ -101,6 +102,8 @@ struct gd_linear {
     uint64_t max_rows = 0;
     float* room = nullptr;  // [kLinearRoom]
     float* part = nullptr;  // [kBiasParts * out]
+    char* pad = nullptr;    // padded copies of operands, where in or out is no whole number of 16-byte chunks
+    uint64_t pad_bytes = 0;
     gd::DeviceMemory mem;
 };
 
@@ -121,11 +124,17 @@ gd_status gd_linear_create(gd_linear** out, uint32_t in, uint32_t out_features, 
     l->type = ty;
     l->act = ac;
     l->max_rows = max_rows;
+    if (ty != GD_F32 && (in % 8 || out_features % 8)) {
+        // the two operands of the forward call, of the input's gradient or of the weight's
+        const uint64_t k = (in + 7ull) / 8 * 16, n = (out_features + 7ull) / 8 * 16, w = out_features * k;
+        l->pad_bytes = std::min(std::max({max_rows * k + w, max_rows * n + w, max_rows * (k + n)}), gd::kLinearPad);
+    }
     gd_status st = GD_OK;
     try {
         if (hipGetDevice(&l->device) != hipSuccess) st = GD_ERR_HIP;
         else if (!l->mem.alloc(&l->room, gd::kLinearRoom) ||
-                 !l->mem.alloc(&l->part, (size_t)gd::kBiasParts * out_features))
+                 !l->mem.alloc(&l->part, (size_t)gd::kBiasParts * out_features) ||
+                 (l->pad_bytes && !l->mem.alloc(&l->pad, l->pad_bytes)))
             st = GD_ERR_OOM;
     } catch (const std::bad_alloc&) {
         st = GD_ERR_OOM;
@@ -177,9 +186,10 @@ gd_status gd_linear_forward(gd_linear* l, const gd_linear_io* io, void* stream) 
     a.fin.q_scale = io->x_scale;
     a.fin.act = l->act;
     const hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = l->type == GD_F32    ? gd::forward<float>(a, int8, st)
-                         : l->type == GD_BF16 ? gd::forward<gd::bf16>(a, int8, st)
-                                              : gd::forward<gd::f16>(a, int8, st);
+    const gd::GemmRoom room{gd::kLinearRoom, l->pad, l->pad_bytes};
+    const hipError_t e = l->type == GD_F32    ? gd::forward<float>(a, room, int8, st)
+                         : l->type == GD_BF16 ? gd::forward<gd::bf16>(a, room, int8, st)
+                                              : gd::forward<gd::f16>(a, room, int8, st);
     return e == hipSuccess ? GD_OK : GD_ERR_HIP;
 }
 
@@ -223,9 +233,10 @@ gd_status gd_linear_backward(gd_linear* l, const gd_linear_grad* io, void* strea
     dw.fin.accumulate = io->accumulate != 0;
     const gd::GemmArgs *want_dx = rows && io->dx ? &dx : nullptr,
                        *want_dw = io->dweight && (rows || !io->accumulate) ? &dw : nullptr;
-    const hipError_t e = l->type == GD_F32    ? gd::backward<float>(want_dx, want_dw, st)
-                         : l->type == GD_BF16 ? gd::backward<gd::bf16>(want_dx, want_dw, st)
-                                              : gd::backward<gd::f16>(want_dx, want_dw, st);
+    const gd::GemmRoom room{gd::kLinearRoom, l->pad, l->pad_bytes};
+    const hipError_t e = l->type == GD_F32    ? gd::backward<float>(want_dx, want_dw, room, st)
+                         : l->type == GD_BF16 ? gd::backward<gd::bf16>(want_dx, want_dw, room, st)
+                                              : gd::backward<gd::f16>(want_dx, want_dw, room, st);
     return e == hipSuccess ? GD_OK : GD_ERR_HIP;
 }
 

@@ -647,7 +647,7 @@ class Linear(_Handle):
     _what = "linear"
 
     def __init__(self, in_features: int, out_features: int, dtype: torch.dtype = torch.bfloat16, act: str = "none",
-                 max_rows: int = 65536, device=None):
+                 max_rows: int = 8192, device=None):
         if act not in ACTIVATIONS:
             raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, not {act!r}")
         self.inf, self.outf, self.dtype, self.act = int(in_features), int(out_features), dtype, act
