@@ -30,20 +30,50 @@ bool pad(const void*& p, uint64_t& stride, uint64_t rows, uint32_t columns, Gemm
     return true;
 }
 
+// What a tile costs, in microseconds, measured on products in bfloat16 with k
+// of 4,096 (64 steps): a step of one tile alone on its compute unit, and of
+// each of several there at once (as many as LDS holds).  Every round of tiles
+// also takes about kRoundUs to fill the pipeline and write results.
+struct TileCost {
+    uint32_t bi, bj, at_once;
+    double alone_us, shared_us;
+};
+constexpr TileCost kBigCost{256, 256, 1, 1.48, 1.48}, kLongCost{256, 192, 1, 1.10, 1.10}, kWideCost{256, 128, 1, 0.82, 0.82},
+    kMidCost{128, 128, 2, 0.58, 0.475}, kSmallCost{64, 64, 5, 0.30, 0.165};
+constexpr double kRoundUs = 5.0, kJoinUs = 4.0, kJoinBytesPerUs = 3.5e6;
+
+struct TilePlan {
+    double us;
+    uint32_t splits;
+};
+
+// The number of shares of k that a product of `steps` steps does best with, and its time: shares fill compute units
+// that the tiles leave idle, and cost the writing and reading of their sums.
+inline TilePlan plan_tiles(const TileCost& c, uint64_t I, uint64_t J, uint64_t steps, uint64_t room) {
+    const uint64_t tiles = ((I + c.bi - 1) / c.bi) * ((J + c.bj - 1) / c.bj);
+    const auto time = [&](uint64_t splits) {
+        const uint64_t each = (steps + splits - 1) / splits, load = (tiles * splits + kUnits - 1) / kUnits;
+        const auto round = [&](uint64_t n) {
+            return n ? (double)each * std::max(c.alone_us, (double)n * c.shared_us) + kRoundUs : 0.0;
+        };
+        const double join = splits > 1 ? kJoinUs + 8.0 * (double)(splits * I) * (double)J / kJoinBytesPerUs : 0.0;
+        return (double)(load / c.at_once) * round(c.at_once) + round(load % c.at_once) + join;
+    };
+    TilePlan best{time(1), 1};
+    for (uint64_t s = 2; s <= 64 && s * 4 <= steps && s * I * J <= room; s += s < 4 ? 1 : s / 4 * 2) {
+        const double us = time(s);
+        if (us < best.us) best = {us, (uint32_t)s};
+    }
+    return best;
+}
+
 template <typename E, typename O, int FORM, typename TL>
-hipError_t launch_tiles(GemmArgs a, uint64_t room, bool direct, hipStream_t st) {
+hipError_t launch_tiles(GemmArgs a, uint64_t splits, bool direct, hipStream_t st) {
     constexpr uint32_t KE = kStepBytes / sizeof(E);
     a.tiles_i = (a.I + TL::BI - 1) / TL::BI;
     a.tiles_j = (a.J + TL::BJ - 1) / TL::BJ;
     const uint64_t tiles = (uint64_t)a.tiles_i * a.tiles_j, steps = ((uint64_t)a.K + KE - 1) / KE;
     if (tiles * TL::kThreads > 0xFFFFFFFFull) return hipErrorInvalidValue;
-    // k is split where the tiles leave most of the compute units idle, into shares of at least four steps
-    uint64_t splits = 1;
-    if (tiles < kUnits) {
-        splits = std::min<uint64_t>(2 * kUnits / tiles, steps / 4);
-        splits = std::min<uint64_t>(splits, room / ((uint64_t)a.I * a.J));
-        splits = std::max<uint64_t>(splits, 1);
-    }
     a.steps = (uint32_t)((steps + splits - 1) / splits);
     if (a.steps) splits = (steps + a.steps - 1) / a.steps;
     float* part = a.part;
@@ -85,12 +115,22 @@ hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
             if (direct) a = b;
         }
     }
-    const auto tiles = [&](uint64_t b) { return ((a.I + b - 1) / b) * ((a.J + b - 1) / b); };
-    const uint64_t room = given.floats;
-    if constexpr (sizeof(E) <= 2)
-        if (direct && tiles(256) >= 200) return launch_tiles<E, O, FORM, TileBig>(a, room, direct, st);
-    if (tiles(128) >= 200) return launch_tiles<E, O, FORM, TileMid>(a, room, direct, st);
-    return launch_tiles<E, O, FORM, TileSmall>(a, room, direct, st);
+    constexpr uint32_t KE = kStepBytes / sizeof(E);
+    const uint64_t steps = ((uint64_t)a.K + KE - 1) / KE;
+    TilePlan best{1e300, 1};
+    int tile = 0;
+    constexpr TileCost kCosts[] = {kSmallCost, kMidCost, kWideCost, kLongCost, kBigCost};
+    for (int t = 0; t < (direct ? 5 : 2); ++t) {  // the larger tiles take operands placed in LDS only
+        const TilePlan p = plan_tiles(kCosts[t], a.I, a.J, steps, given.floats);
+        if (p.us < best.us) best = p, tile = t;
+    }
+    const auto run = [&](auto tl) { return launch_tiles<E, O, FORM, decltype(tl)>(a, best.splits, direct, st); };
+    if constexpr (sizeof(E) <= 2) {
+        if (tile == 4) return run(TileBig());
+        if (tile == 3) return run(TileLong());
+        if (tile == 2) return run(TileWide());
+    }
+    return tile == 1 ? run(TileMid()) : run(TileSmall());
 }
 
 }  // namespace gd
