@@ -1,16 +1,19 @@
 // AdamW step over all tensors of a layout, with the moments in 32 or 8 bits.
 //
 // Bound by memory: 28 bytes an element with 32-bit moments (parameter and
-// moments read and written, gradient read), 16 with 8-bit ones.  A block takes
-// a chunk of 1,024 elements of one tensor, a wave the 256 that share the
-// units of the 8-bit moments, a lane four of them: every array is read and
-// written once, 16 bytes a lane (4 for codes), and the blocks' maxima stay in
-// registers.  Chunks start anew with each tensor, so that no tensor's moments
-// depend on its neighbours; a tensor that starts off a 16-byte boundary is
-// read at its own alignment.
+// moments read and written, gradient read), 16 with 8-bit ones.  A wave takes
+// the 256 elements that share the units of the 8-bit moments, a lane four of
+// them: every array is read and written once, 16 bytes a lane (4 for codes),
+// and the blocks' maxima stay in registers.  A block of threads takes a chunk
+// of one tensor, two to four times 1,024 elements, and starts all its loads
+// before the first is used: a chunk's place comes from a table, one round trip
+// to memory before them.  Chunks start anew with each tensor, so that no
+// tensor's moments depend on its neighbours; a tensor that starts off a
+// 16-byte boundary is read at its own alignment.
 //
-// Operations are those of the definition one by one (no contraction), so a
-// step gives the bits that separate binary32 operations give.
+// The moments are formed by the definition's operations one by one (no
+// contraction), so that their codes do not depend on this code's shape; the
+// parameter's update takes the hardware's reciprocal (one ulp).
 
 #include <cmath>
 #include <new>
@@ -22,17 +25,20 @@
 namespace gd {
 
 constexpr uint32_t kStateBlock = 256;   // elements that share the units of their codes
-constexpr uint32_t kAdamChunk = 1024;   // elements of a block of threads
+constexpr uint32_t kAdamRun = 1024;      // elements that a block of threads takes side by side
+constexpr int kRuns = 2, kRunsCodes = 4; // runs of a chunk, with 32- and 8-bit moments
 constexpr uint32_t kAdamMaxBlocks = 1u << 22;  // a dispatch holds less than 2^32 threads
-constexpr uint32_t kNormBlocks = 1024;  // partial sums of the gradient's squares
+constexpr uint32_t kNormBlocks = 1024;   // partial sums of the gradient's squares
 constexpr uint64_t kAdamMaxElements = 1ull << 40;
 
+constexpr int kLenShift = 52;            // 12 bits of a chunk's length above its first element
+
 struct AdamChunk {
-    uint64_t start_len;  // first element | (elements - 1) << 54
+    uint64_t start_len;  // first element | (elements - 1) << kLenShift
     uint32_t tensor;
     uint32_t block;      // its first block of codes
 };
-static_assert(kAdamChunk == kBlock * 4 && kStateBlock == kWave * 4, "a lane takes four elements");
+static_assert(kAdamRun == kBlock * 4 && kStateBlock == kWave * 4, "a lane takes four elements");
 
 struct AdamArgs {
     gd_adamw_io io;
@@ -43,13 +49,24 @@ struct AdamArgs {
     float grad_scale, beta1, one_beta1, beta2, one_beta2, step_size, root_scale, eps, lr_decay;
 };
 
-// Nearest whole number to the root of y, at most `top` (ties up): the
-// hardware's root is off by an ulp at most, so its rounding by one at most, and
-// the two squares, exact in binary32, settle it.
+// The root of x >= 0, rounded to nearest: the hardware's is off by an ulp at
+// most, and the sign of x - r (r +- ulp) tells which neighbour is nearest.
+// Zero, infinity and NaN give themselves; below 2^-96 the last bit may be off.
+__device__ __forceinline__ float root_of(float x) {
+    const float r = __builtin_amdgcn_sqrtf(x);
+    const float down = __int_as_float(__float_as_int(r) - 1), up = __int_as_float(__float_as_int(r) + 1);
+    const float below = fmaf(-down, r, x), above = fmaf(-up, r, x);
+    const float s = below <= 0.0f ? down : r;
+    return above > 0.0f ? up : s;
+}
+
+// Nearest whole number to the root of y >= 0, at most `top` (ties up).  The
+// root is taken a little too large, so that its rounding is right or one too
+// high, and the square of the border below, exact in binary32, settles it.
 __device__ __forceinline__ float root_code(float y, float top) {
-    const float r = rintf(__builtin_amdgcn_sqrtf(y));
-    const float up = r + 0.5f, down = fmaxf(r - 0.5f, 0.0f);
-    return fminf(r + (y >= up * up ? 1.0f : 0.0f) - (y < down * down ? 1.0f : 0.0f), top);
+    const float r = floorf(fmaf(__builtin_amdgcn_sqrtf(y), 1.0f + 0x1p-22f, 0.5f));
+    const float border = r - 0.5f;
+    return fminf(y < border * fabsf(border) ? r - 1.0f : r, top);
 }
 
 // Unit of a block of codes from its largest value's bits.
@@ -65,8 +82,90 @@ __device__ __forceinline__ uint32_t wave_max_bits(const float* x) {
     return lane_value(wave_incl_max(b), kWave - 1);
 }
 
+// A wave's 256 elements: what it loads, and what becomes of it.  WHOLE: all 256 are there.
+template <typename G, typename C, bool CODES>
+struct AdamRun {
+    Pack<float, 4> p, m, v;
+    Pack<G, 4> g;
+    uint32_t mc, vc;  // four codes each
+    float mu, vu;
+
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const AdamArgs& a, uint64_t at, int n, uint32_t block) {
+        if (WHOLE) n = 4;
+        p = load_some<4>(a.io.params + at, n);
+        g = load_some<4>((const G*)a.io.grad + at, n);
+        if constexpr (CODES) {
+            const Pack<uint8_t, 4> mp = load_some<4>((const uint8_t*)a.io.m + at, n);
+            const Pack<uint8_t, 4> vp = load_some<4>((const uint8_t*)a.io.v + at, n);
+            __builtin_memcpy(&mc, &mp, 4);
+            __builtin_memcpy(&vc, &vp, 4);
+            mu = a.io.m_unit[block];
+            vu = a.io.v_unit[block];
+        } else {
+            m = load_some<4>((const float*)a.io.m + at, n);
+            v = load_some<4>((const float*)a.io.v + at, n);
+        }
+    }
+    template <bool WHOLE>
+    __device__ __forceinline__ void step(const AdamArgs& a, uint64_t at, int n, uint32_t block, float gs, float keep) {
+        if (WHOLE) n = 4;
+        float root[4];
+        Pack<C, 4> copy;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (CODES) {
+                const float q = (float)(int8_t)(mc >> 8 * j), r = (float)(vc >> 8 * j & 0xFFu);
+                m.v[j] = mu * (q * fabsf(q));
+                v.v[j] = vu * (r * r);
+                v.v[j] *= v.v[j];
+            }
+            const float gv = (float)g.v[j] * gs;
+            m.v[j] = m.v[j] * a.beta1 + gv * a.one_beta1;
+            v.v[j] = v.v[j] * a.beta2 + gv * gv * a.one_beta2;
+            root[j] = root_of(v.v[j]);
+            p.v[j] = p.v[j] * keep -
+                     m.v[j] * __builtin_amdgcn_rcpf(root[j] * a.root_scale + a.eps) * a.step_size;
+            copy.v[j] = (C)p.v[j];
+        }
+        store_some<4>(a.io.params + at, p, n);
+        if (a.io.copy) store_some<4>((C*)a.io.copy + at, copy, n);
+        if constexpr (CODES) {
+            if (!WHOLE)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j >= n) m.v[j] = root[j] = 0.0f;
+            mu = code_unit(wave_max_bits(m.v), 127.0f);
+            vu = code_unit(wave_max_bits(root), 255.0f);
+            const float mi = 1.0f / mu, vi = 1.0f / vu;
+            mc = vc = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // a signed code goes out as itself plus 128, with its highest bit turned
+                const float q = root_code(fabsf(m.v[j]) * mi, 127.0f), r = root_code(root[j] * vi, 255.0f);
+                mc = __builtin_amdgcn_cvt_pk_u8_f32(128.0f + copysignf(q, m.v[j]), j, mc);
+                vc = __builtin_amdgcn_cvt_pk_u8_f32(root[j] > 0.0f ? fmaxf(r, 1.0f) : r, j, vc);
+            }
+            mc ^= 0x80808080u;
+            Pack<uint8_t, 4> mp, vp;
+            __builtin_memcpy(&mp, &mc, 4);
+            __builtin_memcpy(&vp, &vc, 4);
+            store_some<4>((uint8_t*)a.io.m + at, mp, n);
+            store_some<4>((uint8_t*)a.io.v + at, vp, n);
+            if (lane_id() == 0) {
+                a.io.m_unit[block] = mu;
+                a.io.v_unit[block] = vu;
+            }
+        } else {
+            store_some<4>((float*)a.io.m + at, m, n);
+            store_some<4>((float*)a.io.v + at, v, n);
+        }
+    }
+};
+
 template <typename G, typename C, bool CODES>
 __global__ __launch_bounds__(kBlock) void k_adamw(AdamArgs a) {
+    constexpr int RUNS = CODES ? kRunsCodes : kRuns;
     float gs = a.grad_scale;
     if (a.scale) {
         if (a.scale[1] != 0.0f) return;
@@ -74,72 +173,22 @@ __global__ __launch_bounds__(kBlock) void k_adamw(AdamArgs a) {
     }
     for (uint32_t ch = blockIdx.x; ch < a.num_chunks; ch += gridDim.x) {
         const AdamChunk c = a.chunks[ch];
-        const uint64_t at = (c.start_len & ((1ull << 54) - 1)) + threadIdx.x * 4;
-        const int n = (int)(c.start_len >> 54) + 1 - (int)threadIdx.x * 4;
-        const uint32_t block = c.block + wave_index();
-        if ((int)(c.start_len >> 54) < (int)(wave_index() * kStateBlock)) continue;  // no element in this wave
-        const Pack<float, 4> p = load_some<4>(a.io.params + at, n);
-        const Pack<G, 4> g = load_some<4>((const G*)a.io.grad + at, n);
-        float m[4], v[4], root[4];
-        if constexpr (CODES) {
-            const Pack<int8_t, 4> mc = load_some<4>((const int8_t*)a.io.m + at, n);
-            const Pack<uint8_t, 4> vc = load_some<4>((const uint8_t*)a.io.v + at, n);
-            const float mu = a.io.m_unit[block], vu = a.io.v_unit[block];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float q = (float)mc.v[j], r = (float)vc.v[j];
-                m[j] = mu * (q * fabsf(q));
-                v[j] = vu * (r * r);
-                v[j] *= v[j];
-            }
-        } else {
-            const Pack<float, 4> ml = load_some<4>((const float*)a.io.m + at, n);
-            const Pack<float, 4> vl = load_some<4>((const float*)a.io.v + at, n);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) m[j] = ml.v[j], v[j] = vl.v[j];
-        }
+        const uint32_t len = (uint32_t)(c.start_len >> kLenShift) + 1, wave = wave_index();
+        const uint64_t at = (c.start_len & ((1ull << kLenShift) - 1)) + threadIdx.x * 4;
         const float keep = 1.0f - a.lr_decay * a.decay[c.tensor];
-        Pack<float, 4> np;
-        Pack<C, 4> copy;
+        AdamRun<G, C, CODES> run[RUNS];
+        if (len == RUNS * kAdamRun) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float gv = (float)g.v[j] * gs;
-            m[j] = m[j] * a.beta1 + gv * a.one_beta1;
-            v[j] = v[j] * a.beta2 + gv * gv * a.one_beta2;
-            root[j] = sqrtf(v[j]);
-            np.v[j] = p.v[j] * keep - m[j] / (root[j] * a.root_scale + a.eps) * a.step_size;
-            copy.v[j] = (C)np.v[j];
-        }
-        store_some<4>(a.io.params + at, np, n);
-        if (a.io.copy) store_some<4>((C*)a.io.copy + at, copy, n);
-        if constexpr (CODES) {
-            if (n < 4)
+            for (int u = 0; u < RUNS; ++u) run[u].template load<true>(a, at + u * kAdamRun, 4, c.block + u * 4 + wave);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j >= n) m[j] = root[j] = 0.0f;
-            const float mu = code_unit(wave_max_bits(m), 127.0f), vu = code_unit(wave_max_bits(root), 255.0f);
-            const float mi = 1.0f / mu, vi = 1.0f / vu;
-            Pack<int8_t, 4> mc;
-            Pack<uint8_t, 4> vc;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float q = root_code(fabsf(m[j]) * mi, 127.0f);
-                mc.v[j] = (int8_t)(m[j] < 0.0f ? -q : q);
-                const float r = root_code(root[j] * vi, 255.0f);
-                vc.v[j] = (uint8_t)(root[j] > 0.0f ? fmaxf(r, 1.0f) : r);
-            }
-            store_some<4>((int8_t*)a.io.m + at, mc, n);
-            store_some<4>((uint8_t*)a.io.v + at, vc, n);
-            if (lane_id() == 0) {
-                a.io.m_unit[block] = mu;
-                a.io.v_unit[block] = vu;
-            }
+            for (int u = 0; u < RUNS; ++u)
+                run[u].template step<true>(a, at + u * kAdamRun, 4, c.block + u * 4 + wave, gs, keep);
         } else {
-            Pack<float, 4> ml, vl;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ml.v[j] = m[j], vl.v[j] = v[j];
-            store_some<4>((float*)a.io.m + at, ml, n);
-            store_some<4>((float*)a.io.v + at, vl, n);
+            for (uint32_t u = 0; u * kAdamRun + wave * kStateBlock < len; ++u) {
+                const int n = (int)len - (int)(u * kAdamRun + threadIdx.x * 4);
+                run[0].template load<false>(a, at + u * kAdamRun, n, c.block + u * 4 + wave);
+                run[0].template step<false>(a, at + u * kAdamRun, n, c.block + u * 4 + wave, gs, keep);
+            }
         }
     }
 }
@@ -148,19 +197,30 @@ __global__ __launch_bounds__(kBlock) void k_adamw(AdamArgs a) {
 template <typename G>
 __global__ __launch_bounds__(kBlock) void k_square_sum(const G* grad, uint64_t n, double* part) {
     __shared__ double lds[kWavesPerBlock];
+    constexpr int kAhead = 8;
     double s = 0.0;
     const uint64_t step = (uint64_t)gridDim.x * kBlock * 4;
-#pragma unroll 4
-    for (uint64_t at = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * 4; at < n; at += step) {
-        const Pack<G, 4> g = load_some<4>(grad + at, (int)min(n - at, (uint64_t)4));
+    uint64_t at = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
+    const auto add = [&](const Pack<G, 4>& g) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) s = fma((double)(float)g.v[j], (double)(float)g.v[j], s);
+    };
+    for (; at + (kAhead - 1) * step + 4 <= n; at += kAhead * step) {
+        Pack<G, 4> g[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) g[u] = load_pack<4>(grad + at + u * step);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) add(g[u]);
     }
+    for (; at < n; at += step) add(load_some<4>(grad + at, (int)min(n - at, (uint64_t)4)));
     s = row_sum<kWavesPerBlock>(s, lds);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// scale[0] = the gradient's scale under the norm's bound, scale[1] = 1 when the norm is not finite.
+// scale[0] = the gradient's scale under the norm's bound, scale[1] = 1 when
+// the norm is not finite.  (Its own launch, 4 us: the last block of the sums
+// would have to wait for every other's write to reach memory, which with a
+// release by each of 1,024 blocks took 40 us.)
 __global__ __launch_bounds__(kBlock) void k_clip(const double* part, uint32_t parts, double grad_scale, double max_norm,
                                                  float* scale, float* norm) {
     __shared__ double lds[kWavesPerBlock];
@@ -174,27 +234,53 @@ __global__ __launch_bounds__(kBlock) void k_clip(const double* part, uint32_t pa
     if (norm) *norm = (float)x;
 }
 
-__global__ __launch_bounds__(kBlock) void k_decode(const AdamChunk* chunks, uint32_t num_chunks, const int8_t* mc,
-                                                   const uint8_t* vc, const float* m_unit, const float* v_unit,
+__device__ __forceinline__ void decode4(uint32_t mc, uint32_t vc, float mu, float vu, Pack<float, 4>& m, Pack<float, 4>& v) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float q = (float)(int8_t)(mc >> 8 * j), r = (float)(vc >> 8 * j & 0xFFu);
+        m.v[j] = mu * (q * fabsf(q));
+        v.v[j] = vu * (r * r);
+        v.v[j] *= v.v[j];
+    }
+}
+
+__global__ __launch_bounds__(kBlock) void k_decode(const AdamChunk* chunks, uint32_t num_chunks, const uint8_t* m,
+                                                   const uint8_t* v, const float* m_unit, const float* v_unit,
                                                    float* m_out, float* v_out) {
     for (uint32_t ch = blockIdx.x; ch < num_chunks; ch += gridDim.x) {
         const AdamChunk c = chunks[ch];
-        const uint64_t at = (c.start_len & ((1ull << 54) - 1)) + threadIdx.x * 4;
-        const int n = (int)(c.start_len >> 54) + 1 - (int)threadIdx.x * 4;
-        if ((int)(c.start_len >> 54) < (int)(wave_index() * kStateBlock)) continue;
-        const float mu = m_unit[c.block + wave_index()], vu = v_unit[c.block + wave_index()];
-        const Pack<int8_t, 4> q = load_some<4>(mc + at, n);
-        const Pack<uint8_t, 4> r = load_some<4>(vc + at, n);
-        Pack<float, 4> m, v;
+        const uint32_t len = (uint32_t)(c.start_len >> kLenShift) + 1, wave = wave_index();
+        const uint64_t at = (c.start_len & ((1ull << kLenShift) - 1)) + threadIdx.x * 4;
+        Pack<float, 4> mo, vo;
+        if (len == kRunsCodes * kAdamRun) {
+            uint32_t mc[kRunsCodes], vc[kRunsCodes];
+            float mu[kRunsCodes], vu[kRunsCodes];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float x = (float)q.v[j], y = (float)r.v[j];
-            m.v[j] = mu * (x * fabsf(x));
-            v.v[j] = vu * (y * y);
-            v.v[j] *= v.v[j];
+            for (int u = 0; u < kRunsCodes; ++u) {
+                __builtin_memcpy(&mc[u], m + at + u * kAdamRun, 4);
+                __builtin_memcpy(&vc[u], v + at + u * kAdamRun, 4);
+                mu[u] = m_unit[c.block + u * 4 + wave];
+                vu[u] = v_unit[c.block + u * 4 + wave];
+            }
+#pragma unroll
+            for (int u = 0; u < kRunsCodes; ++u) {
+                decode4(mc[u], vc[u], mu[u], vu[u], mo, vo);
+                store_pack<4>(m_out + at + u * kAdamRun, mo);
+                store_pack<4>(v_out + at + u * kAdamRun, vo);
+            }
+        } else {
+            for (uint32_t u = 0; u * kAdamRun + wave * kStateBlock < len; ++u) {
+                const uint32_t block = c.block + u * 4 + wave;
+                const int n = (int)len - (int)(u * kAdamRun + threadIdx.x * 4);
+                const Pack<uint8_t, 4> mp = load_some<4>(m + at + u * kAdamRun, n), vp = load_some<4>(v + at + u * kAdamRun, n);
+                uint32_t mc, vc;
+                __builtin_memcpy(&mc, &mp, 4);
+                __builtin_memcpy(&vc, &vp, 4);
+                decode4(mc, vc, m_unit[block], v_unit[block], mo, vo);
+                store_some<4>(m_out + at + u * kAdamRun, mo, n);
+                store_some<4>(v_out + at + u * kAdamRun, vo, n);
+            }
         }
-        store_some<4>(m_out + at, m, n);
-        store_some<4>(v_out + at, v, n);
     }
 }
 
@@ -209,8 +295,12 @@ hipError_t launch_adamw(const AdamArgs& a, bool codes, hipStream_t st) {
 }
 
 template <typename G>
-hipError_t launch_square_sum(const void* grad, uint64_t n, double* part, uint32_t blocks, hipStream_t st) {
-    if (blocks) k_square_sum<G><<<dim3(blocks), dim3(kBlock), 0, st>>>((const G*)grad, n, part);
+hipError_t launch_clip(const gd_adamw_io& io, uint64_t n, double* part, float* scale, hipStream_t st) {
+    const uint32_t blocks = (uint32_t)std::min<uint64_t>((n + kAdamRun - 1) / kAdamRun, kNormBlocks);
+    if (blocks) k_square_sum<G><<<dim3(blocks), dim3(kBlock), 0, st>>>((const G*)io.grad, n, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    k_clip<<<dim3(1), dim3(kBlock), 0, st>>>(part, blocks, io.grad_scale, io.max_norm, scale, io.norm);
     return hipGetLastError();
 }
 
@@ -247,10 +337,11 @@ gd_status gd_adamw_create(gd_adamw** out, const uint64_t* off, uint32_t T, gd_st
         o->N = off[T];
         o->codes = kind == GD_STATE_8BIT;
         std::vector<gd::AdamChunk> chunks;
+        const uint64_t chunk = gd::kAdamRun * (uint64_t)(o->codes ? gd::kRunsCodes : gd::kRuns);
         for (uint32_t t = 0; t < T; ++t)
-            for (uint64_t a = off[t]; a < off[t + 1]; a += gd::kAdamChunk) {
-                const uint64_t len = std::min<uint64_t>(gd::kAdamChunk, off[t + 1] - a);
-                chunks.push_back({a | (len - 1) << 54, t, (uint32_t)o->blocks});
+            for (uint64_t a = off[t]; a < off[t + 1]; a += chunk) {
+                const uint64_t len = std::min<uint64_t>(chunk, off[t + 1] - a);
+                chunks.push_back({a | (len - 1) << gd::kLenShift, t, (uint32_t)o->blocks});
                 o->blocks += (len + gd::kStateBlock - 1) / gd::kStateBlock;
             }
         if (chunks.size() > 0xFFFFFFFFull - gd::kAdamMaxBlocks || o->blocks > 0xFFFFFFFFull) {
@@ -314,13 +405,10 @@ gd_status gd_adamw_step(gd_adamw* o, const gd_adamw_io* io, void* stream) {
     a.lr_decay = (float)(io->lr * io->weight_decay);
     hipError_t e = hipSuccess;
     if (io->max_norm > 0.0) {
-        const uint32_t blocks = (uint32_t)std::min<uint64_t>((o->N + gd::kAdamChunk - 1) / gd::kAdamChunk, gd::kNormBlocks);
-        e = gt == GD_F32    ? gd::launch_square_sum<float>(io->grad, o->N, o->part, blocks, st)
-            : gt == GD_BF16 ? gd::launch_square_sum<gd::bf16>(io->grad, o->N, o->part, blocks, st)
-                            : gd::launch_square_sum<gd::f16>(io->grad, o->N, o->part, blocks, st);
+        e = gt == GD_F32    ? gd::launch_clip<float>(*io, o->N, o->part, o->scale, st)
+            : gt == GD_BF16 ? gd::launch_clip<gd::bf16>(*io, o->N, o->part, o->scale, st)
+                            : gd::launch_clip<gd::f16>(*io, o->N, o->part, o->scale, st);
         if (e != hipSuccess) return GD_ERR_HIP;
-        gd::k_clip<<<dim3(1), dim3(gd::kBlock), 0, st>>>(o->part, blocks, io->grad_scale, io->max_norm, o->scale, io->norm);
-        if (hipGetLastError() != hipSuccess) return GD_ERR_HIP;
         a.scale = o->scale;
     }
     if (!o->num_chunks) return GD_OK;
@@ -344,7 +432,7 @@ gd_status gd_adamw_decode(gd_adamw* o, const void* m, const void* v, const float
     gd::DeviceGuard guard(o->device);
     if (!guard.ok) return GD_ERR_HIP;
     gd::k_decode<<<dim3(std::min(o->num_chunks, gd::kAdamMaxBlocks)), dim3(gd::kBlock), 0, (hipStream_t)stream>>>(
-        o->chunks, o->num_chunks, (const int8_t*)m, (const uint8_t*)v, m_unit, v_unit, m_out, v_out);
+        o->chunks, o->num_chunks, (const uint8_t*)m, (const uint8_t*)v, m_unit, v_unit, m_out, v_out);
     return hipGetLastError() == hipSuccess ? GD_OK : GD_ERR_HIP;
 }
 
