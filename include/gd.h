@@ -326,8 +326,8 @@ typedef enum {
  * sum is split; h is rounded where it is written, and y is formed from the
  * sum as it was before that rounding.
  * gd_norm_create plans rows of `dim` elements (1..32768) in `type` on the
- * current device and allocates the scratch of the backward pass (at most
- * 2 KB per element of dim).
+ * current device and allocates the scratch of the backward pass (4 KB per
+ * element of dim).
  */
 typedef struct gd_norm gd_norm;
 gd_status gd_norm_create(gd_norm** out, uint32_t dim, gd_dtype type);
@@ -391,8 +391,8 @@ typedef enum { GD_STATE_F32 = 0, GD_STATE_8BIT = 1 } gd_state;
 
 /* offsets (host, num_tensors + 1 entries): as gd_create, but up to 2^40
  * elements.  decay (host, num_tensors finite floats of 0 or more, or NULL for
- * all 1).  Allocates about 16 bytes per 1,024 elements and 20 per tensor on
- * the current device. */
+ * all 1).  Allocates about 16 bytes per 2,048 elements (4,096 in 8 bits) and 20
+ * per tensor on the current device. */
 gd_status gd_adamw_create(gd_adamw** out, const uint64_t* tensor_offsets, uint32_t num_tensors, gd_state state,
                           const float* decay);
 void gd_adamw_destroy(gd_adamw* opt);

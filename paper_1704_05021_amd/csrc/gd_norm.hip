@@ -2,11 +2,13 @@
 // in the type or in 8 bits with a scale per row) and backward.
 //
 // Both directions are bound by memory: a row is read once, held in registers
-// between the sum of its squares and its output, and written once.  A row
-// takes one wave up to 1,024 elements, four up to 8,192 and sixteen above, so
-// that a thread holds 8 to 32 elements.  Sums over a row are in 64 bits: the
-// norm's factor then comes out the same whatever the split, at one 64-bit
-// multiply-add per element, which the memory's time hides.
+// between its sums and its output, and written once, past the caches' reuse
+// (8192 x 4096 in bfloat16 forward: 47 us so, 5.7 TB/s, and 50 us with
+// ordinary stores).  Sums over a row are in 64 bits: the norm's factor then
+// comes out the same whatever the split, at one 64-bit multiply-add per
+// element, which the memory's time hides.  The backward pass, 70 us at that
+// size, 3.8 TB/s, is bound by the chain of a row's loads, its two sums over
+// eight waves and its output, in what waves its registers leave room for.
 
 #include <cmath>
 #include <new>
@@ -18,7 +20,8 @@
 namespace gd {
 
 constexpr uint32_t kNormMaxDim = 32768;
-constexpr uint32_t kNormParts = 512;        // partial sums of the weight's gradient
+constexpr uint32_t kNormParts = 1024;       // partial sums of the weight's gradient, at most
+constexpr uint32_t kNormBackWaves = 4096;   // waves of the backward pass: four a SIMD, as many as its registers hold
 constexpr uint32_t kNormMaxBlocks = 1u << 20;  // a dispatch holds less than 2^32 threads
 
 template <int WAVES>
@@ -76,8 +79,8 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_norm(gd_norm_io 
                 y.v[j] = (T)h[i][j];
                 if (j < n) big = max(big, __float_as_uint(h[i][j]) & 0x7FFFFFFFu);
             }
-            if (io.sum) store_some<8>((T*)io.sum + row * io.sum_stride + e, s, n);
-            if (!INT8) store_some<8>((T*)io.y + row * io.y_stride + e, y, n);
+            if (io.sum) store_stream<8>((T*)io.sum + row * io.sum_stride + e, s, n);
+            if (!INT8) store_stream<8>((T*)io.y + row * io.y_stride + e, y, n);
         }
         if constexpr (INT8) {
             const RowScale q = row_scale(row_max<WAVES>(big, lds_max));
@@ -96,71 +99,84 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_norm(gd_norm_io 
 }
 
 // dx = rstd (a - xhat mean(a xhat)) + dsum with a = dy weight, xhat = x rstd;
-// the block's share of sum_rows dy xhat goes to part[blockIdx.x].
+// the block's share of sum_rows dy xhat goes to part[blockIdx.x].  A block
+// takes several rows, and loads each while it works on the one before.
 template <typename T, int WAVES, int V>
-__global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_norm_back(gd_norm_grad io, uint32_t dim,
-                                                                                 float* part) {
+__global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_norm_back(gd_norm_grad io, uint32_t dim, float* part) {
     using S = NormShape<WAVES>;
-    __shared__ double lds_sum[2][S::kThreads / kWave];
+    __shared__ double lds_sum[2][2][S::kThreads / kWave];
     const uint32_t t = threadIdx.x % S::kRow;
+    const uint64_t turn = (uint64_t)gridDim.x * S::kRows;
+    struct Row {
+        Pack<T, 8> x[V], dy[V], dsum[V];
+    };
+    const auto here = [&](int i) { return (t + i * S::kRow) * 8; };
+    const auto load = [&](Row& r, uint64_t first) {
+        const uint64_t row = first + threadIdx.x / S::kRow;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const uint32_t e = here(i);
+            const int n = row < io.rows ? (int)(dim - min(e, dim)) : 0;
+            r.x[i] = load_some<8>((const T*)io.x + row * io.x_stride + e, n);
+            r.dy[i] = load_some<8>((const T*)io.dy + row * io.dy_stride + e, n);
+            if (io.dsum) r.dsum[i] = load_some<8>((const T*)io.dsum + row * io.dsum_stride + e, n);
+        }
+    };
+    constexpr bool kAhead = V == 1;  // more elements a thread leave no registers for it
     Pack<T, 8> w[V];
     float dw[V][8];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const uint32_t e = (t + i * S::kRow) * 8;
+        const uint32_t e = here(i);
         w[i] = load_some<8>((const T*)io.weight + min(e, dim), (int)(dim - min(e, dim)));
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
     }
-    for (uint64_t first = (uint64_t)blockIdx.x * S::kRows; first < io.rows; first += (uint64_t)gridDim.x * S::kRows) {
+    Row next;
+    uint64_t first = (uint64_t)blockIdx.x * S::kRows;
+    if (kAhead) load(next, first);
+    for (uint32_t odd = 0; first < io.rows; first += turn, odd ^= 1) {
         const uint64_t row = first + threadIdx.x / S::kRow;
         const bool on = row < io.rows;
-        Pack<T, 8> x[V], dy[V];
+        if (!kAhead) load(next, first);
+        const Row r = next;
+        if (kAhead && first + turn < io.rows) load(next, first + turn);
         double ss = 0.0, ax = 0.0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const uint32_t e = (t + i * S::kRow) * 8;
-            const int n = on ? (int)(dim - min(e, dim)) : 0;
-            x[i] = load_some<8>((const T*)io.x + row * io.x_stride + e, n);
-            dy[i] = load_some<8>((const T*)io.dy + row * io.dy_stride + e, n);
-        }
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float xv = (float)x[i].v[j];
+                const float xv = (float)r.x[i].v[j];
                 ss = fma((double)xv, (double)xv, ss);
-                ax = fma((double)((float)dy[i].v[j] * (float)w[i].v[j]), (double)xv, ax);
+                ax = fma((double)((float)r.dy[i].v[j] * (float)w[i].v[j]), (double)xv, ax);
             }
-        ss = row_sum<WAVES>(ss, lds_sum[0]);
-        ax = row_sum<WAVES>(ax, lds_sum[1]);
+        // the two turns' sums lie apart, so one barrier a row is enough
+        row_sums<WAVES>(ss, ax, lds_sum[odd][0], lds_sum[odd][1]);
         const float rstd = (float)rsqrt(ss / dim + (double)io.eps);
         const float mean = (float)(ax / dim * rstd);  // mean(a xhat)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t e = (t + i * S::kRow) * 8;
+            const uint32_t e = here(i);
             const int n = on ? (int)(dim - min(e, dim)) : 0;
-            Pack<T, 8> d, more{};
-            if (io.dsum) more = load_some<8>((const T*)io.dsum + row * io.dsum_stride + e, n);
+            Pack<T, 8> d;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float g = (float)dy[i].v[j], xhat = (float)x[i].v[j] * rstd;
+                const float g = (float)r.dy[i].v[j], xhat = (float)r.x[i].v[j] * rstd;
                 dw[i][j] += n > 0 ? g * xhat : 0.0f;
                 float v = rstd * (g * (float)w[i].v[j] - xhat * mean);
-                if (io.dsum) v += (float)more.v[j];
+                if (io.dsum) v += (float)r.dsum[i].v[j];
                 d.v[j] = (T)v;
             }
-            store_some<8>((T*)io.dx + row * io.dx_stride + e, d, n);
+            store_stream<8>((T*)io.dx + row * io.dx_stride + e, d, n);
         }
-        if constexpr (WAVES > 1) __syncthreads();
     }
     if (!part) return;
     if constexpr (S::kRows > 1) {  // the block's rows join before the partial is written
-        __shared__ float lds_dw[S::kRows][V * 8 * kWave];
+        __shared__ float lds_dw[S::kRows][V * 8 * S::kRow];
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) lds_dw[threadIdx.x / kWave][(i * 8 + j) * kWave + t] = dw[i][j];
+            for (int j = 0; j < 8; ++j) lds_dw[threadIdx.x / S::kRow][(i * 8 + j) * S::kRow + t] = dw[i][j];
         __syncthreads();
         if (threadIdx.x >= (uint32_t)S::kRow) return;
 #pragma unroll
@@ -168,7 +184,7 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_norm_back(gd_nor
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int r = 1; r < S::kRows; ++r) dw[i][j] += lds_dw[r][(i * 8 + j) * kWave + t];
+                for (int r = 1; r < S::kRows; ++r) dw[i][j] += lds_dw[r][(i * 8 + j) * S::kRow + t];
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -225,7 +241,8 @@ hipError_t launch_norm(const gd_norm_io& io, uint32_t dim, hipStream_t st) {
 template <typename T, int WAVES, int V>
 hipError_t launch_norm_back(const gd_norm_grad& io, uint32_t dim, float* part, hipStream_t st) {
     using S = NormShape<WAVES>;
-    const uint32_t parts = (uint32_t)std::min<uint64_t>((io.rows + S::kRows - 1) / S::kRows, kNormParts);
+    const uint32_t most = std::min(kNormBackWaves * kWave / S::kThreads, kNormParts);
+    const uint32_t parts = (uint32_t)std::min<uint64_t>((io.rows + S::kRows - 1) / S::kRows, most);
     if (parts) {
         k_norm_back<T, WAVES, V><<<dim3(parts), dim3(S::kThreads), 0, st>>>(io, dim, io.dweight ? part : nullptr);
         const hipError_t e = hipGetLastError();
@@ -289,14 +306,20 @@ hipError_t launch_quantise(const void* x, uint64_t rows, uint32_t columns, uint6
     return hipGetLastError();
 }
 
-// Calls f with the waves of a row and the 8-element vectors of a thread as constants.
+// Calls f with the waves of a row and the 8-element vectors of a thread as
+// constants.  One vector a thread does best (8192 x 4096 in bfloat16 forward:
+// 50 us with eight waves a row, 63 with four, 91 with one; 8192 x 1024: 13 us
+// with two, 16 with one), up to blocks of 512 threads, whose barriers cost
+// less than those of 1,024 (4096 x 8192: 57 and 60 us; backward, where a
+// thread holds more, 97 and 77).
 template <typename F>
-hipError_t with_shape(uint32_t dim, F f) {
+hipError_t with_shape(uint32_t dim, bool back, F f) {
     if (dim <= 512) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-    if (dim <= 1024) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+    if (dim <= 1024) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
     if (dim <= 2048) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
-    if (dim <= 4096) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
-    if (dim <= 8192) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+    if (dim <= 4096) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+    if (dim <= 8192 && !back) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
+    if (dim <= 8192) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
     if (dim <= 16384) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
     return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
 }
@@ -358,7 +381,7 @@ gd_status gd_norm_forward(gd_norm* n, const gd_norm_io* io, void* stream) {
     gd::DeviceGuard guard(n->device);
     if (!guard.ok) return GD_ERR_HIP;
     const hipError_t e = gd::with_type(n->type, [&](auto zero) {
-        return gd::with_shape(n->dim, [&](auto waves, auto v) {
+        return gd::with_shape(n->dim, false, [&](auto waves, auto v) {
             return gd::launch_norm<decltype(zero), waves(), v()>(*io, n->dim, (hipStream_t)stream);
         });
     });
@@ -373,7 +396,7 @@ gd_status gd_norm_backward(gd_norm* n, const gd_norm_grad* io, void* stream) {
     gd::DeviceGuard guard(n->device);
     if (!guard.ok) return GD_ERR_HIP;
     const hipError_t e = gd::with_type(n->type, [&](auto zero) {
-        return gd::with_shape(n->dim, [&](auto waves, auto v) {
+        return gd::with_shape(n->dim, true, [&](auto waves, auto v) {
             return gd::launch_norm_back<decltype(zero), waves(), v()>(*io, n->dim, n->part, (hipStream_t)stream);
         });
     });
@@ -387,7 +410,7 @@ gd_status gd_quantise_rows(const void* x, gd_dtype type, uint64_t rows, uint64_t
     if (rows == 0) return GD_OK;
     if (!x || !q || !scale || x_stride < columns || q_stride < columns) return GD_ERR_ARG;
     const hipError_t e = gd::with_type(ty, [&](auto zero) {
-        return gd::with_shape((uint32_t)columns, [&](auto waves, auto v) {
+        return gd::with_shape((uint32_t)columns, false, [&](auto waves, auto v) {
             return gd::launch_quantise<decltype(zero), waves(), v()>(x, rows, (uint32_t)columns, x_stride, q, q_stride,
                                                                      scale, (hipStream_t)stream);
         });

@@ -45,6 +45,23 @@ __device__ __forceinline__ void store_some(T* p, const Pack<T, N>& r, int n) {
         if (i < n) p[i] = r.v[i];
 }
 
+// store_some for results that nothing reads back soon.
+template <int N, typename T>
+__device__ __forceinline__ void store_stream(T* p, const Pack<T, N>& r, int n) {
+    if (n < N) {
+        store_some<N>(p, r, n);
+        return;
+    }
+    typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+    static_assert(sizeof(r) % 16 == 0 && alignof(T) >= 2);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r) / 16); ++i) {
+        words v;
+        __builtin_memcpy(&v, (const char*)&r + i * 16, 16);
+        __builtin_nontemporal_store(v, (words*)p + i);
+    }
+}
+
 // Sum over the threads of one row: WAVES consecutive waves of the block, in a
 // fixed order, in every thread.  lds holds one double per wave of the block;
 // every thread of the block calls it, with a barrier after the last use of
@@ -61,6 +78,21 @@ __device__ __forceinline__ double row_sum(double v, double* lds) {
         for (int i = 0; i < WAVES; ++i) v += lds[w / WAVES * WAVES + i];
     }
     return v;
+}
+
+// Two such sums behind one barrier.
+template <int WAVES>
+__device__ __forceinline__ void row_sums(double& a, double& b, double* lds_a, double* lds_b) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if constexpr (WAVES > 1) {
+        const uint32_t w = wave_index();
+        if (lane_id() == 0) lds_a[w] = a, lds_b[w] = b;
+        __syncthreads();
+        a = b = 0.0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) a += lds_a[w / WAVES * WAVES + i], b += lds_b[w / WAVES * WAVES + i];
+    }
 }
 
 // Largest of unsigned words over the threads of one row, likewise.
