@@ -278,9 +278,9 @@ struct TileLoad<E, true, R, THREADS> {
 };
 
 // WI x WJ waves of NI x NJ 16 x 16 results each.
-template <int WI_, int WJ_, int NI_, int NJ_>
+template <int WI_, int WJ_, int NI_, int NJ_, int DEEP_ = 2>
 struct Tile {
-    static constexpr int WI = WI_, WJ = WJ_, NI = NI_, NJ = NJ_;
+    static constexpr int WI = WI_, WJ = WJ_, NI = NI_, NJ = NJ_, DEEP = DEEP_;  // DEEP: steps in LDS, where they go straight there
     static constexpr int BI = WI * NI * 16, BJ = WJ * NJ * 16, kThreads = WI * WJ * kWave;
     static constexpr int kStage = (BI + BJ) * kStepBytes;           // bytes of LDS of one step
     static constexpr int kLds = 2 * kStage;
@@ -290,7 +290,7 @@ typedef Tile<2, 4, 8, 4> TileBig;    // 256 x 256
 typedef Tile<2, 4, 8, 3> TileLong;   // 256 x 192
 typedef Tile<2, 4, 8, 2> TileWide;   // 256 x 128
 typedef Tile<2, 2, 4, 4> TileMid;    // 128 x 128
-typedef Tile<2, 2, 2, 2> TileSmall;  // 64 x 64
+typedef Tile<2, 2, 2, 2, 4> TileSmall;  // 64 x 64; four deep: 256 x 4096 x 4096 took 47 us with two, 23 with four
 
 // The tile of block b: blocks go to the eight dies in turn, so each die is
 // given a run of neighbouring tiles, and a run goes through 8 tiles along j
@@ -450,10 +450,11 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
 // For 16- and 8-bit operands whose rows start at 16-byte boundaries and whose
 // last 16 bytes may be read whole (along k with zeros behind the end of k):
 // the caller's where their sizes are so, else copies made by k_pad.
-// LDS has room for two steps.  While step s is multiplied, step s + 1 is on
-// its way from memory straight into LDS, in no register; one barrier, behind
-// the last reads of step s, both shows that step s + 1 has come for every
-// wave and frees the room of step s for step s + 2.  Each fragment is read
+// LDS has room for DEEP steps, two for the larger tiles.  While step s is
+// multiplied, the next DEEP - 1 are on their way from memory straight into
+// LDS, in no register; one barrier, behind the last reads of step s, both
+// shows that step s + 1 has come for every wave and frees the room of step s
+// for step s + DEEP.  Each fragment is read
 // right behind the last use of the one whose registers it takes.
 //
 // Along k a row's eight 16-byte chunks change places by the row's low bits.
@@ -579,7 +580,8 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
     using FP = TileFetch<E, PA, TL::BI, TL::kThreads>;
     using FQ = TileFetch<E, QA, TL::BJ, TL::kThreads>;
     static_assert(FP::kBytes + FQ::kBytes == TL::kStage);
-    __shared__ __align__(1024) char lds[TL::kLds];
+    constexpr int DEEP = TL::DEEP, kLoads = FP::N + FQ::N;
+    __shared__ __align__(1024) char lds[DEEP * TL::kStage];
     uint32_t ti, tj;
     tile_of(a, blockIdx.x, ti, tj);
     const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
@@ -605,7 +607,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
     for (int c = 0; c < 2; ++c) p_at[c] = FP::lane_at(c), q_at[c] = FQ::lane_at(c);
     const auto issue = [&](uint32_t s) {
         if (s >= steps) return;
-        const uint32_t to = lds_at + (s & 1) * TL::kStage;
+        const uint32_t to = lds_at + s % DEEP * TL::kStage;
         if (s < whole) {
             fp.template issue<true>(s, 0, to);
             fq.template issue<true>(s, 0, to + FP::kBytes);
@@ -616,10 +618,10 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
     };
     u4 p[TL::NI], qa[TL::NJ], qb[TL::NJ];
     const auto read_p = [&](uint32_t s, int c, int i) {
-        p[i] = FP::fragment(lds + (s & 1) * TL::kStage, (wi * TL::NI + i) * 16, p_at[c]);
+        p[i] = FP::fragment(lds + s % DEEP * TL::kStage, (wi * TL::NI + i) * 16, p_at[c]);
     };
     const auto read_q = [&](uint32_t s, int c, int j) {
-        return FQ::fragment(lds + (s & 1) * TL::kStage + FP::kBytes, (wj * TL::NJ + j) * 16, q_at[c]);
+        return FQ::fragment(lds + s % DEEP * TL::kStage + FP::kBytes, (wj * TL::NJ + j) * 16, q_at[c]);
     };
     // The products of p and q; each fragment of group nc of step ns is read behind the last use of the one whose
     // place it takes.  `before` comes before the first read, more(m) behind product m.
@@ -643,10 +645,10 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
     const auto nothing = [] {};
     const auto no_more = [](int) {};
     if (steps) {
-        issue(0);
-        issue(1);
-        if (steps > 1)
-            load_wait<FP::N + FQ::N>();
+#pragma unroll 1
+        for (uint32_t d = 0; d < DEEP; ++d) issue(d);
+        if (steps >= DEEP)
+            load_wait<(DEEP - 1) * kLoads>();
         else
             load_wait<0>();
 #pragma unroll
@@ -655,14 +657,14 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
         for (int j = 0; j < TL::NJ; ++j) qa[j] = read_q(0, 0, j);
     }
     uint32_t s = 0;
-    for (; s + 2 < whole; ++s) {
+    for (; s + DEEP < whole; ++s) {
         group(s, 1, qb, qa, nothing, no_more);
-        const char* from_p = (const char*)fp.base + (s + 2) * fp.per_step;
-        const char* from_q = (const char*)fq.base + (s + 2) * fq.per_step;
-        const uint32_t to = lds_at + (s & 1) * TL::kStage;
+        const char* from_p = (const char*)fp.base + (s + DEEP) * fp.per_step;
+        const char* from_q = (const char*)fq.base + (s + DEEP) * fq.per_step;
+        const uint32_t to = lds_at + s % DEEP * TL::kStage;
         // the loads are spread over the group: side by side they would hold up its reads of LDS
-        group(s + 1, 0, qa, qb, [] { load_wait<0>(); }, [&](int m) {
-            constexpr int kLoads = FP::N + FQ::N, kRoom = TL::NI * TL::NJ - TL::NJ;
+        group(s + 1, 0, qa, qb, [] { load_wait<(DEEP - 2) * kLoads>(); }, [&](int m) {
+            constexpr int kRoom = TL::NI * TL::NJ - TL::NJ;
 #pragma unroll
             for (int d = 0; d < kLoads; ++d) {
                 if (TL::NJ + d * kRoom / kLoads != m) continue;
@@ -683,7 +685,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
             for (int j = 0; j < TL::NJ; ++j) acc[i][j] = M::multiply(p[i], qb[j], acc[i][j]);
         if (s + 1 < steps) {
             load_wait<0>();
-            issue(s + 2);
+            issue(s + DEEP);
 #pragma unroll
             for (int i = 0; i < TL::NI; ++i) read_p(s + 1, 0, i);
 #pragma unroll

@@ -39,7 +39,7 @@ struct TileCost {
     double alone_us, shared_us;
 };
 constexpr TileCost kBigCost{256, 256, 1, 1.48, 1.48}, kLongCost{256, 192, 1, 1.10, 1.10}, kWideCost{256, 128, 1, 0.82, 0.82},
-    kMidCost{128, 128, 2, 0.58, 0.475}, kSmallCost{64, 64, 5, 0.30, 0.165};
+    kMidCost{128, 128, 2, 0.58, 0.475}, kSmallCost{64, 64, 2, 0.17, 0.165};
 constexpr double kRoundUs = 5.0, kJoinUs = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct TilePlan {

@@ -31,12 +31,14 @@ __device__ __forceinline__ float act_slope(int act, float z) {
 // 512 columns of a row at a time, a lane 8; the block's four waves take rows
 // in turn.  Bound by memory: 6 bytes an element in 16 bits.
 constexpr int kSlopeColumns = kWave * 8;
+// The sums of few rows, one block's, go out at once.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_slope(gd_linear_grad io, uint32_t columns, int act, float* part) {
     __shared__ float lds[kWavesPerBlock][kSlopeColumns];
     const uint32_t c = blockIdx.x * kSlopeColumns + lane_id() * 8;
     const int n = (int)(columns - min(c, columns));
     float sum[8] = {};
+#pragma unroll 4
     for (uint64_t row = (uint64_t)blockIdx.y * kWavesPerBlock + wave_index(); row < io.rows;
          row += (uint64_t)gridDim.y * kWavesPerBlock) {
         Pack<T, 8> d = load_some<8>((const T*)io.dy + row * io.dy_stride + c, n);
@@ -49,7 +51,7 @@ __global__ __launch_bounds__(kBlock) void k_slope(gd_linear_grad io, uint32_t co
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += (float)d.v[j];
     }
-    if (!part) return;
+    if (!io.dbias) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) lds[wave_index()][lane_id() * 8 + j] = sum[j];
     __syncthreads();
@@ -58,25 +60,29 @@ __global__ __launch_bounds__(kBlock) void k_slope(gd_linear_grad io, uint32_t co
 #pragma unroll
         for (int w = 0; w < kWavesPerBlock; ++w) s += lds[w][j];
         const uint32_t col = blockIdx.x * kSlopeColumns + j;
-        if (col < columns) part[(uint64_t)blockIdx.y * columns + col] = s;
+        if (col >= columns) continue;
+        if (gridDim.y == 1)
+            io.dbias[col] = io.accumulate ? io.dbias[col] + s : s;
+        else
+            part[(uint64_t)blockIdx.y * columns + col] = s;
     }
 }
 
 hipError_t launch_slope(const gd_linear_grad& io, int type, uint32_t columns, int act, float* part, hipStream_t st) {
-    const uint32_t groups = (uint32_t)std::min<uint64_t>((io.rows + 15) / 16, kBiasParts);
+    // one block down the rows up to 64 of them: a second launch costs more than the 16 turns of its waves
+    const uint32_t groups = io.rows <= 64 ? (io.rows != 0) : (uint32_t)std::min<uint64_t>((io.rows + 15) / 16, kBiasParts);
     if (groups) {
         const dim3 grid((columns + kSlopeColumns - 1) / kSlopeColumns, groups);
-        float* sums = io.dbias ? part : nullptr;
         if (type == GD_F32)
-            k_slope<float><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, sums);
+            k_slope<float><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, part);
         else if (type == GD_BF16)
-            k_slope<bf16><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, sums);
+            k_slope<bf16><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, part);
         else
-            k_slope<f16><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, sums);
+            k_slope<f16><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, part);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (!io.dbias || (!groups && io.accumulate)) return hipSuccess;
+    if (!io.dbias || groups == 1 || (!groups && io.accumulate)) return hipSuccess;
     return launch_sum_parts(part, groups, columns, io.dbias, io.accumulate != 0, st);
 }
 

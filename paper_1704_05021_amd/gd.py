@@ -495,6 +495,45 @@ def _dtype_code(dtype: torch.dtype) -> int:
     return _DTYPES[dtype]
 
 
+def _flat_on(device: int, t: torch.Tensor, name: str, dtype: torch.dtype, n: int) -> int:
+    """Address of a contiguous tensor of n elements on the device."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor on cuda:{device}")
+    if t.numel() != n:
+        raise ValueError(f"{name} has {t.numel()} elements, not {n}")
+    return t.data_ptr()
+
+
+def _rows_on(device: int, t: torch.Tensor, name: str, dtype: torch.dtype, columns: int, rows: Optional[int] = None):
+    """(rows, address, row stride) of a tensor [..., columns] on the device whose rows are contiguous and evenly
+    spaced."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on cuda:{device}")
+    dim = t.dim()
+    if dim == 0 or t.size(-1) != columns:
+        raise ValueError(f"{name} must have rows of {columns} elements, not shape {tuple(t.shape)}")
+    if dim != 2:
+        t = t.view(-1, columns)
+    n = t.size(0)
+    if rows is not None and n != rows:
+        raise ValueError(f"{name} has {n} rows, not {rows}")
+    down, across = t.stride()
+    if across != 1 and columns > 1 and n > 0:
+        raise ValueError(f"{name} must be contiguous within its rows")
+    return n, t.data_ptr(), down if n > 1 else columns
+
+
+def _stream_on(device: int, stream: Optional[torch.cuda.Stream], *tensors) -> Optional[int]:
+    """The stream's handle.  Tensors used on a stream that is not the current one are kept from reuse until its work so
+    far is done; that the work before them is done is the caller's to see to."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device) or None
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream or None
+
+
 class _Handle:
     """A library handle on one device, freed with the object."""
 
@@ -505,6 +544,7 @@ class _Handle:
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         if self.device.index is None:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self._index = self.device.index
         self._h = None
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
@@ -524,38 +564,14 @@ class _Handle:
         except Exception:
             pass
 
-    def _tensor(self, t: torch.Tensor, name: str, dtype: torch.dtype, n: int) -> int:
-        """Address of a contiguous tensor of n elements."""
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
-            raise TypeError(f"{name} must be a contiguous {dtype} tensor on {self.device}")
-        if t.numel() != n:
-            raise ValueError(f"{name} has {t.numel()} elements, not {n}")
-        return t.data_ptr()
+    def _tensor(self, t, name, dtype, n) -> int:
+        return _flat_on(self._index, t, name, dtype, n)
 
-    def _matrix(self, t: torch.Tensor, name: str, dtype: torch.dtype, columns: int, rows: Optional[int] = None):
-        """(rows, address, row stride) of a tensor [..., columns] whose rows are contiguous and evenly spaced."""
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device:
-            raise TypeError(f"{name} must be a {dtype} tensor on {self.device}")
-        if t.dim() == 0 or t.shape[-1] != columns:
-            raise ValueError(f"{name} must have rows of {columns} elements, not shape {tuple(t.shape)}")
-        if t.dim() != 2:
-            t = t.view(-1, columns)
-        n = t.shape[0]
-        if rows is not None and n != rows:
-            raise ValueError(f"{name} has {n} rows, not {rows}")
-        if columns > 1 and t.stride(1) != 1 and n > 0:
-            raise ValueError(f"{name} must be contiguous within its rows")
-        return n, t.data_ptr(), t.stride(0) if n > 1 else columns
+    def _matrix(self, t, name, dtype, columns, rows=None):
+        return _rows_on(self._index, t, name, dtype, columns, rows)
 
-    def _stream(self, stream: Optional[torch.cuda.Stream], *tensors) -> Optional[int]:
-        """The stream's handle.  Tensors used on a stream that is not the current one are kept from reuse until
-        its work so far is done; that the work before them is done is the caller's to see to."""
-        if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self.device.index) or None
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-        return stream.cuda_stream or None
+    def _stream(self, stream, *tensors) -> Optional[int]:
+        return _stream_on(self._index, stream, *tensors)
 
 
 class RMSNorm(_Handle):
@@ -575,15 +591,15 @@ class RMSNorm(_Handle):
 
     def forward(self, x, weight, residual=None, out=None, sum_out=None, stream=None):
         """(y, h); h is x itself without a residual.  ``sum_out`` may be x or residual, ``out`` may be x."""
-        y = torch.empty(x.shape, dtype=self.dtype, device=self.device) if out is None else out
+        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
         h = self._run(x, weight, residual, y, None, sum_out, stream)
         return y, h
 
     def forward_int8(self, x, weight, residual=None, out=None, scale=None, sum_out=None, stream=None):
         """(q, scale, h): rows of y in 8 bits, y = q * scale[row], scale[row] = max|y| / 127."""
-        q = torch.empty(x.shape, dtype=torch.int8, device=self.device) if out is None else out
+        q = x.new_empty(x.shape, dtype=torch.int8) if out is None else out
         if scale is None:
-            scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=self.device)
+            scale = x.new_empty(x.shape[:-1], dtype=torch.float32)
         h = self._run(x, weight, residual, q, scale, sum_out, stream)
         return q, scale, h
 
@@ -598,7 +614,7 @@ class RMSNorm(_Handle):
         h = x
         if residual is not None:
             _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.dim, rows)
-            h = torch.empty(x.shape, dtype=self.dtype, device=self.device) if sum_out is None else sum_out
+            h = torch.empty_like(x, memory_format=torch.contiguous_format) if sum_out is None else sum_out
         elif sum_out is not None:
             h = sum_out
         if h is not x or sum_out is not None:
@@ -619,7 +635,7 @@ class RMSNorm(_Handle):
         if dsum is not None:
             _, io.dsum, io.dsum_stride = self._matrix(dsum, "dsum", self.dtype, self.dim, rows)
         if dx is None:
-            dx = torch.empty(dy.shape, dtype=self.dtype, device=self.device)
+            dx = torch.empty_like(dy, memory_format=torch.contiguous_format)
         _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.dim, rows)
         dweight = _gradient(dweight, accumulate, (self.dim,), self.device)
         io.dweight = self._tensor(dweight, "dweight", torch.float32, self.dim)
@@ -680,11 +696,11 @@ class Linear(_Handle):
             _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.outf, rows)
         shape = (*x.shape[:-1], self.outf)
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = x.new_empty(shape, dtype=self.dtype)
         _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.outf, rows)
         pre = None
         if keep_pre is not False:
-            pre = torch.empty(shape, dtype=self.dtype, device=self.device) if keep_pre is True else keep_pre
+            pre = x.new_empty(shape, dtype=self.dtype) if keep_pre is True else keep_pre
             _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, self.outf, rows)
         st = _lib().gd_linear_forward(self._h, io, self._stream(stream, x, weight, xs, ws, bias, residual, out, pre))
         if st != 0:
@@ -707,14 +723,14 @@ class Linear(_Handle):
                 raise ValueError(f"the backward of {self.act} needs pre")
             _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, self.outf, rows)
             if dz is None:
-                dz = torch.empty(dy.shape, dtype=self.dtype, device=self.device)
+                dz = torch.empty_like(dy, memory_format=torch.contiguous_format)
             _, io.dz, io.dz_stride = self._matrix(dz, "dz", self.dtype, self.outf, rows)
         else:
             pre, dz = None, dy
         if need_dx:
             _, io.weight, io.weight_stride = self._matrix(weight, "weight", self.dtype, self.inf, self.outf)
             if dx is None:
-                dx = torch.empty((*dy.shape[:-1], self.inf), dtype=self.dtype, device=self.device)
+                dx = dy.new_empty((*dy.shape[:-1], self.inf))
             _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.inf, rows)
         else:
             dx = None
@@ -735,18 +751,20 @@ class Linear(_Handle):
 
 def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.cuda.Stream] = None):
     """(q, scale): rows of x in 8 bits, x = q * scale[row], scale[row] = max|x| / 127 (gd_quantise_rows)."""
-    code = _dtype_code(x.dtype)
-    if not x.is_cuda or x.dim() == 0 or x.shape[-1] == 0:
+    code, index = _dtype_code(x.dtype), x.get_device()
+    if index < 0 or x.dim() == 0 or x.size(-1) == 0:
         raise ValueError("x must be a GPU tensor of rows of at least one element")
-    q = torch.empty(x.shape, dtype=torch.int8, device=x.device) if out is None else out
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
-    on = _Handle()
-    on.device, on._h = x.device, None
-    rows, xp, xs = on._matrix(x, "x", x.dtype, x.shape[-1])
-    _, qp, qs = on._matrix(q, "out", torch.int8, x.shape[-1], rows)
-    sp = on._tensor(scale, "scale", torch.float32, rows)
-    with torch.cuda.device(x.device):
-        st = _lib().gd_quantise_rows(xp, code, rows, x.shape[-1], xs, qp, qs, sp, on._stream(stream, x, q, scale))
+    columns = x.size(-1)
+    q = x.new_empty(x.shape, dtype=torch.int8) if out is None else out
+    scale = x.new_empty(x.shape[:-1], dtype=torch.float32) if scale is None else scale
+    rows, xp, xs = _rows_on(index, x, "x", x.dtype, columns)
+    _, qp, qs = _rows_on(index, q, "out", torch.int8, columns, rows)
+    sp = _flat_on(index, scale, "scale", torch.float32, rows)
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            st = _lib().gd_quantise_rows(xp, code, rows, columns, xs, qp, qs, sp, _stream_on(index, stream, x, q, scale))
+    else:
+        st = _lib().gd_quantise_rows(xp, code, rows, columns, xs, qp, qs, sp, _stream_on(index, stream, x, q, scale))
     if st != 0:
         raise GDError(st, "gd_quantise_rows")
     return q, scale
