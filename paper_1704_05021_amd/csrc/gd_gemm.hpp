@@ -89,6 +89,7 @@ struct Finish {
     const float* q_scale;
     int act;
     int accumulate;         // O float: out += instead of =
+    int stream;             // results are more than the caches keep for a reader: stored past them
 };
 
 struct GemmArgs {
@@ -127,6 +128,14 @@ __device__ __forceinline__ float activate(int act, float z) {
     return z;
 }
 
+template <int N, typename O>
+__device__ __forceinline__ void store_result(O* p, const Pack<O, N>& r, int n, bool stream) {
+    if constexpr (N * sizeof(O) % 16 == 0) {
+        if (stream) return store_stream<N>(p, r, n);
+    }
+    store_some<N>(p, r, n);
+}
+
 // Results (j, i) to (j, i + N - 1), n of which exist, from their sums.
 template <typename O, int N>
 __device__ __forceinline__ void finish(const Finish& f, uint64_t j, uint32_t i, float (&s)[N], int n) {
@@ -145,7 +154,7 @@ __device__ __forceinline__ void finish(const Finish& f, uint64_t j, uint32_t i, 
         Pack<O, N> z;
 #pragma unroll
         for (int c = 0; c < N; ++c) z.v[c] = (O)s[c];
-        store_some<N>((O*)f.pre + j * f.pre_stride + i, z, n);
+        store_result((O*)f.pre + j * f.pre_stride + i, z, n, f.stream);
     }
     if (f.act != GD_ACT_NONE)
 #pragma unroll
@@ -164,7 +173,7 @@ __device__ __forceinline__ void finish(const Finish& f, uint64_t j, uint32_t i, 
     Pack<O, N> y;
 #pragma unroll
     for (int c = 0; c < N; ++c) y.v[c] = (O)s[c];
-    store_some<N>(out, y, n);
+    store_result(out, y, n, f.stream);
 }
 
 constexpr int kStepBytes = 128;  // of k in a step
@@ -465,13 +474,16 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
 static __device__ const u4 zero_chunk = {0, 0, 0, 0};  // what lanes past the end of k fetch
 
 // 16 bytes from base + off to each lane's place after lds_at (uniform).  The
-// instruction writes no register; load_wait says when its data is there.
+// instruction writes no register; load_wait says when its data is there.  (The
+// compiler's builtin would have it wait for all of them before the next read
+// of LDS.  m0 is reserved: the compiler sets it before each use of its own.)
 __device__ __forceinline__ void fetch(const void* base, uint32_t off, uint32_t lds_at) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds_at)
                  : "memory");
 }
 __device__ __forceinline__ void fetch_far(const void* at, uint32_t lds_at) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds_at) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds_at)
+                 : "memory");
 }
 // Until at most N fetches of this wave are under way and its LDS reads are done; then until all waves are here.
 template <int N>

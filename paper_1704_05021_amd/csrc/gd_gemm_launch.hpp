@@ -101,6 +101,8 @@ hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
             k_thin<E, O><<<dim3((a.I + kThinRows - 1) / kThinRows), dim3(kThinWaves * kWave), 0, st>>>(a);
             return hipGetLastError();
         }
+    // 32 MB is what the dies' L2 hold together (8192 x 4096 x 4096 in bfloat16: 197 us stored past them, 213 through)
+    a.fin.stream = (uint64_t)a.I * a.J * sizeof(O) >= 32ull << 20;
     bool direct = false;
     if constexpr (sizeof(E) <= 2) {
         const uint64_t p_rows = FORM >= kPAcross ? a.K : a.I, q_rows = FORM == kBothAcross ? a.K : a.J;

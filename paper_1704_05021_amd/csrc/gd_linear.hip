@@ -28,19 +28,17 @@ __device__ __forceinline__ float act_slope(int act, float z) {
 }
 
 // dz = dy act'(pre), rounded, and its sums over the block's rows.  A wave takes
-// 512 columns of a row at a time, a lane 8; the block's four waves take rows
-// in turn.  Bound by memory: 6 bytes an element in 16 bits.
+// 512 columns of a row at a time, a lane 8; the block's waves take rows in
+// turn.  Bound by memory: 6 bytes an element in 16 bits.
 constexpr int kSlopeColumns = kWave * 8;
-// The sums of few rows, one block's, go out at once.
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_slope(gd_linear_grad io, uint32_t columns, int act, float* part) {
-    __shared__ float lds[kWavesPerBlock][kSlopeColumns];
+// The sums of few rows, one block's of sixteen waves, go out at once.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave) void k_slope(gd_linear_grad io, uint32_t columns, int act, float* part) {
+    __shared__ float lds[WAVES][kSlopeColumns];
     const uint32_t c = blockIdx.x * kSlopeColumns + lane_id() * 8;
     const int n = (int)(columns - min(c, columns));
     float sum[8] = {};
-#pragma unroll 4
-    for (uint64_t row = (uint64_t)blockIdx.y * kWavesPerBlock + wave_index(); row < io.rows;
-         row += (uint64_t)gridDim.y * kWavesPerBlock) {
+    for (uint64_t row = (uint64_t)blockIdx.y * WAVES + wave_index(); row < io.rows; row += (uint64_t)gridDim.y * WAVES) {
         Pack<T, 8> d = load_some<8>((const T*)io.dy + row * io.dy_stride + c, n);
         if (act != GD_ACT_NONE) {
             const Pack<T, 8> z = load_some<8>((const T*)io.pre + row * io.pre_stride + c, n);
@@ -55,10 +53,10 @@ __global__ __launch_bounds__(kBlock) void k_slope(gd_linear_grad io, uint32_t co
 #pragma unroll
     for (int j = 0; j < 8; ++j) lds[wave_index()][lane_id() * 8 + j] = sum[j];
     __syncthreads();
-    for (uint32_t j = threadIdx.x; j < (uint32_t)kSlopeColumns; j += kBlock) {
+    for (uint32_t j = threadIdx.x; j < (uint32_t)kSlopeColumns; j += WAVES * kWave) {
         float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWavesPerBlock; ++w) s += lds[w][j];
+        for (int w = 0; w < WAVES; ++w) s += lds[w][j];
         const uint32_t col = blockIdx.x * kSlopeColumns + j;
         if (col >= columns) continue;
         if (gridDim.y == 1)
@@ -69,16 +67,23 @@ __global__ __launch_bounds__(kBlock) void k_slope(gd_linear_grad io, uint32_t co
 }
 
 hipError_t launch_slope(const gd_linear_grad& io, int type, uint32_t columns, int act, float* part, hipStream_t st) {
-    // one block down the rows up to 64 of them: a second launch costs more than the 16 turns of its waves
+    // one block down the rows up to 64 of them: a second launch costs more than the four turns of its waves
     const uint32_t groups = io.rows <= 64 ? (io.rows != 0) : (uint32_t)std::min<uint64_t>((io.rows + 15) / 16, kBiasParts);
     if (groups) {
         const dim3 grid((columns + kSlopeColumns - 1) / kSlopeColumns, groups);
+        const auto run = [&](auto zero) {
+            using T = decltype(zero);
+            if (groups == 1)
+                k_slope<T, 16><<<grid, dim3(16 * kWave), 0, st>>>(io, columns, act, part);
+            else
+                k_slope<T, 4><<<grid, dim3(4 * kWave), 0, st>>>(io, columns, act, part);
+        };
         if (type == GD_F32)
-            k_slope<float><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, part);
+            run(0.0f);
         else if (type == GD_BF16)
-            k_slope<bf16><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, part);
+            run((bf16)0.0f);
         else
-            k_slope<f16><<<grid, dim3(kBlock), 0, st>>>(io, columns, act, part);
+            run((f16)0.0f);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
