@@ -12,7 +12,7 @@
 // loaded into registers while the step before is multiplied, then stored to
 // the other half of LDS: rows of eight 16-byte chunks, the chunk's place
 // exclusive-ored with bits of the row, so that neither the stores nor the
-// matrix fragments' reads of 32 rows pile onto a bank.  Operands that lie
+// matrix fragments' reads of 16 rows pile onto a bank.  Operands that lie
 // across k are transposed in registers on their way (16-bit elements: one
 // byte permutation per two elements; 32-bit ones: none).  A matrix
 // instruction's lanes each take 16 bytes along k from one row; which k they
@@ -181,7 +181,7 @@ constexpr int kRowChunks = kStepBytes / 16;
 
 // Byte of chunk c of a tile's row in LDS.
 __device__ __forceinline__ uint32_t chunk_at(uint32_t row, uint32_t c) {
-    return row * kStepBytes + ((c ^ (row & 7u) ^ ((row >> 3) & 3u)) << 4);
+    return row * kStepBytes + ((c ^ (row >> 1 & 7u)) << 4);
 }
 
 // A step's R rows of one operand on their way from memory to LDS, the
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
 
     const uint32_t wave = wave_index(), lane = lane_id();
     const uint32_t wi = wave % TL::WI, wj = wave / TL::WI;
-    // this lane's fragment of row r, chunk pair s: the row's bits 0..4 set the chunk's place
+    // this lane's row and chunk of a fragment: bits 1 to 3 of the row set the chunk's place, those of 16 rows on do not
     const uint32_t at = chunk_at(lane & 15, lane >> 4);
     const uint32_t p_at = wi * TL::NI * 16 * kStepBytes + at;
     const uint32_t q_at = TL::BI * kStepBytes + wj * TL::NJ * 16 * kStepBytes + at;
@@ -410,10 +410,10 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
         u4 p[TL::NI], q[TL::NJ];
 #pragma unroll
         for (int i = 0; i < TL::NI; ++i)
-            p[i] = *(const u4*)(now + (((p_at ^ (c << 6)) ^ ((i & 1) << 5)) + i * 16 * kStepBytes));
+            p[i] = *(const u4*)(now + ((p_at ^ (c << 6)) + i * 16 * kStepBytes));
 #pragma unroll
         for (int j = 0; j < TL::NJ; ++j)
-            q[j] = *(const u4*)(now + (((q_at ^ (c << 6)) ^ ((j & 1) << 5)) + j * 16 * kStepBytes));
+            q[j] = *(const u4*)(now + ((q_at ^ (c << 6)) + j * 16 * kStepBytes));
 #pragma unroll
         for (int i = 0; i < TL::NI; ++i)
 #pragma unroll
@@ -466,7 +466,9 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
 // for step s + DEEP.  Each fragment is read
 // right behind the last use of the one whose registers it takes.
 //
-// Along k a row's eight 16-byte chunks change places by the row's low bits.
+// Along k a row's eight 16-byte chunks change places by bits 1 to 3 of the row:
+// the 16 lanes that a 16-byte read serves at once take their rows from both
+// halves of a fragment (bits 0 to 2 cost a second turn for every read).
 // Across k the tile lies in LDS as in memory, a row for each k, and the
 // transposing LDS read gives each lane four k of one row; pairs of 16-byte
 // chunks change places by the low bits of k.  A load puts its lanes' data
@@ -507,9 +509,14 @@ struct TileFetch {
     static __device__ __forceinline__ uint32_t at(int n) {
         return (n * (THREADS / kWave) + wave_index()) * kWave * 16 + lane_id() * 16;
     }
-    static __device__ __forceinline__ uint32_t place(uint32_t k) { return kUnits >= 8 ? (k & 3) << 1 : k & 3; }
+    // The 32 lanes that a transposing read serves at once take k to k + 3 and k + 8 to k + 11 of one pair of chunks: eight
+    // runs of 32 bytes, one on each eighth of the banks.  (Tiles of 64 rows turn by half the banks with every k.)
+    static __device__ __forceinline__ uint32_t place(uint32_t k) {
+        static_assert(!ACROSS || kUnits == 4 || kUnits == 8 || kUnits == 16, "exclusive-or stays within a row");
+        return kUnits >= 8 ? (k & 3) << 1 | (k >> 3 & 1) : (k >> 1 & 1) | (k >> 3 & 1) << 1;
+    }
     static __device__ __forceinline__ uint32_t row_place(uint32_t row) {
-        return (row & 7) ^ ((row >> 3) & 1);
+        return row >> 1 & 7;
     }
     static __device__ __forceinline__ uint32_t k_of(int n) {
         if constexpr (ACROSS) return at(n) / kRowBytes;
@@ -558,7 +565,7 @@ struct TileFetch {
     // The fragment of rows row0 (a multiple of 32) on; lane is lane_at(c), the tile starts at `tile` in LDS.
     static __device__ __forceinline__ u4 fragment(const char* tile, uint32_t row0, uint32_t lane) {
         if constexpr (ACROSS) {
-            // rows 32 on are two units on; the place's exclusive-or does not carry into them beyond 8 units
+            // rows 16 on are the next pair of chunks; a k's row is a power of two, so the exclusive-or keeps to it
             typedef short s4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s4 lds_s4;
             const char* p = tile + (lane ^ (row0 / 16 << 5));

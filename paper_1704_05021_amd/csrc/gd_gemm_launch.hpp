@@ -123,13 +123,15 @@ hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
     int tile = 0;
     constexpr TileCost kCosts[] = {kSmallCost, kMidCost, kWideCost, kLongCost, kBigCost};
     for (int t = 0; t < (direct ? 5 : 2); ++t) {  // the larger tiles take operands placed in LDS only
+        if (FORM == kBothAcross && t == 3) continue;  // rows of 192 across k would not be a power of two in LDS
         const TilePlan p = plan_tiles(kCosts[t], a.I, a.J, steps, given.floats);
         if (p.us < best.us) best = p, tile = t;
     }
     const auto run = [&](auto tl) { return launch_tiles<E, O, FORM, decltype(tl)>(a, best.splits, direct, st); };
     if constexpr (sizeof(E) <= 2) {
         if (tile == 4) return run(TileBig());
-        if (tile == 3) return run(TileLong());
+        if constexpr (FORM != kBothAcross)
+            if (tile == 3) return run(TileLong());
         if (tile == 2) return run(TileWide());
     }
     return tile == 1 ? run(TileMid()) : run(TileSmall());

@@ -90,7 +90,10 @@ def test_sizes(kind, rows, k, n):
                                       (100, 256 * 14 + 8, 256 * 15 - 9), (256 * 15, 256 * 14, 64), (128 * 15, 136, 128 * 14),
                                       (128 * 14 + 5, 200, 128 * 15 - 4), (64, 128 * 15, 128 * 14 + 4), (128 * 15 - 3, 128 * 14, 40),
                                       (64, 4096, 64), (90, 4100, 70), (4096, 64, 64), (5000, 70, 90), (70, 64, 4096),
-                                      (60, 90, 5003), (10, 4096, 4096), (7, 8191, 33)])
+                                      (60, 90, 5003), (10, 4096, 4096), (7, 8191, 33),
+                                      # tiles of 192 and 128 rows beside 256, in each of the three products
+                                      (64, 4096, 3000), (3000, 128, 4096), (3000, 4096, 128), (2990, 136, 4080),
+                                      (2048, 128, 4096), (2048, 4096, 128), (128, 4096, 2048), (200, 4088, 2040)])
 def test_tiles_are_exact_on_whole_numbers(kind, rows, k, n):
     """Sums below 2^24 of whole numbers are exact, so every result is the exact one, rounded once."""
     t = TYPES[kind]
