@@ -184,48 +184,73 @@ __device__ __forceinline__ uint32_t chunk_at(uint32_t row, uint32_t c) {
     return row * kStepBytes + ((c ^ (row >> 1 & 7u)) << 4);
 }
 
+// v moved `bytes` towards its start, zeros behind it.
+__device__ __forceinline__ u4 shift_down(u4 v, uint32_t bytes) {
+    const u4 zero = {0, 0, 0, 0};
+    if (bytes >= 16) v = zero;
+    if (bytes & 8) v = u4{v[2], v[3], 0, 0};
+    if (bytes & 4) v = u4{v[1], v[2], v[3], 0};
+    const uint32_t by = bytes & 3;
+    return u4{__builtin_amdgcn_alignbyte(v[1], v[0], by), __builtin_amdgcn_alignbyte(v[2], v[1], by),
+              __builtin_amdgcn_alignbyte(v[3], v[2], by), __builtin_amdgcn_alignbyte(0u, v[3], by)};
+}
+
 // A step's R rows of one operand on their way from memory to LDS, the
-// block's THREADS threads sharing them.
+// block's THREADS threads sharing them.  Where a row or k ends inside a
+// vector, the vector that ends there is read, and moved into place on its way
+// to LDS: no load waits for another (element by element, each behind its own
+// condition, 20 x 650 x 650 took 33 us backward, so 13).  Rows shorter than a vector
+// (few) are read by elements.
 template <typename E, bool ACROSS, int R, int THREADS>
 struct TileLoad;
 
 template <typename E, int R, int THREADS>
 struct TileLoad<E, false, R, THREADS> {
-    static constexpr int CE = 16 / sizeof(E), N = R * kRowChunks / THREADS;
+    static constexpr int CE = 16 / sizeof(E), KE = kStepBytes / sizeof(E), N = R * kRowChunks / THREADS;
     static_assert(R * kRowChunks % THREADS == 0, "every thread carries whole chunks");
     const E* base;       // the tile's first row at the first step's k
     uint32_t off[N];     // elements
+    bool few;            // k is shorter than a chunk
     struct Regs {
         u4 r[N];
     };
+    static __device__ __forceinline__ uint32_t first_k(int n) { return (n * THREADS + threadIdx.x) % kRowChunks * CE; }
 
-    __device__ void start(const void* p, uint64_t stride, uint32_t row0, uint32_t rows, uint32_t k0) {
+    __device__ void start(const void* p, uint64_t stride, uint32_t row0, uint32_t rows, uint32_t k0, uint32_t k) {
         base = (const E*)p + (uint64_t)row0 * stride + k0;
+        few = k < (uint32_t)CE;
 #pragma unroll
         for (int n = 0; n < N; ++n) {  // rows past the end repeat the last one; their results are dropped
             const uint32_t id = n * THREADS + threadIdx.x;
-            off[n] = min(id / kRowChunks, rows - row0 - 1) * (uint32_t)stride + id % kRowChunks * CE;
+            off[n] = min(id / kRowChunks, rows - row0 - 1) * (uint32_t)stride + first_k(n);
         }
     }
+    __device__ __forceinline__ bool always_whole() const { return true; }
     __device__ __forceinline__ void load_whole(Regs& g, uint32_t step) const {
-        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E));
+        const E* at = base + (uint64_t)step * KE;
 #pragma unroll
         for (int n = 0; n < N; ++n) g.r[n] = bits_as<u4>(load_pack<CE>(at + off[n]));
     }
     __device__ __forceinline__ void load(Regs& g, uint32_t step, uint32_t k_left) const {
-        if (k_left >= kStepBytes / sizeof(E)) return load_whole(g, step);
-        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E));
+        if (k_left >= (uint32_t)KE) return load_whole(g, step);
+        const E* at = base + (uint64_t)step * KE;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int have = (int)k_left - (int)((n * THREADS + threadIdx.x) % kRowChunks * CE);
-            g.r[n] = bits_as<u4>(load_some<CE>(at + off[n], have));
+            const int have = (int)k_left - (int)first_k(n);
+            if (few)
+                g.r[n] = bits_as<u4>(load_some<CE>(at + off[n], have));
+            else
+                g.r[n] = bits_as<u4>(load_pack<CE>(at + off[n] + min(have - CE, 0)));
         }
     }
-    __device__ __forceinline__ void store(const Regs& g, char* lds) const {
+    __device__ __forceinline__ void store(const Regs& g, char* lds, uint32_t k_left) const {
+        const bool end = k_left < (uint32_t)KE && !few;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const uint32_t id = n * THREADS + threadIdx.x;
-            *(u4*)(lds + chunk_at(id / kRowChunks, id % kRowChunks)) = g.r[n];
+            u4 v = g.r[n];
+            if (end) v = shift_down(v, (uint32_t)max((int)first_k(n) + CE - (int)k_left, 0) * (uint32_t)sizeof(E));
+            *(u4*)(lds + chunk_at(id / kRowChunks, id % kRowChunks)) = v;
         }
     }
 };
@@ -233,55 +258,90 @@ struct TileLoad<E, false, R, THREADS> {
 template <typename E, int R, int THREADS>
 struct TileLoad<E, true, R, THREADS> {
     // an item: one chunk of k of four neighbouring rows of the tile
-    static constexpr int CE = 16 / sizeof(E), ITEMS = R / 4 * kRowChunks, N = (ITEMS + THREADS - 1) / THREADS;
+    static constexpr int CE = 16 / sizeof(E), KE = kStepBytes / sizeof(E);
+    static constexpr int ITEMS = R / 4 * kRowChunks, N = (ITEMS + THREADS - 1) / THREADS;
     const E* base;
     uint64_t stride;
-    int cols[N];         // how many of the item's four rows exist
+    uint32_t rows;       // of the operand from the tile's first on
+    bool few, edge;      // the operand has fewer than four rows; the tile has rows past its end
     struct Regs {
         Pack<E, 4> r[N][CE];
     };
 
     static __device__ __forceinline__ uint32_t group(int n) { return (n * THREADS + threadIdx.x) % (R / 4); }
     static __device__ __forceinline__ uint32_t chunk(int n) { return (n * THREADS + threadIdx.x) / (R / 4); }
+    // how far the item's vector of four rows lies before the item
+    __device__ __forceinline__ int before(int n) const { return max((int)group(n) * 4 + 4 - (int)rows, 0); }
 
-    __device__ void start(const void* p, uint64_t st, uint32_t row0, uint32_t rows, uint32_t k0) {
+    __device__ void start(const void* p, uint64_t st, uint32_t row0, uint32_t all, uint32_t k0, uint32_t) {
         stride = st;
         base = (const E*)p + (uint64_t)k0 * st + row0;
-#pragma unroll
-        for (int n = 0; n < N; ++n) cols[n] = (int)(rows - row0) - (int)(group(n) * 4);
+        rows = min(all - row0, (uint32_t)R);
+        few = all < 4;
+        edge = rows < (uint32_t)R;
     }
+    __device__ __forceinline__ bool always_whole() const { return !few; }
     __device__ __forceinline__ void load_whole(Regs& g, uint32_t step) const {
-        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E)) * stride;
+        const E* at = base + (uint64_t)step * KE * stride;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
-            const uint32_t off = chunk(n) * CE * (uint32_t)stride + group(n) * 4;
+            const int64_t off = (int64_t)(chunk(n) * CE * (uint32_t)stride + group(n) * 4) - before(n);
 #pragma unroll
             for (int e = 0; e < CE; ++e) g.r[n][e] = load_pack<4>(at + (uint64_t)e * stride + off);
         }
     }
     __device__ __forceinline__ void load(Regs& g, uint32_t step, uint32_t k_left) const {
-        const E* at = base + (uint64_t)step * (kStepBytes / sizeof(E)) * stride;
+        const E* at = base + (uint64_t)step * KE * stride;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
-            const uint32_t off = chunk(n) * CE * (uint32_t)stride + group(n) * 4;
 #pragma unroll
-            for (int e = 0; e < CE; ++e)
-                g.r[n][e] = load_some<4>(at + (uint64_t)e * stride + off, chunk(n) * CE + e < k_left ? cols[n] : 0);
+            for (int e = 0; e < CE; ++e) {
+                const uint32_t k = chunk(n) * CE + e;
+                const E* row = at + (uint64_t)min(k, k_left - 1) * stride + group(n) * 4;  // past the end of k the last again
+                if (few)
+                    g.r[n][e] = load_some<4>(row, (int)rows - (int)(group(n) * 4));
+                else
+                    g.r[n][e] = load_pack<4>(row - before(n));
+            }
         }
     }
-    __device__ __forceinline__ void store(const Regs& g, char* lds) const {
+    __device__ __forceinline__ void store(const Regs& g, char* lds, uint32_t k_left) const {
+        const bool end = k_left < (uint32_t)KE;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (N * THREADS > ITEMS && chunk(n) >= (uint32_t)kRowChunks) continue;
+            Pack<E, 4> r[CE];
+#pragma unroll
+            for (int e = 0; e < CE; ++e) r[e] = g.r[n][e];
+            if (edge && !few) {
+#pragma unroll
+                for (int e = 0; e < CE; ++e) r[e] = moved(r[e], before(n));
+            }
+            if (end) {
+#pragma unroll
+                for (int e = 0; e < CE; ++e)
+                    if (chunk(n) * CE + e >= k_left) r[e] = Pack<E, 4>{};
+            }
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
                 Pack<E, CE> c;
 #pragma unroll
-                for (int e = 0; e < CE; ++e) c.v[e] = g.r[n][e].v[m];
+                for (int e = 0; e < CE; ++e) c.v[e] = r[e].v[m];
                 *(u4*)(lds + chunk_at(group(n) * 4 + m, chunk(n))) = bits_as<u4>(c);
             }
+        }
+    }
+    // r with its first `by` elements gone; what fills the end is a row past the operand's, whose results are dropped
+    static __device__ __forceinline__ Pack<E, 4> moved(const Pack<E, 4>& r, int by) {
+        if constexpr (sizeof(E) == 2) {
+            return bits_as<Pack<E, 4>>(bits_as<uint64_t>(r) >> (by * 16 & 63));
+        } else {
+            Pack<E, 4> m = r;
+            if (by & 2) m.v[0] = m.v[2], m.v[1] = m.v[3];
+            if (by & 1) m.v[0] = m.v[1], m.v[1] = m.v[2], m.v[2] = m.v[3];
+            return m;
         }
     }
 };
@@ -317,7 +377,7 @@ __device__ __forceinline__ void tile_of(const GemmArgs& a, uint32_t b, uint32_t&
 // all its i at a time, so that it reads and writes whole runs of memory.
 template <typename E, typename O, typename TL>
 __device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::Sum (&acc)[TL::NI][TL::NJ], char* lds,
-                                           uint32_t i0, uint32_t j0) {
+                                           uint32_t i0, uint32_t j0, uint32_t split) {
     const uint32_t wave = wave_index(), lane = lane_id(), wi = wave % TL::WI, wj = wave / TL::WI;
     constexpr int W = TL::NI * 16;  // results of a row
     float* rows = (float*)(lds + wave * (W * 16 * 4));
@@ -345,7 +405,7 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::S
                     Pack<float, kPer> v;
 #pragma unroll
                     for (int c = 0; c < kPer; ++c) v.v[c] = s[c];
-                    store_some<kPer>(a.part + ((uint64_t)blockIdx.y * a.J + row) * a.I + i, v, n);
+                    store_some<kPer>(a.part + ((uint64_t)split * a.J + row) * a.I + i, v, n);
                 } else {
                     if constexpr (sizeof(E) == 1)
 #pragma unroll
@@ -358,22 +418,22 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::S
     }
 }
 
+// Tile `block` of a product, its share `split` of k, through registers; lds holds TL::kLds bytes.
 template <typename E, typename O, bool PA, bool QA, typename TL, int SETS = 2>
-__global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
+__device__ __forceinline__ void gemm_staged(const GemmArgs& a, uint32_t block, uint32_t split, char* lds) {
     using M = Mma<E>;
-    __shared__ __align__(16) char lds[TL::kLds];
     constexpr uint32_t KE = kStepBytes / sizeof(E);
     uint32_t ti, tj;
-    tile_of(a, blockIdx.x, ti, tj);
+    tile_of(a, block, ti, tj);
     const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
-    const uint32_t k0 = blockIdx.y * a.steps * KE;
+    const uint32_t k0 = split * a.steps * KE;
     const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * KE);
     const uint32_t steps = k_end > k0 ? (k_end - k0 + KE - 1) / KE : 0;
 
     TileLoad<E, PA, TL::BI, TL::kThreads> lp;
     TileLoad<E, QA, TL::BJ, TL::kThreads> lq;
-    lp.start(a.p, a.p_stride, i0, a.I, k0);
-    lq.start(a.q, a.q_stride, j0, a.J, k0);
+    lp.start(a.p, a.p_stride, i0, a.I, k0, a.K);
+    lq.start(a.q, a.q_stride, j0, a.J, k0, a.K);
     typename M::Sum acc[TL::NI][TL::NJ];
 #pragma unroll
     for (int i = 0; i < TL::NI; ++i)
@@ -392,18 +452,16 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
     typename decltype(lp)::Regs rp[SETS];
     typename decltype(lq)::Regs rq[SETS];
     const uint32_t left = k_end > k0 ? k_end - k0 : 0;
-    // steps whose every load is a whole vector: those of whole length, in tiles with no ragged edge across k
-    const bool edge = (PA && a.I - i0 < (uint32_t)TL::BI) || (QA && a.J - j0 < (uint32_t)TL::BJ);
-    const uint32_t whole = edge ? 0 : left / KE;
+    const uint32_t whole = lp.always_whole() && lq.always_whole() ? left / KE : 0;  // steps whose every load is a vector
     const auto load = [&](int set, uint32_t s) {
         if (s >= steps) return;
         lp.load(rp[set], s, left - s * KE);
         lq.load(rq[set], s, left - s * KE);
     };
-    const auto store = [&](int set, uint32_t s) {
+    const auto store = [&](int set, uint32_t s, uint32_t k_left) {
         char* to = lds + (s & 1) * TL::kStage;
-        lp.store(rp[set], to);
-        lq.store(rq[set], to + TL::BI * kStepBytes);
+        lp.store(rp[set], to, k_left);
+        lq.store(rq[set], to + TL::BI * kStepBytes, k_left);
     };
     const auto multiply = [&](uint32_t s, int c) {
         const char* now = lds + (s & 1) * TL::kStage;
@@ -423,7 +481,7 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
     // ago, to the other half, and loads into its registers anew
     if (steps) {
         load(0, 0);
-        store(0, 0);
+        store(0, 0, left);
 #pragma unroll
         for (int d = 0; d < SETS; ++d) load(d, d + 1);
     }
@@ -433,7 +491,7 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
 #pragma unroll
         for (int d = 0; d < SETS; ++d) {
             multiply(s + d, 0);
-            store(d, s + d + 1);
+            store(d, s + d + 1, KE);
             lp.load_whole(rp[d], s + d + 1 + SETS);
             lq.load_whole(rq[d], s + d + 1 + SETS);
             multiply(s + d, 1);
@@ -445,13 +503,19 @@ __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
         for (int d = 0; d < SETS; ++d) {
             if (s + d >= steps) break;
             multiply(s + d, 0);
-            if (s + d + 1 < steps) store(d, s + d + 1);
+            if (s + d + 1 < steps) store(d, s + d + 1, left - (s + d + 1) * KE);
             load(d, s + d + 1 + SETS);
             multiply(s + d, 1);
             __syncthreads();
         }
 
-    store_tile<E, O, TL>(a, acc, lds, i0, j0);
+    store_tile<E, O, TL>(a, acc, lds, i0, j0, split);
+}
+
+template <typename E, typename O, bool PA, bool QA, typename TL>
+__global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
+    __shared__ __align__(16) char lds[TL::kLds];
+    gemm_staged<E, O, PA, QA, TL>(a, blockIdx.x, blockIdx.y, lds);
 }
 
 // ---- The same product with operands that memory instructions place in LDS ----
@@ -593,18 +657,18 @@ __global__ __launch_bounds__(kBlock) void k_pad(const E* from, uint64_t stride, 
     }
 }
 
+// Tile `block` of a product, its share `split` of k; lds holds TL::DEEP steps.
 template <typename E, typename O, bool PA, bool QA, typename TL>
-__global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
+__device__ __forceinline__ void gemm_fetch(const GemmArgs& a, uint32_t block, uint32_t split, char* lds) {
     using M = Mma<E>;
     using FP = TileFetch<E, PA, TL::BI, TL::kThreads>;
     using FQ = TileFetch<E, QA, TL::BJ, TL::kThreads>;
     static_assert(FP::kBytes + FQ::kBytes == TL::kStage);
     constexpr int DEEP = TL::DEEP, kLoads = FP::N + FQ::N;
-    __shared__ __align__(1024) char lds[DEEP * TL::kStage];
     uint32_t ti, tj;
-    tile_of(a, blockIdx.x, ti, tj);
+    tile_of(a, block, ti, tj);
     const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
-    const uint32_t k0 = blockIdx.y * a.steps * FP::KE;
+    const uint32_t k0 = split * a.steps * FP::KE;
     const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * FP::KE);
     const uint32_t left = k_end > k0 ? k_end - k0 : 0, steps = (left + FP::KE - 1) / FP::KE, whole = left / FP::KE;
     FP fp;
@@ -712,7 +776,32 @@ __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
         }
     }
     __syncthreads();
-    store_tile<E, O, TL>(a, acc, lds, i0, j0);
+    store_tile<E, O, TL>(a, acc, lds, i0, j0, split);
+}
+
+template <typename E, typename O, bool PA, bool QA, typename TL>
+__global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
+    __shared__ __align__(1024) char lds[TL::DEEP * TL::kStage];
+    gemm_fetch<E, O, PA, QA, TL>(a, blockIdx.x, blockIdx.y, lds);
+}
+
+// The two products of a small layer's backward pass in one launch: blocks
+// below `first` take the input's gradient, the others the weight's.
+template <typename E, bool DIRECT>
+__global__ __launch_bounds__(TileSmall::kThreads, DIRECT ? 1 : 2) void k_gemm_pair(GemmArgs dx, GemmArgs dw, uint32_t first) {
+    __shared__ __align__(1024) char lds[DIRECT ? TileSmall::DEEP * TileSmall::kStage : TileSmall::kLds];
+    const bool is_dx = blockIdx.x < first;
+    if constexpr (DIRECT) {
+        if (is_dx)
+            gemm_fetch<E, E, true, false, TileSmall>(dx, blockIdx.x, 0, lds);
+        else
+            gemm_fetch<E, float, true, true, TileSmall>(dw, blockIdx.x - first, 0, lds);
+    } else {
+        if (is_dx)
+            gemm_staged<E, E, true, false, TileSmall>(dx, blockIdx.x, 0, lds);
+        else
+            gemm_staged<E, float, true, true, TileSmall>(dw, blockIdx.x - first, 0, lds);
+    }
 }
 
 // Joins the splits' sums, four results a thread.
@@ -822,5 +911,9 @@ struct GemmRoom {
 // One product.  Operand types: E is O's type, or int8 with kAlong.
 template <typename E, typename O, int FORM>
 hipError_t launch_gemm(GemmArgs a, const GemmRoom& room, hipStream_t st);
+
+// The products of a layer's backward pass in its type T, each where it is given.
+template <typename T>
+hipError_t launch_backward(const GemmArgs* dx, const GemmArgs* dw, const GemmRoom& room, hipStream_t st);
 
 }  // namespace gd

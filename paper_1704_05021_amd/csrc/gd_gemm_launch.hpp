@@ -94,6 +94,26 @@ hipError_t launch_tiles(GemmArgs a, uint64_t splits, bool direct, hipStream_t st
     return hipGetLastError();
 }
 
+// The tile (0 the smallest) and the split of k of a product.
+struct Choice {
+    int tile;
+    uint32_t splits;
+};
+template <typename E, int FORM>
+Choice choose(const GemmArgs& a, bool direct, uint64_t room) {
+    constexpr uint32_t KE = kStepBytes / sizeof(E);
+    const uint64_t steps = ((uint64_t)a.K + KE - 1) / KE;
+    TilePlan best{1e300, 1};
+    int tile = 0;
+    constexpr TileCost kCosts[] = {kSmallCost, kMidCost, kWideCost, kLongCost, kBigCost};
+    for (int t = 0; t < (direct ? 5 : 2); ++t) {  // the larger tiles take operands placed in LDS only
+        if (FORM == kBothAcross && t == 3) continue;  // rows of 192 across k would not be a power of two in LDS
+        const TilePlan p = plan_tiles(kCosts[t], a.I, a.J, steps, room);
+        if (p.us < best.us) best = p, tile = t;
+    }
+    return {tile, best.splits};
+}
+
 template <typename E, typename O, int FORM>
 hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
     if constexpr (FORM == kAlong)
@@ -117,17 +137,9 @@ hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
             if (direct) a = b;
         }
     }
-    constexpr uint32_t KE = kStepBytes / sizeof(E);
-    const uint64_t steps = ((uint64_t)a.K + KE - 1) / KE;
-    TilePlan best{1e300, 1};
-    int tile = 0;
-    constexpr TileCost kCosts[] = {kSmallCost, kMidCost, kWideCost, kLongCost, kBigCost};
-    for (int t = 0; t < (direct ? 5 : 2); ++t) {  // the larger tiles take operands placed in LDS only
-        if (FORM == kBothAcross && t == 3) continue;  // rows of 192 across k would not be a power of two in LDS
-        const TilePlan p = plan_tiles(kCosts[t], a.I, a.J, steps, given.floats);
-        if (p.us < best.us) best = p, tile = t;
-    }
+    const Choice best = choose<E, FORM>(a, direct, given.floats);
     const auto run = [&](auto tl) { return launch_tiles<E, O, FORM, decltype(tl)>(a, best.splits, direct, st); };
+    const int tile = best.tile;
     if constexpr (sizeof(E) <= 2) {
         if (tile == 4) return run(TileBig());
         if constexpr (FORM != kBothAcross)
@@ -135,6 +147,43 @@ hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
         if (tile == 2) return run(TileWide());
     }
     return tile == 1 ? run(TileMid()) : run(TileSmall());
+}
+
+// Both products in one launch, where each takes the smallest tile and does
+// not split k (40 x 784 x 512: 11.6 us in place of 15.0).
+template <typename T>
+bool pair_backward(GemmArgs dx, GemmArgs dw, const GemmRoom& room, hipStream_t st, hipError_t& e) {
+    const bool direct = sizeof(T) == 2 && whole_chunks<T>(dx.p, dx.p_stride, dx.I) &&
+                        whole_chunks<T>(dx.q, dx.q_stride, dx.K) && whole_chunks<T>(dw.p, dw.p_stride, dw.I);
+    if (!direct && room.pad && (double)dx.I * dx.J * dx.K >= kPadWork) return false;
+    const Choice a = choose<T, kPAcross>(dx, direct, room.floats), b = choose<T, kBothAcross>(dw, direct, room.floats);
+    if (a.tile || b.tile || a.splits > 1 || b.splits > 1) return false;
+    uint64_t blocks = 0, first = 0;
+    for (GemmArgs* g : {&dx, &dw}) {
+        constexpr uint32_t KE = kStepBytes / sizeof(T);
+        g->tiles_i = (g->I + TileSmall::BI - 1) / TileSmall::BI;
+        g->tiles_j = (g->J + TileSmall::BJ - 1) / TileSmall::BJ;
+        g->steps = (g->K + KE - 1) / KE;
+        g->part = nullptr;
+        first = blocks;
+        blocks += (uint64_t)g->tiles_i * g->tiles_j;
+    }
+    if (blocks * TileSmall::kThreads > 0xFFFFFFFFull) return false;
+    const dim3 grid((uint32_t)blocks), block(TileSmall::kThreads);
+    if constexpr (sizeof(T) == 2)
+        if (direct) k_gemm_pair<T, true><<<grid, block, 0, st>>>(dx, dw, (uint32_t)first);
+    if (!direct) k_gemm_pair<T, false><<<grid, block, 0, st>>>(dx, dw, (uint32_t)first);
+    e = hipGetLastError();
+    return true;
+}
+
+template <typename T>
+hipError_t launch_backward(const GemmArgs* dx, const GemmArgs* dw, const GemmRoom& room, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    if (dx && dw && pair_backward<T>(*dx, *dw, room, st, e)) return e;
+    if (dx) e = launch_gemm<T, T, kPAcross>(*dx, room, st);
+    if (dw && e == hipSuccess) e = launch_gemm<T, float, kBothAcross>(*dw, room, st);
+    return e;
 }
 
 }  // namespace gd

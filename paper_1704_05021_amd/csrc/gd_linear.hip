@@ -96,14 +96,6 @@ hipError_t forward(const GemmArgs& a, const GemmRoom& room, bool int8, hipStream
     return int8 ? launch_gemm<int8_t, T, kAlong>(a, room, st) : launch_gemm<T, T, kAlong>(a, room, st);
 }
 
-template <typename T>
-hipError_t backward(const GemmArgs* dx, const GemmArgs* dw, const GemmRoom& room, hipStream_t st) {
-    hipError_t e = hipSuccess;
-    if (dx) e = launch_gemm<T, T, kPAcross>(*dx, room, st);
-    if (dw && e == hipSuccess) e = launch_gemm<T, float, kBothAcross>(*dw, room, st);
-    return e;
-}
-
 }  // namespace gd
 
 struct gd_linear {
@@ -245,9 +237,9 @@ gd_status gd_linear_backward(gd_linear* l, const gd_linear_grad* io, void* strea
     const gd::GemmArgs *want_dx = rows && io->dx ? &dx : nullptr,
                        *want_dw = io->dweight && (rows || !io->accumulate) ? &dw : nullptr;
     const gd::GemmRoom room{gd::kLinearRoom, l->pad, l->pad_bytes};
-    const hipError_t e = l->type == GD_F32    ? gd::backward<float>(want_dx, want_dw, room, st)
-                         : l->type == GD_BF16 ? gd::backward<gd::bf16>(want_dx, want_dw, room, st)
-                                              : gd::backward<gd::f16>(want_dx, want_dw, room, st);
+    const hipError_t e = l->type == GD_F32    ? gd::launch_backward<float>(want_dx, want_dw, room, st)
+                         : l->type == GD_BF16 ? gd::launch_backward<gd::bf16>(want_dx, want_dw, room, st)
+                                              : gd::launch_backward<gd::f16>(want_dx, want_dw, room, st);
     return e == hipSuccess ? GD_OK : GD_ERR_HIP;
 }
 

@@ -192,7 +192,17 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_norm_back(gd_nor
         Pack<float, 8> d;
 #pragma unroll
         for (int j = 0; j < 8; ++j) d.v[j] = dw[i][j];
-        store_some<8>(part + (uint64_t)blockIdx.x * dim + min(e, dim), d, (int)(dim - min(e, dim)));
+        const int n = (int)(dim - min(e, dim));
+        if (gridDim.x == 1) {  // few rows: the block's share is all of it
+            if (io.accumulate) {
+                const Pack<float, 8> was = load_some<8>(io.dweight + min(e, dim), n);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d.v[j] += was.v[j];
+            }
+            store_some<8>(io.dweight + min(e, dim), d, n);
+        } else {
+            store_some<8>(part + (uint64_t)blockIdx.x * dim + min(e, dim), d, n);
+        }
     }
 }
 
@@ -242,13 +252,17 @@ template <typename T, int WAVES, int V>
 hipError_t launch_norm_back(const gd_norm_grad& io, uint32_t dim, float* part, hipStream_t st) {
     using S = NormShape<WAVES>;
     const uint32_t most = std::min(kNormBackWaves * kWave / S::kThreads, kNormParts);
-    const uint32_t parts = (uint32_t)std::min<uint64_t>((io.rows + S::kRows - 1) / S::kRows, most);
+    const uint64_t turns = (io.rows + S::kRows - 1) / S::kRows;
+    // few rows go to one block, which writes the weight's gradient itself: 8 x 500 take 8.2 us, with the second launch
+    // 11.2; 4 x 8192 would take 12.1, with it 11.5
+    const bool one = turns <= 4 && turns * dim <= 1u << 14;
+    const uint32_t parts = one ? (turns != 0) : (uint32_t)std::min<uint64_t>(turns, most);
     if (parts) {
         k_norm_back<T, WAVES, V><<<dim3(parts), dim3(S::kThreads), 0, st>>>(io, dim, io.dweight ? part : nullptr);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (!io.dweight || (!parts && io.accumulate)) return hipSuccess;
+    if (!io.dweight || parts == 1 || (!parts && io.accumulate)) return hipSuccess;
     return launch_sum_parts(part, parts, dim, io.dweight, io.accumulate != 0, st);
 }
 

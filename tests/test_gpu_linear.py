@@ -112,6 +112,46 @@ def test_tiles_are_exact_on_whole_numbers(kind, rows, k, n):
         assert torch.equal(op.forward_int8(q, s, wq, ws), want.to(t))
 
 
+def guarded(a, seed):
+    """a inside a wider buffer of NaN, off any alignment."""
+    lead, gap = seed % 5, 1 + seed % 7
+    wide = torch.full((a.shape[0] + 2, a.shape[1] + lead + gap), math.nan, dtype=a.dtype, device="cuda")
+    inner = wide[1:1 + a.shape[0], lead:lead + a.shape[1]]
+    inner.copy_(a)
+    return inner
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("k", [1, 2, 3, 4, 5, 7, 8, 9, 31, 33, 62, 65, 131, 257])
+def test_ends_inside_a_vector(kind, k):
+    """Rows and k that end anywhere in a vector: exact sums, and nothing read past the operands reaches them."""
+    t, f = TYPES[kind], lambda a: a.double()  # noqa: E731
+    for rows in (1, 2, 3, 5, 18, 66, 131):
+        for n in (1, 2, 3, 6, 13, 67, 130):
+            x, w, dy = (guarded(whole(i + k, *s, dtype=t), rows + n + i) for i, s in enumerate([(rows, k), (n, k), (rows, n)]))
+            op = gd.Linear(k, n, t, max_rows=rows)
+            assert torch.equal(op.forward(x, w), (f(x) @ f(w).t()).to(t)), (rows, n)
+            dx, dw, db, _ = op.backward(dy, x, w, dbias=True)
+            assert torch.equal(dx, (f(dy) @ f(w)).to(t)), (rows, n)
+            assert torch.equal(dw, (f(dy).t() @ f(x)).float()) and torch.equal(db, f(dy).sum(0).float()), (rows, n)
+            q, wq = whole(7, rows, k, dtype=torch.int8), whole(8, n, k, dtype=torch.int8)
+            y = op.forward_int8(q, torch.ones(rows, device="cuda"), wq, torch.ones(n, device="cuda"))
+            assert torch.equal(y, (f(q) @ f(wq).t()).to(t)), (rows, n)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,k,n", [(40, 96, 80), (37, 90, 75), (150, 301, 67)])
+def test_gradients_that_are_not_finite_stay_in_their_rows(kind, rows, k, n):
+    t, f = TYPES[kind], lambda a: a.double()  # noqa: E731
+    x, w, dy = whole(1, rows, k, dtype=t), whole(2, n, k, dtype=t), whole(3, rows, n, dtype=t)
+    op = gd.Linear(k, n, t, max_rows=rows)
+    dx, dw = (f(dy) @ f(w)).to(t), (f(dy).t() @ f(x)).float()
+    dy[rows - 1, n - 1] = math.nan  # the last of the last row, which loads past the end repeat
+    gx, gw = op.backward(dy, x, w)[:2]
+    assert torch.equal(gx[:-1], dx[:-1]) and bool(gx[-1].isnan().all())
+    assert torch.equal(gw[:-1], dw[:-1]) and bool(gw[-1].isnan().all())
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("rows,k,n", [(1, 784, 512), (5, 100, 7), (40, 1000, 300), (200, 4096, 130)])
 def test_int8_with_everything_in_the_epilogue(kind, rows, k, n):

@@ -128,6 +128,19 @@ def test_accumulate_and_no_rows():
     assert float(total.abs().sum()) == 0
 
 
+@pytest.mark.parametrize("rows,dim", [(1, 5), (7, 60), (9, 60), (16, 500), (17, 500), (4, 2000), (5, 2000), (2, 8000), (3, 8000)])
+def test_few_rows_accumulate(rows, dim):
+    """Up to a few rows the weight's gradient is written by the block that sums it, past them by a second launch."""
+    x, dy, w = draw(1, rows, dim), draw(2, rows, dim), draw(3, dim)
+    op = gd.RMSNorm(dim, torch.float32)
+    dx, dw = op.backward(dy, x, w)
+    flat = torch.full((dim + 4,), 0.5, device="cuda")
+    dx2, _ = op.backward(dy, x, w, dweight=flat[1:1 + dim], accumulate=True)
+    assert torch.equal(dx, dx2) and bool((flat[:1] == 0.5).all() and (flat[1 + dim:] == 0.5).all())
+    total = d(dw) + 0.5  # dw is rounded once more than the sum that was added, and the total once
+    close(flat[1:1 + dim], total, E * d(dw).abs() + E * total.abs(), "accumulated")
+
+
 def test_rows_of_zeros_and_of_values_that_are_not_finite():
     dim = 128
     x = draw(1, 5, dim)

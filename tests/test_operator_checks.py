@@ -48,7 +48,8 @@ for bad in (dict(x=None), dict(weight=None), dict(y=None), dict(x_stride=63), di
             dict(eps=float("nan")), dict(eps=float("inf")), dict(residual=P), dict(sum=P, sum_stride=63)):
     assert call("gd_norm_forward", n, io(gd._NormIO, **but(ok, **bad)))[0] == 1, bad
 ok = dict(rows=5, dy=P, x=P, weight=P, dx=P, dweight=P, dy_stride=64, x_stride=64, dx_stride=64, eps=1e-6)
-assert call("gd_norm_backward", n, io(gd._NormGrad, **ok)) == (0, 2)
+assert call("gd_norm_backward", n, io(gd._NormGrad, **ok)) == (0, 1)  # few rows: one block
+assert call("gd_norm_backward", n, io(gd._NormGrad, **but(ok, rows=2**20))) == (0, 2)
 assert call("gd_norm_backward", n, io(gd._NormGrad, **but(ok, dweight=None))) == (0, 1)
 assert call("gd_norm_backward", n, io(gd._NormGrad, **but(ok, rows=0, dy=None))) == (0, 1)  # zeros
 assert call("gd_norm_backward", n, io(gd._NormGrad, **but(ok, rows=0, accumulate=1))) == (0, 0)
@@ -117,7 +118,7 @@ for ty in (0, 1, 2):
             b = dict(rows=rows, dy=P, x=P, weight=P, pre=P, dz=P, dx=P, dweight=P, dbias=P, dy_stride=n, x_stride=k,
                      weight_stride=k, pre_stride=n, dz_stride=n, dx_stride=k, dweight_stride=k)
             st, launches = call("gd_linear_backward", l, io(gd._LinearGrad, **b))
-            assert st == 0 and 3 <= launches <= 10, (ty, k, n, rows, launches)
+            assert st == 0 and 2 <= launches <= 10, (ty, k, n, rows, launches)
         G.gd_linear_destroy(l)
 l = made("linear", 64, 48, 1, 1, 100)
 f = dict(rows=20, x=P, weight=P, y=P, x_stride=64, weight_stride=64, y_stride=48)
