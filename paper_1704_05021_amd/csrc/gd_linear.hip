@@ -14,17 +14,24 @@ constexpr uint32_t kLinearMaxDim = 1u << 22, kLinearMaxInt8 = 1u << 17;
 constexpr uint64_t kLinearPad = 512ull << 20; // bytes of padded copies, at most
 constexpr uint32_t kBiasParts = 256;          // partial sums of the bias's gradient
 
-__device__ __forceinline__ float act_slope(int act, float z) {
-    switch (act) {
-        case GD_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-        case GD_ACT_GELU:
-            return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * (expf(-0.5f * (z * z)) / 2.5066282746310002f);
-        case GD_ACT_SILU: {
-            const float s = 1.0f / (1.0f + expf(-z));
-            return s * (1.0f + z * (1.0f - s));
+// s act'(z) in place of s.  A choice of act is one branch for all of them: one
+// an element took longer than the memory.
+template <int N>
+__device__ __forceinline__ void act_slope(int act, const float (&z)[N], float (&s)[N]) {
+    if (act == GD_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] *= z[j] > 0.0f ? 1.0f : 0.0f;
+    } else if (act == GD_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            s[j] *= 0.5f * (1.0f + erff(z[j] * 0.70710678118654752f)) + z[j] * (expf(-0.5f * (z[j] * z[j])) / 2.5066282746310002f);
+    } else if (act == GD_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float q = 1.0f / (1.0f + expf(-z[j]));
+            s[j] *= q * (1.0f + z[j] * (1.0f - q));
         }
     }
-    return 1.0f;
 }
 
 // dz = dy act'(pre), rounded, and its sums over the block's rows.  A wave takes
@@ -42,8 +49,12 @@ __global__ __launch_bounds__(WAVES* kWave) void k_slope(gd_linear_grad io, uint3
         Pack<T, 8> d = load_some<8>((const T*)io.dy + row * io.dy_stride + c, n);
         if (act != GD_ACT_NONE) {
             const Pack<T, 8> z = load_some<8>((const T*)io.pre + row * io.pre_stride + c, n);
+            float at[8], v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d.v[j] = (T)((float)d.v[j] * act_slope(act, (float)z.v[j]));
+            for (int j = 0; j < 8; ++j) at[j] = (float)z.v[j], v[j] = (float)d.v[j];
+            act_slope(act, at, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d.v[j] = (T)v[j];
             store_some<8>((T*)io.dz + row * io.dz_stride + c, d, n);
         }
 #pragma unroll
@@ -233,7 +244,10 @@ gd_status gd_linear_backward(gd_linear* l, const gd_linear_grad* io, void* strea
     dw.part = l->room;
     dw.fin.out = io->dweight;
     dw.fin.out_stride = io->dweight_stride;
-    dw.fin.accumulate = io->accumulate != 0;
+    if (io->accumulate) {
+        dw.fin.residual = io->dweight;
+        dw.fin.residual_stride = io->dweight_stride;
+    }
     const gd::GemmArgs *want_dx = rows && io->dx ? &dx : nullptr,
                        *want_dw = io->dweight && (rows || !io->accumulate) ? &dw : nullptr;
     const gd::GemmRoom room{gd::kLinearRoom, l->pad, l->pad_bytes};
