@@ -105,22 +105,30 @@ struct GemmArgs {
 // Activations.  For results of 16 bits the hardware's exponential and
 // reciprocal serve, and erf by Abramowitz and Stegun's 7.1.26 (absolute error
 // below 1.5e-7): a tile's epilogue is not hidden behind products, and erff
-// and expf took 45 us of it over 8192 x 4096 results, these 15.
+// and expf took 45 us of it over 8192 x 4096 results, these 13.  The slopes
+// of that many take 46 us so, with erff and expf 65.
+
+// Phi(z), the normal distribution's, and e = exp(-z^2 / 2).
 template <bool EXACT>
-__device__ __forceinline__ float gelu(float z) {
-    if (EXACT) return z * (0.5f * (1.0f + erff(z * 0.70710678118654752f)));
+__device__ __forceinline__ float normal(float z, float& e) {
+    if (EXACT) {
+        e = expf(-0.5f * (z * z));
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    }
     const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
     float p = fmaf(1.061405429f, t, -1.453152027f);
     p = fmaf(p, t, 1.421413741f);
     p = fmaf(p, t, -0.284496736f);
     p = fmaf(p, t, 0.254829592f);
-    const float half = 0.5f * p * t * __builtin_amdgcn_exp2f(x * x * -1.44269504088896341f);  // (1 - erf x) / 2
-    return z * (z < 0.0f ? half : 1.0f - half);
+    e = __builtin_amdgcn_exp2f(x * x * -1.44269504088896341f);
+    const float half = 0.5f * p * t * e;  // (1 - erf x) / 2
+    return z < 0.0f ? half : 1.0f - half;
 }
+// 1 / (1 + exp(-z))
 template <bool EXACT>
-__device__ __forceinline__ float silu(float z) {
-    if (EXACT) return z / (1.0f + expf(-z));
-    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
+__device__ __forceinline__ float sigmoid(float z) {
+    if (EXACT) return 1.0f / (1.0f + expf(-z));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
 }
 // All of s at once, so that a choice of act is one branch: with one an element
 // ReLU took 2.3 us over 3739 x 672 results, so 0.6, and SiLU 4.1, so 0.9.
@@ -131,10 +139,13 @@ __device__ __forceinline__ void activate(int act, float (&s)[N]) {
         for (int c = 0; c < N; ++c) s[c] = s[c] < 0.0f ? 0.0f : s[c];
     } else if (act == GD_ACT_GELU) {
 #pragma unroll
-        for (int c = 0; c < N; ++c) s[c] = gelu<EXACT>(s[c]);
+        for (int c = 0; c < N; ++c) {
+            float e;
+            s[c] *= normal<EXACT>(s[c], e);
+        }
     } else if (act == GD_ACT_SILU) {
 #pragma unroll
-        for (int c = 0; c < N; ++c) s[c] = silu<EXACT>(s[c]);
+        for (int c = 0; c < N; ++c) s[c] = EXACT ? s[c] / (1.0f + expf(-s[c])) : s[c] * sigmoid<false>(s[c]);
     }
 }
 

@@ -16,19 +16,22 @@ constexpr uint32_t kBiasParts = 256;          // partial sums of the bias's grad
 
 // s act'(z) in place of s.  A choice of act is one branch for all of them: one
 // an element took longer than the memory.
-template <int N>
+template <bool EXACT, int N>
 __device__ __forceinline__ void act_slope(int act, const float (&z)[N], float (&s)[N]) {
     if (act == GD_ACT_RELU) {
 #pragma unroll
         for (int j = 0; j < N; ++j) s[j] *= z[j] > 0.0f ? 1.0f : 0.0f;
     } else if (act == GD_ACT_GELU) {
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            s[j] *= 0.5f * (1.0f + erff(z[j] * 0.70710678118654752f)) + z[j] * (expf(-0.5f * (z[j] * z[j])) / 2.5066282746310002f);
+        for (int j = 0; j < N; ++j) {
+            float e;
+            const float cdf = normal<EXACT>(z[j], e);
+            s[j] *= cdf + z[j] * (e * 0.39894228040143268f);
+        }
     } else if (act == GD_ACT_SILU) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const float q = 1.0f / (1.0f + expf(-z[j]));
+            const float q = sigmoid<EXACT>(z[j]);
             s[j] *= q * (1.0f + z[j] * (1.0f - q));
         }
     }
@@ -52,7 +55,7 @@ __global__ __launch_bounds__(WAVES* kWave) void k_slope(gd_linear_grad io, uint3
             float at[8], v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) at[j] = (float)z.v[j], v[j] = (float)d.v[j];
-            act_slope(act, at, v);
+            act_slope<sizeof(T) == 4>(act, at, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) d.v[j] = (T)v[j];
             store_some<8>((T*)io.dz + row * io.dz_stride + c, d, n);

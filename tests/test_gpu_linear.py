@@ -153,6 +153,18 @@ def test_gradients_that_are_not_finite_stay_in_their_rows(kind, rows, k, n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_slopes_over_the_whole_range(kind, act):
+    """Each slope from far below zero to far above, the steep part closely."""
+    t, n = TYPES[kind], 1000
+    pre = torch.cat([torch.linspace(-60, 60, 2 * n), torch.linspace(-6, 6, 3 * n), torch.tensor([0.0, -0.0] * (n // 2)),
+                     torch.linspace(-3e4, 3e4, n), 10.0 ** torch.linspace(-30, 0, n)]).view(-1, n).to(t).cuda()
+    x, w, dy = draw(1, pre.shape[0], 8, dtype=t), draw(2, n, 8, dtype=t), draw(3, *pre.shape, dtype=t)
+    op = gd.Linear(8, n, t, act, max_rows=pre.shape[0])
+    check_backward(op, dy, x, w, pre, op.backward(dy, x, w, pre, dbias=True), f"{kind} {act}")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("rows,k,n", [(1, 784, 512), (5, 100, 7), (40, 1000, 300), (200, 4096, 130)])
 def test_int8_with_everything_in_the_epilogue(kind, rows, k, n):
     t = TYPES[kind]
