@@ -222,8 +222,8 @@ __device__ __forceinline__ u4 shift_down(u4 v, uint32_t bytes) {
 // block's THREADS threads sharing them.  Where a row or k ends inside a
 // vector, the vector that ends there is read, and moved into place on its way
 // to LDS: no load waits for another (element by element, each behind its own
-// condition, 20 x 650 x 650 took 33 us backward, so 13).  Rows shorter than a vector
-// (few) are read by elements.
+// condition, 20 x 650 x 650 took 33 us backward, so 13).  Rows shorter than a
+// vector (few) are read by elements.
 template <typename E, bool ACROSS, int R, int THREADS>
 struct TileLoad;
 
