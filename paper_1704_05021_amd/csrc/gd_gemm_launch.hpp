@@ -6,7 +6,12 @@
 namespace gd {
 
 constexpr uint64_t kUnits = 256;  // compute units
-constexpr double kPadWork = 2e8;  // products from which padded copies pay
+
+// Multiplications from which padded copies of ragged operands pay: the copies cost two launches, the form without them
+// passes operands through registers and transposes there those across k.  Forward 2001 x 2001 x 2001 takes 33 us without
+// and 45 with them, 3001 x 3001 x 1501 70 and 57; the input's gradient of those 40 and 44, 68 and 46; the weight's
+// gradient of 1000 x 1001 x 1001 18 and 17, of 8000 x 301 x 999 39 and 33.
+constexpr double pad_work(int form) { return form == kAlong ? 1e10 : form == kPAcross ? 7e9 : 1e9; }
 
 // Whether rows of an operand start at 16-byte boundaries and are whole 16-byte chunks long.
 template <typename E>
@@ -130,7 +135,7 @@ hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
         const bool p_whole = whole_chunks<E>(a.p, a.p_stride, p_cols), q_whole = whole_chunks<E>(a.q, a.q_stride, q_cols);
         direct = p_whole && q_whole;
         GemmRoom room = given;
-        if (!direct && room.pad && a.K && (double)a.I * a.J * a.K >= kPadWork) {
+        if (!direct && room.pad && a.K && (double)a.I * a.J * a.K >= pad_work(FORM)) {
             GemmArgs b = a;
             direct = (p_whole || pad<E>(b.p, b.p_stride, p_rows, p_cols, room, st)) &&
                      (q_whole || pad<E>(b.q, b.q_stride, q_rows, q_cols, room, st));
@@ -155,7 +160,7 @@ template <typename T>
 bool pair_backward(GemmArgs dx, GemmArgs dw, const GemmRoom& room, hipStream_t st, hipError_t& e) {
     const bool direct = sizeof(T) == 2 && whole_chunks<T>(dx.p, dx.p_stride, dx.I) &&
                         whole_chunks<T>(dx.q, dx.q_stride, dx.K) && whole_chunks<T>(dw.p, dw.p_stride, dw.I);
-    if (!direct && room.pad && (double)dx.I * dx.J * dx.K >= kPadWork) return false;
+    if (!direct && room.pad && (double)dx.I * dx.J * dx.K >= pad_work(kBothAcross)) return false;
     const Choice a = choose<T, kPAcross>(dx, direct, room.floats), b = choose<T, kBothAcross>(dw, direct, room.floats);
     if (a.tile || b.tile || a.splits > 1 || b.splits > 1) return false;
     uint64_t blocks = 0, first = 0;

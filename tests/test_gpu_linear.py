@@ -152,6 +152,20 @@ def test_gradients_that_are_not_finite_stay_in_their_rows(kind, rows, k, n):
     assert torch.equal(gw[:-1], dw[:-1]) and bool(gw[-1].isnan().all())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_large_ragged_products_are_exact(kind):
+    """Sizes at which operands off any alignment are copied into padded rows first, forward too."""
+    t, f, (rows, k, n) = TYPES[kind], lambda a: a.double(), (2101, 2203, 2201)  # noqa: E731
+    x, w, dy = whole(1, rows, k, dtype=t), whole(2, n, k, dtype=t), whole(3, rows, n, dtype=t)
+    op = gd.Linear(k, n, t, max_rows=rows)
+    dx, dw, db, _ = op.backward(dy, x, w, dbias=True)
+    assert torch.equal(op.forward(x, w), (f(x) @ f(w).t()).to(t)) and torch.equal(dx, (f(dy) @ f(w)).to(t))
+    assert torch.equal(dw, (f(dy).t() @ f(x)).float()) and torch.equal(db, f(dy).sum(0).float())
+    q, wq = whole(4, rows, k, dtype=torch.int8), whole(5, n, k, dtype=torch.int8)
+    y = op.forward_int8(q, torch.ones(rows, device="cuda"), wq, torch.ones(n, device="cuda"))
+    assert torch.equal(y, (f(q) @ f(wq).t()).to(t))
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
 def test_slopes_over_the_whole_range(kind, act):
