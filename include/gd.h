@@ -340,8 +340,8 @@ typedef struct {
     const void* weight;       /* [dim] */
     void* sum;                /* [rows][dim] receives h, or NULL; may be x or residual */
     void* y;                  /* [rows][dim] in the type, or int8 when y_scale is given; in the type it may be x */
-    float* y_scale;           /* [rows], or NULL: y[i][j] * y_scale[i] is then the value, y_scale[i] =
-                                 max_j |value| / 127, y rounded to nearest even.  A row of zeros has scale
+    float* y_scale;           /* [rows], or NULL: y[i][j] * y_scale[i] is then the value, rounded as by
+                                 gd_quantise_rows from the value in binary32.  A row of zeros has scale
                                  0; one with an infinity or NaN has a scale that is not finite. */
     uint64_t x_stride, residual_stride, sum_stride, y_stride; /* at least dim */
     float eps;                /* 0 or more */
@@ -484,10 +484,13 @@ typedef struct {
 gd_status gd_linear_backward(gd_linear* layer, const gd_linear_grad* io, void* stream);
 
 /*
- * Rows in 8 bits, as the 8-bit products take them: scale[i] = max_j |x[i][j]|
- * / 127 and q = x / scale rounded to nearest even (a row of zeros has scale 0,
- * one with an infinity or NaN a scale that is not finite; a row below 2^-119
- * is stored as zeros).  columns at least 1; x_stride, q_stride >= columns.
+ * Rows in 8 bits, as the 8-bit products take them: with max = max_j |x[i][j]|,
+ * scale[i] = max / 127 and q = x * (127 * (1 / max)) rounded to the nearest
+ * whole number (ties to even), every operation rounded to binary32.  So q is
+ * x / scale rounded to nearest, but that a value within 2^-15 of the middle
+ * of two codes may take either.  A row of zeros has scale 0, one with an
+ * infinity or NaN a scale that is not finite; a row below 2^-119 is stored as
+ * zeros.  columns at least 1; x_stride, q_stride >= columns.
  */
 gd_status gd_quantise_rows(const void* x, gd_dtype type, uint64_t rows, uint64_t columns, uint64_t x_stride, int8_t* q,
                            uint64_t q_stride, float* scale, void* stream);

@@ -112,14 +112,18 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {
 
 // Scale and step of a row stored in 8 bits, from its largest magnitude's bit
 // pattern (the order of the patterns puts infinities and NaN last, so the
-// scale of a row that holds one is not finite).  Rows below 2^-119, whose
-// step would overflow, are stored as zeros.
+// scale of a row that holds one is not finite).  The step is 127 times the
+// rounded reciprocal, one rounding each: what 127.0 / max is in torch, so
+// codes equal those of the elementary operations bit for bit.  (127 / max
+// rounded once puts 1.4e-4 of a bfloat16 row's codes, halves of the largest
+// magnitude most of them, on the other side of the middle.)  Rows below
+// 2^-119, whose step would overflow, are stored as zeros.
 struct RowScale {
     float scale, step;
 };
 __device__ __forceinline__ RowScale row_scale(uint32_t max_bits) {
     const float big = __uint_as_float(max_bits);
-    return {big / 127.0f, big >= 0x1p-119f ? 127.0f / big : 0.0f};
+    return {big / 127.0f, big >= 0x1p-119f ? 127.0f * (1.0f / big) : 0.0f};
 }
 __device__ __forceinline__ int8_t quantise(float y, float step) {
     return (int8_t)fminf(fmaxf(rintf(y * step), -127.0f), 127.0f);  // a NaN gives -127, under a NaN scale
