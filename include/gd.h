@@ -473,6 +473,7 @@ typedef struct {
     const void* pre;          /* [rows][out] pre of the forward call; not read for GD_ACT_NONE */
     void* dz;                 /* [rows][out] receives dy act'(pre), rounded to the type, the gradient at the
                                  activation's input that the products below are taken with; may be dy or pre.
+                                 Under GD_ACT_RELU it is 0 where pre is not above 0, whatever dy is there.
                                  Not written for GD_ACT_NONE, where it is dy. */
     void* dx;                 /* [rows][in] receives dz weight, or NULL */
     float* dweight;           /* [out][in] in binary32, rows at dweight_stride: dz^T x, or NULL */

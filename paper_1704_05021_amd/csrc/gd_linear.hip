@@ -15,12 +15,13 @@ constexpr uint64_t kLinearPad = 512ull << 20; // bytes of padded copies, at most
 constexpr uint32_t kBiasParts = 256;          // partial sums of the bias's gradient
 
 // s act'(z) in place of s.  A choice of act is one branch for all of them: one
-// an element took longer than the memory.
+// an element took longer than the memory.  ReLU chooses and does not multiply:
+// a unit that is off passes nothing, a gradient that is not finite neither.
 template <bool EXACT, int N>
 __device__ __forceinline__ void act_slope(int act, const float (&z)[N], float (&s)[N]) {
     if (act == GD_ACT_RELU) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) s[j] *= z[j] > 0.0f ? 1.0f : 0.0f;
+        for (int j = 0; j < N; ++j) s[j] = z[j] > 0.0f ? s[j] : 0.0f;
     } else if (act == GD_ACT_GELU) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
