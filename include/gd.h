@@ -373,7 +373,8 @@ gd_status gd_norm_backward(gd_norm* norm, const gd_norm_grad* io, void* stream);
  *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * s is grad_scale, or with max_norm > 0 grad_scale * min(1, max_norm / norm),
  * norm the 2-norm of grad_scale * g over all tensors (summed in 64 bits); a
- * norm that is not finite skips the step: nothing but *norm is written.
+ * norm that is not finite in binary32, as *norm receives it, skips the step:
+ * nothing but *norm is written.
  *
  * The moments are the caller's, in 32 bits (m and v, N floats each) or in 8
  * (N bytes each and a unit per block).  A block is 256 consecutive elements

@@ -224,7 +224,8 @@ __global__ __launch_bounds__(kBlock) void k_square_sum(const G* grad, uint64_t n
 }
 
 // scale[0] = the gradient's scale under the norm's bound, scale[1] = 1 when
-// the norm is not finite.  (Its own launch, 4 us: the last block of the sums
+// the norm is not finite: the one in 32 bits, which is what the caller gets to
+// see, so finite gradients whose norm is past that range skip the step too.  (Its own launch, 4 us: the last block of the sums
 // would have to wait for every other's write to reach memory, which with a
 // release by each of 1,024 blocks took 40 us.)
 __global__ __launch_bounds__(kBlock) void k_clip(const double* part, uint32_t parts, double grad_scale, double max_norm,
@@ -235,9 +236,10 @@ __global__ __launch_bounds__(kBlock) void k_clip(const double* part, uint32_t pa
     s = row_sum<kWavesPerBlock>(s, lds);
     if (threadIdx.x != 0) return;
     const double x = fabs(grad_scale) * sqrt(s);
+    const float seen = (float)x;
     scale[0] = (float)(x > max_norm ? grad_scale * (max_norm / x) : grad_scale);
-    scale[1] = x <= 1.7976931348623157e308 ? 0.0f : 1.0f;
-    if (norm) *norm = (float)x;
+    scale[1] = seen <= 3.4028234663852886e38f ? 0.0f : 1.0f;
+    if (norm) *norm = seen;
 }
 
 __device__ __forceinline__ void decode4(uint32_t mc, uint32_t vc, float mu, float vu, Pack<float, 4>& m, Pack<float, 4>& v) {
