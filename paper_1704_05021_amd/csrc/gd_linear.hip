@@ -172,7 +172,8 @@ void gd_linear_destroy(gd_linear* l) {
 }
 
 gd_status gd_linear_forward(gd_linear* l, const gd_linear_io* io, void* stream) {
-    if (!l || !io || io->rows > l->max_rows || (io->x_scale == nullptr) != (io->weight_scale == nullptr))
+    // no rows have no scales, and an empty buffer may have no address
+    if (!l || !io || io->rows > l->max_rows || (io->rows && (io->x_scale == nullptr) != (io->weight_scale == nullptr)))
         return GD_ERR_ARG;
     const auto bad = [](uint64_t stride, uint64_t least) { return stride < least || stride > gd::kLinearMaxDim; };
     if (bad(io->weight_stride, l->in) || (io->rows && (bad(io->x_stride, l->in) || bad(io->y_stride, l->out))) ||
