@@ -391,7 +391,7 @@ typedef struct gd_adamw gd_adamw;
 typedef enum { GD_STATE_F32 = 0, GD_STATE_8BIT = 1 } gd_state;
 
 /* offsets (host, num_tensors + 1 entries): as gd_create, but up to 2^40
- * elements.  decay (host, num_tensors finite floats of 0 or more, or NULL for
+ * elements and 2^32 blocks (GD_ERR_LAYOUT past either).  decay (host, num_tensors finite floats of 0 or more, or NULL for
  * all 1).  Allocates about 16 bytes per 2,048 elements (4,096 in 8 bits) and 20
  * per tensor on the current device. */
 gd_status gd_adamw_create(gd_adamw** out, const uint64_t* tensor_offsets, uint32_t num_tensors, gd_state state,

@@ -33,7 +33,7 @@ constexpr uint32_t kAdamRun = 1024;      // elements that a block of threads tak
 constexpr int kRuns = 2, kRunsCodes = 4; // runs of a chunk, with 32- and 8-bit moments
 constexpr uint32_t kAdamMaxBlocks = 1u << 22;  // a dispatch holds less than 2^32 threads
 constexpr uint32_t kNormBlocks = 1024;   // partial sums of the gradient's squares
-constexpr uint64_t kAdamMaxElements = 1ull << 40;
+constexpr uint64_t kAdamMaxElements = 1ull << 40, kAdamBlockNumbers = 1ull << 32;
 
 constexpr int kLenShift = 52;            // 12 bits of a chunk's length above its first element
 
@@ -339,23 +339,28 @@ gd_status gd_adamw_create(gd_adamw** out, const uint64_t* off, uint32_t T, gd_st
     if (decay)
         for (uint32_t t = 0; t < T; ++t)
             if (!(decay[t] >= 0.0f) || std::isinf(decay[t])) return GD_ERR_ARG;
+    // counted before the table is made: one too long to be held is refused at once
+    const uint64_t chunk = gd::kAdamRun * (uint64_t)(kind == GD_STATE_8BIT ? gd::kRunsCodes : gd::kRuns);
+    uint64_t num_chunks = 0, blocks = 0;
+    for (uint32_t t = 0; t < T; ++t) {
+        const uint64_t len = off[t + 1] - off[t];
+        num_chunks += (len + chunk - 1) / chunk;
+        blocks += (len + gd::kStateBlock - 1) / gd::kStateBlock;
+    }
+    if (num_chunks > 0xFFFFFFFFull - gd::kAdamMaxBlocks || blocks > gd::kAdamBlockNumbers) return GD_ERR_LAYOUT;
     gd_adamw* o = nullptr;
     try {
         o = new gd_adamw();
         o->N = off[T];
         o->codes = kind == GD_STATE_8BIT;
         std::vector<gd::AdamChunk> chunks;
-        const uint64_t chunk = gd::kAdamRun * (uint64_t)(o->codes ? gd::kRunsCodes : gd::kRuns);
+        chunks.reserve(num_chunks);
         for (uint32_t t = 0; t < T; ++t)
             for (uint64_t a = off[t]; a < off[t + 1]; a += chunk) {
                 const uint64_t len = std::min<uint64_t>(chunk, off[t + 1] - a);
                 chunks.push_back({a | (len - 1) << gd::kLenShift, t, (uint32_t)o->blocks});
                 o->blocks += (len + gd::kStateBlock - 1) / gd::kStateBlock;
             }
-        if (chunks.size() > 0xFFFFFFFFull - gd::kAdamMaxBlocks || o->blocks > 0xFFFFFFFFull) {
-            delete o;
-            return GD_ERR_LAYOUT;
-        }
         o->num_chunks = (uint32_t)chunks.size();
         std::vector<float> d(T, 1.0f);
         if (decay) d.assign(decay, decay + T);
