@@ -463,7 +463,9 @@ typedef struct {
 
 /* GD_ERR_ARG for a NULL pointer, rows above max_rows, a bad stride, one scale
  * without the other; GD_ERR_LAYOUT when in is above 131,072 with scales (the
- * exact sums are held in 32 bits). */
+ * exact sums are held in 32 bits), or when the results make 2^24 or more tiles
+ * of 128 x 128 (rows and out each counted up to whole tiles: 2^38 results; of
+ * narrow layers 2^31 - 127 rows). */
 gd_status gd_linear_forward(gd_linear* layer, const gd_linear_io* io, void* stream);
 
 typedef struct {
@@ -483,6 +485,7 @@ typedef struct {
     int accumulate;           /* not 0: dweight and dbias += instead of = */
 } gd_linear_grad;
 
+/* Errors as the forward call's, the tiles of dx and of dweight counted. */
 gd_status gd_linear_backward(gd_linear* layer, const gd_linear_grad* io, void* stream);
 
 /*

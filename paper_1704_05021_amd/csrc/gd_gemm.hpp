@@ -933,7 +933,14 @@ struct GemmRoom {
     uint64_t pad_bytes;
 };
 
-// One product.  Operand types: E is O's type, or int8 with kAlong.
+// Whether a product of I x J results is one that can be launched: a dispatch
+// holds less than 2^32 threads, and the middle tile serves every form.
+constexpr uint32_t kProductTile = 128, kProductThreads = 256;
+inline bool product_fits(uint64_t I, uint64_t J) {
+    return ((I + kProductTile - 1) / kProductTile) * ((J + kProductTile - 1) / kProductTile) * kProductThreads <= 0xFFFFFFFFull;
+}
+
+// One product that fits.  Operand types: E is O's type, or int8 with kAlong.
 template <typename E, typename O, int FORM>
 hipError_t launch_gemm(GemmArgs a, const GemmRoom& room, hipStream_t st);
 

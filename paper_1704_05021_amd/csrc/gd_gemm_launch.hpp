@@ -40,11 +40,16 @@ bool pad(const void*& p, uint64_t& stride, uint64_t rows, uint32_t columns, Gemm
 // each of several there at once (as many as LDS holds).  Every round of tiles
 // also takes about kRoundUs to fill the pipeline and write results.
 struct TileCost {
-    uint32_t bi, bj, at_once;
+    uint32_t bi, bj, threads, at_once;
     double alone_us, shared_us;
+    uint64_t tiles(uint64_t I, uint64_t J) const { return ((I + bi - 1) / bi) * ((J + bj - 1) / bj); }
+    bool fits(uint64_t I, uint64_t J) const { return tiles(I, J) * threads <= 0xFFFFFFFFull; }  // threads of a dispatch
 };
-constexpr TileCost kBigCost{256, 256, 1, 1.48, 1.48}, kLongCost{256, 192, 1, 1.10, 1.10}, kWideCost{256, 128, 1, 0.82, 0.82},
-    kMidCost{128, 128, 2, 0.58, 0.475}, kSmallCost{64, 64, 2, 0.17, 0.165};
+constexpr TileCost kBigCost{256, 256, TileBig::kThreads, 1, 1.48, 1.48}, kLongCost{256, 192, TileLong::kThreads, 1, 1.10, 1.10},
+    kWideCost{256, 128, TileWide::kThreads, 1, 0.82, 0.82}, kMidCost{128, 128, TileMid::kThreads, 2, 0.58, 0.475},
+    kSmallCost{64, 64, TileSmall::kThreads, 2, 0.17, 0.165};
+static_assert(TileMid::BI == kProductTile && TileMid::BJ == kProductTile && TileMid::kThreads == kProductThreads,
+              "the tile that every product which product_fits can take");
 constexpr double kRoundUs = 5.0, kJoinUs = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct TilePlan {
@@ -55,7 +60,7 @@ struct TilePlan {
 // The number of shares of k that a product of `steps` steps does best with, and its time: shares fill compute units
 // that the tiles leave idle, and cost the writing and reading of their sums.
 inline TilePlan plan_tiles(const TileCost& c, uint64_t I, uint64_t J, uint64_t steps, uint64_t room) {
-    const uint64_t tiles = ((I + c.bi - 1) / c.bi) * ((J + c.bj - 1) / c.bj);
+    const uint64_t tiles = c.tiles(I, J);
     const auto time = [&](uint64_t splits) {
         const uint64_t each = (steps + splits - 1) / splits, load = (tiles * splits + kUnits - 1) / kUnits;
         const auto round = [&](uint64_t n) {
@@ -78,7 +83,6 @@ hipError_t launch_tiles(GemmArgs a, uint64_t splits, bool direct, hipStream_t st
     a.tiles_i = (a.I + TL::BI - 1) / TL::BI;
     a.tiles_j = (a.J + TL::BJ - 1) / TL::BJ;
     const uint64_t tiles = (uint64_t)a.tiles_i * a.tiles_j, steps = ((uint64_t)a.K + KE - 1) / KE;
-    if (tiles * TL::kThreads > 0xFFFFFFFFull) return hipErrorInvalidValue;
     a.steps = (uint32_t)((steps + splits - 1) / splits);
     if (a.steps) splits = (steps + a.steps - 1) / a.steps;
     float* part = a.part;
@@ -113,6 +117,7 @@ Choice choose(const GemmArgs& a, bool direct, uint64_t room) {
     constexpr TileCost kCosts[] = {kSmallCost, kMidCost, kWideCost, kLongCost, kBigCost};
     for (int t = 0; t < (direct ? 5 : 2); ++t) {  // the larger tiles take operands placed in LDS only
         if (FORM == kBothAcross && t == 3) continue;  // rows of 192 across k would not be a power of two in LDS
+        if (!kCosts[t].fits(a.I, a.J)) continue;
         const TilePlan p = plan_tiles(kCosts[t], a.I, a.J, steps, room);
         if (p.us < best.us) best = p, tile = t;
     }

@@ -180,7 +180,7 @@ gd_status gd_linear_forward(gd_linear* l, const gd_linear_io* io, void* stream) 
         (io->residual && bad(io->residual_stride, l->out)) || (io->pre && bad(io->pre_stride, l->out)))
         return GD_ERR_ARG;
     const bool int8 = io->x_scale != nullptr;
-    if (int8 && l->in > gd::kLinearMaxInt8) return GD_ERR_LAYOUT;
+    if ((int8 && l->in > gd::kLinearMaxInt8) || !gd::product_fits(l->out, io->rows)) return GD_ERR_LAYOUT;
     if (io->rows == 0) return GD_OK;
     if (!io->x || !io->weight || !io->y) return GD_ERR_ARG;
     gd::DeviceGuard guard(l->device);
@@ -221,6 +221,8 @@ gd_status gd_linear_backward(gd_linear* l, const gd_linear_grad* io, void* strea
         (rows && io->dx && (!io->weight || bad(io->weight_stride, l->in) || bad(io->dx_stride, l->in))) ||
         (io->dweight && (bad(io->dweight_stride, l->in) || (rows && (!io->x || bad(io->x_stride, l->in))))))
         return GD_ERR_ARG;
+    if ((io->dx && !gd::product_fits(l->in, io->rows)) || (io->dweight && !gd::product_fits(l->in, l->out)))
+        return GD_ERR_LAYOUT;
     gd::DeviceGuard guard(l->device);
     if (!guard.ok) return GD_ERR_HIP;
     const hipStream_t st = (hipStream_t)stream;
