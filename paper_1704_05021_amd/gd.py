@@ -523,6 +523,17 @@ def _rows_on(device: int, t: torch.Tensor, name: str, dtype: torch.dtype, column
     return n, t.data_ptr(), down if n > 1 else columns
 
 
+def _new(stream: Optional[torch.cuda.Stream], make, *args, **kwargs) -> torch.Tensor:
+    """A tensor that a call on ``stream`` writes: memory of that stream, which no work queued on another one still uses,
+    and which is not used again before the work that the current stream has by then is done."""
+    if stream is None:
+        return make(*args, **kwargs)
+    with torch.cuda.stream(stream):
+        t = make(*args, **kwargs)
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def _stream_on(device: int, stream: Optional[torch.cuda.Stream], *tensors) -> Optional[int]:
     """The stream's handle.  Tensors used on a stream that is not the current one are kept from reuse until its work so
     far is done; that the work before them is done is the caller's to see to."""
@@ -591,15 +602,15 @@ class RMSNorm(_Handle):
 
     def forward(self, x, weight, residual=None, out=None, sum_out=None, stream=None):
         """(y, h); h is x itself without a residual.  ``sum_out`` may be x or residual, ``out`` may be x."""
-        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
+        y = _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format) if out is None else out
         h = self._run(x, weight, residual, y, None, sum_out, stream)
         return y, h
 
     def forward_int8(self, x, weight, residual=None, out=None, scale=None, sum_out=None, stream=None):
         """(q, scale, h): rows of y in 8 bits, y = q * scale[row], scale[row] = max|y| / 127."""
-        q = x.new_empty(x.shape, dtype=torch.int8) if out is None else out
+        q = _new(stream, x.new_empty, x.shape, dtype=torch.int8) if out is None else out
         if scale is None:
-            scale = x.new_empty(x.shape[:-1], dtype=torch.float32)
+            scale = _new(stream, x.new_empty, x.shape[:-1], dtype=torch.float32)
         h = self._run(x, weight, residual, q, scale, sum_out, stream)
         return q, scale, h
 
@@ -614,7 +625,7 @@ class RMSNorm(_Handle):
         h = x
         if residual is not None:
             _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.dim, rows)
-            h = torch.empty_like(x, memory_format=torch.contiguous_format) if sum_out is None else sum_out
+            h = _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format) if sum_out is None else sum_out
         elif sum_out is not None:
             h = sum_out
         if h is not x or sum_out is not None:
@@ -635,9 +646,9 @@ class RMSNorm(_Handle):
         if dsum is not None:
             _, io.dsum, io.dsum_stride = self._matrix(dsum, "dsum", self.dtype, self.dim, rows)
         if dx is None:
-            dx = torch.empty_like(dy, memory_format=torch.contiguous_format)
+            dx = _new(stream, torch.empty_like, dy, memory_format=torch.contiguous_format)
         _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.dim, rows)
-        dweight = _gradient(dweight, accumulate, (self.dim,), self.device)
+        dweight = _gradient(dweight, accumulate, (self.dim,), self.device, stream)
         io.dweight = self._tensor(dweight, "dweight", torch.float32, self.dim)
         st = _lib().gd_norm_backward(self._h, io, self._stream(stream, dy, h, weight, dsum, dx, dweight))
         if st != 0:
@@ -645,12 +656,12 @@ class RMSNorm(_Handle):
         return dx, dweight
 
 
-def _gradient(given, accumulate, shape, device):
+def _gradient(given, accumulate, shape, device, stream):
     if given is not None:
         return given
     if accumulate:
         raise ValueError("accumulate needs the gradient to add to")
-    return torch.empty(shape, dtype=torch.float32, device=device)
+    return _new(stream, torch.empty, shape, dtype=torch.float32, device=device)
 
 
 class Linear(_Handle):
@@ -696,11 +707,11 @@ class Linear(_Handle):
             _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.outf, rows)
         shape = (*x.shape[:-1], self.outf)
         if out is None:
-            out = x.new_empty(shape, dtype=self.dtype)
+            out = _new(stream, x.new_empty, shape, dtype=self.dtype)
         _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.outf, rows)
         pre = None
         if keep_pre is not False:
-            pre = x.new_empty(shape, dtype=self.dtype) if keep_pre is True else keep_pre
+            pre = _new(stream, x.new_empty, shape, dtype=self.dtype) if keep_pre is True else keep_pre
             _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, self.outf, rows)
         st = _lib().gd_linear_forward(self._h, io, self._stream(stream, x, weight, xs, ws, bias, residual, out, pre))
         if st != 0:
@@ -723,25 +734,25 @@ class Linear(_Handle):
                 raise ValueError(f"the backward of {self.act} needs pre")
             _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, self.outf, rows)
             if dz is None:
-                dz = torch.empty_like(dy, memory_format=torch.contiguous_format)
+                dz = _new(stream, torch.empty_like, dy, memory_format=torch.contiguous_format)
             _, io.dz, io.dz_stride = self._matrix(dz, "dz", self.dtype, self.outf, rows)
         else:
             pre, dz = None, dy
         if need_dx:
             _, io.weight, io.weight_stride = self._matrix(weight, "weight", self.dtype, self.inf, self.outf)
             if dx is None:
-                dx = dy.new_empty((*dy.shape[:-1], self.inf))
+                dx = _new(stream, dy.new_empty, (*dy.shape[:-1], self.inf))
             _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.inf, rows)
         else:
             dx = None
         if need_dweight:
             _, io.x, io.x_stride = self._matrix(x, "x", self.dtype, self.inf, rows)
-            dweight = _gradient(dweight, accumulate, (self.outf, self.inf), self.device)
+            dweight = _gradient(dweight, accumulate, (self.outf, self.inf), self.device, stream)
             _, io.dweight, io.dweight_stride = self._matrix(dweight, "dweight", torch.float32, self.inf, self.outf)
         else:
             dweight = None
         if dbias is not None:
-            dbias = _gradient(None if dbias is True else dbias, accumulate, (self.outf,), self.device)
+            dbias = _gradient(None if dbias is True else dbias, accumulate, (self.outf,), self.device, stream)
             io.dbias = self._tensor(dbias, "dbias", torch.float32, self.outf)
         st = _lib().gd_linear_backward(self._h, io, self._stream(stream, dy, x, weight, pre, dz, dx, dweight, dbias))
         if st != 0:
@@ -755,8 +766,8 @@ def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.
     if index < 0 or x.dim() == 0 or x.size(-1) == 0:
         raise ValueError("x must be a GPU tensor of rows of at least one element")
     columns = x.size(-1)
-    q = x.new_empty(x.shape, dtype=torch.int8) if out is None else out
-    scale = x.new_empty(x.shape[:-1], dtype=torch.float32) if scale is None else scale
+    q = _new(stream, x.new_empty, x.shape, dtype=torch.int8) if out is None else out
+    scale = _new(stream, x.new_empty, x.shape[:-1], dtype=torch.float32) if scale is None else scale
     rows, xp, xs = _rows_on(index, x, "x", x.dtype, columns)
     _, qp, qs = _rows_on(index, q, "out", torch.int8, columns, rows)
     sp = _flat_on(index, scale, "scale", torch.float32, rows)
@@ -837,7 +848,7 @@ class AdamW(_Handle):
         if max_norm is not None:
             if not max_norm > 0:
                 raise ValueError("max_norm must be above 0")
-            norm = torch.empty(1, dtype=torch.float32, device=self.device)
+            norm = _new(stream, torch.empty, 1, dtype=torch.float32, device=self.device)
             io.max_norm, io.norm = max_norm, norm.data_ptr()
         st = _lib().gd_adamw_step(self._h, io, self._stream(stream, params, grad, state.m, state.v, state.m_unit,
                                                             state.v_unit, copy, norm))
@@ -861,7 +872,7 @@ class AdamW(_Handle):
             raise ValueError("the state is in 32 bits already")
         io = _AdamWIO()
         self._state(state, io)
-        m, v = (torch.empty(self.N, dtype=torch.float32, device=self.device) for _ in range(2))
+        m, v = (_new(stream, torch.empty, self.N, dtype=torch.float32, device=self.device) for _ in range(2))
         st = _lib().gd_adamw_decode(self._h, io.m, io.v, io.m_unit, io.v_unit, m.data_ptr(), v.data_ptr(),
                                     self._stream(stream, state.m, state.v, state.m_unit, state.v_unit, m, v))
         if st != 0:
