@@ -339,7 +339,8 @@ typedef struct {
     const void* residual;     /* [rows][dim], or NULL */
     const void* weight;       /* [dim] */
     void* sum;                /* [rows][dim] receives h, or NULL; may be x or residual */
-    void* y;                  /* [rows][dim] in the type, or int8 when y_scale is given; in the type it may be x */
+    void* y;                  /* [rows][dim] in the type, or int8 when y_scale is given; in the type it may be x or
+                                 residual */
     float* y_scale;           /* [rows], or NULL: y[i][j] * y_scale[i] is then the value, rounded as by
                                  gd_quantise_rows from the value in binary32.  A row of zeros has scale
                                  0; one with an infinity or NaN has a scale that is not finite. */

@@ -7,6 +7,7 @@ no CPU fallback: if ``libgd.so`` has not been built, loading fails loudly.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -523,6 +524,30 @@ def _rows_on(device: int, t: torch.Tensor, name: str, dtype: torch.dtype, column
     return n, t.data_ptr(), down if n > 1 else columns
 
 
+def _meet(a, b, size: int) -> bool:
+    """Whether two matrices share memory: (address, rows, row stride, columns) in elements of ``size`` bytes."""
+    (pa, na, sa, ca), (pb, nb, sb, cb) = a, b
+    if not na or not nb or pa >= pb + ((nb - 1) * sb + cb) * size or pb >= pa + ((na - 1) * sa + ca) * size:
+        return False
+    if sa == ca:  # one run
+        na, ca = 1, na * ca
+    if sb == cb:
+        nb, cb = 1, nb * cb
+    if na == nb == 1 or (na > 1 and nb > 1 and sa != sb):  # rows at two distances: not told apart
+        return True
+    step = (sa if na > 1 else sb) * size
+    at = (pa - pb) % step  # where a's rows lie between those of b
+    return at < cb * size or at + ca * size > step
+
+
+def _apart(size: int, name: str, span, others: dict, same=()) -> None:
+    """Raises unless a given output lies apart from the others, matrices of its own type, or is exactly the one of
+    those named in ``same``."""
+    for other, o in others.items():
+        if _meet(span, o, size) and not (other in same and span == o):
+            raise ValueError(f"{name} overlaps {other}" + (f"; it may be the same rows as {' or '.join(same)}" if same else ""))
+
+
 def _new(stream: Optional[torch.cuda.Stream], make, *args, **kwargs) -> torch.Tensor:
     """A tensor that a call on ``stream`` writes: memory of that stream, which no work queued on another one still uses,
     and which is not used again before the work that the current stream has by then is done."""
@@ -546,7 +571,11 @@ def _stream_on(device: int, stream: Optional[torch.cuda.Stream], *tensors) -> Op
 
 
 class _Handle:
-    """A library handle on one device, freed with the object."""
+    """A library handle on one device, freed with the object.
+
+    Outputs in the layer's type that the caller gives are checked to lie apart from the call's inputs and its other
+    outputs in that type, but where a call says that they may be the same rows.
+    """
 
     _what = ""
 
@@ -555,7 +584,8 @@ class _Handle:
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         if self.device.index is None:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
-        self._index = self.device.index
+        index = self.device.index
+        self._tensor, self._matrix, self._stream = (functools.partial(f, index) for f in (_flat_on, _rows_on, _stream_on))
         self._h = None
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
@@ -575,15 +605,6 @@ class _Handle:
         except Exception:
             pass
 
-    def _tensor(self, t, name, dtype, n) -> int:
-        return _flat_on(self._index, t, name, dtype, n)
-
-    def _matrix(self, t, name, dtype, columns, rows=None):
-        return _rows_on(self._index, t, name, dtype, columns, rows)
-
-    def _stream(self, stream, *tensors) -> Optional[int]:
-        return _stream_on(self._index, stream, *tensors)
-
 
 class RMSNorm(_Handle):
     """Root-mean-square norm of rows of ``dim`` elements with the residual's addition (gd_norm_*).
@@ -601,26 +622,27 @@ class RMSNorm(_Handle):
         self._create(device, self.dim, _dtype_code(dtype))
 
     def forward(self, x, weight, residual=None, out=None, sum_out=None, stream=None):
-        """(y, h); h is x itself without a residual.  ``sum_out`` may be x or residual, ``out`` may be x."""
-        y = _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format) if out is None else out
-        h = self._run(x, weight, residual, y, None, sum_out, stream)
+        """(y, h); h is x itself without a residual.  ``sum_out`` and ``out`` may be x or residual."""
+        y, _, h = self._run(x, weight, residual, out, None, False, sum_out, stream)
         return y, h
 
     def forward_int8(self, x, weight, residual=None, out=None, scale=None, sum_out=None, stream=None):
         """(q, scale, h): rows of y in 8 bits, y = q * scale[row], scale[row] = max|y| / 127."""
-        q = _new(stream, x.new_empty, x.shape, dtype=torch.int8) if out is None else out
-        if scale is None:
-            scale = _new(stream, x.new_empty, x.shape[:-1], dtype=torch.float32)
-        h = self._run(x, weight, residual, q, scale, sum_out, stream)
-        return q, scale, h
+        return self._run(x, weight, residual, out, scale, True, sum_out, stream)
 
-    def _run(self, x, weight, residual, y, scale, sum_out, stream):
+    def _run(self, x, weight, residual, out, scale, int8, sum_out, stream):
         io = _NormIO(eps=self.eps)
         rows, io.x, io.x_stride = self._matrix(x, "x", self.dtype, self.dim)
         io.rows = rows
         io.weight = self._tensor(weight, "weight", self.dtype, self.dim)
-        _, io.y, io.y_stride = self._matrix(y, "out", self.dtype if scale is None else torch.int8, self.dim, rows)
-        if scale is not None:
+        y = out
+        if y is None:
+            y = (_new(stream, x.new_empty, x.shape, dtype=torch.int8) if int8
+                 else _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format))
+        _, io.y, io.y_stride = self._matrix(y, "out", torch.int8 if int8 else self.dtype, self.dim, rows)
+        if int8:
+            if scale is None:
+                scale = _new(stream, x.new_empty, x.shape[:-1], dtype=torch.float32)
             io.y_scale = self._tensor(scale, "scale", torch.float32, rows)
         h = x
         if residual is not None:
@@ -630,10 +652,25 @@ class RMSNorm(_Handle):
             h = sum_out
         if h is not x or sum_out is not None:
             _, io.sum, io.sum_stride = self._matrix(h, "sum_out", self.dtype, self.dim, rows)
+        if rows and (out is not None or sum_out is not None):
+            self._outputs_apart(io, out is not None and not int8, sum_out is not None)
         st = _lib().gd_norm_forward(self._h, io, self._stream(stream, x, weight, residual, y, scale, h))
         if st != 0:
             raise GDError(st, "gd_norm_forward")
-        return h
+        return y, scale, h
+
+    def _outputs_apart(self, io, out, sum_out) -> None:
+        """A given out or sum_out lies apart from what the call reads, and from the other."""
+        rows, dim, size = io.rows, self.dim, self.dtype.itemsize
+        others = {"x": (io.x, rows, io.x_stride, dim), "weight": (io.weight, 1, dim, dim)}
+        if io.residual:
+            others["residual"] = (io.residual, rows, io.residual_stride, dim)
+        if sum_out:
+            _apart(size, "sum_out", (io.sum, rows, io.sum_stride, dim), others, ("x", "residual"))
+        if io.sum:
+            others["sum_out"] = (io.sum, rows, io.sum_stride, dim)
+        if out:
+            _apart(size, "out", (io.y, rows, io.y_stride, dim), others, ("x", "residual"))
 
     def backward(self, dy, h, weight, dsum=None, dx=None, dweight=None, accumulate=False, stream=None):
         """(dx, dweight): the gradient of x and of residual, and the weight's in float32 (a slice of a flat
@@ -645,11 +682,19 @@ class RMSNorm(_Handle):
         io.weight = self._tensor(weight, "weight", self.dtype, self.dim)
         if dsum is not None:
             _, io.dsum, io.dsum_stride = self._matrix(dsum, "dsum", self.dtype, self.dim, rows)
-        if dx is None:
+        given = dx is not None
+        if not given:
             dx = _new(stream, torch.empty_like, dy, memory_format=torch.contiguous_format)
         _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.dim, rows)
         dweight = _gradient(dweight, accumulate, (self.dim,), self.device, stream)
         io.dweight = self._tensor(dweight, "dweight", torch.float32, self.dim)
+        if rows and given:
+            dim = self.dim
+            others = {"dy": (io.dy, rows, io.dy_stride, dim), "h": (io.x, rows, io.x_stride, dim),
+                      "weight": (io.weight, 1, dim, dim)}
+            if dsum is not None:
+                others["dsum"] = (io.dsum, rows, io.dsum_stride, dim)
+            _apart(self.dtype.itemsize, "dx", (io.dx, rows, io.dx_stride, dim), others, ("dy", "dsum"))
         st = _lib().gd_norm_backward(self._h, io, self._stream(stream, dy, h, weight, dsum, dx, dweight))
         if st != 0:
             raise GDError(st, "gd_norm_backward")
@@ -706,13 +751,27 @@ class Linear(_Handle):
         if residual is not None:
             _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.outf, rows)
         shape = (*x.shape[:-1], self.outf)
-        if out is None:
+        given = out is not None
+        if not given:
             out = _new(stream, x.new_empty, shape, dtype=self.dtype)
         _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.outf, rows)
         pre = None
         if keep_pre is not False:
             pre = _new(stream, x.new_empty, shape, dtype=self.dtype) if keep_pre is True else keep_pre
             _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, self.outf, rows)
+        if rows and (given or (pre is not None and keep_pre is not True)):
+            k, n, size, others = self.inf, self.outf, self.dtype.itemsize, {}
+            if xs is None:
+                others = {"x": (io.x, rows, io.x_stride, k), "weight": (io.weight, n, io.weight_stride, k)}
+            if bias is not None:
+                others["bias"] = (io.bias, 1, n, n)
+            if residual is not None:
+                others["residual"] = (io.residual, rows, io.residual_stride, n)
+            span = (io.y, rows, io.y_stride, n)
+            if given:
+                _apart(size, "out", span, others, ("residual",))
+            if pre is not None:
+                _apart(size, "pre", (io.pre, rows, io.pre_stride, n), {**others, "out": span})
         st = _lib().gd_linear_forward(self._h, io, self._stream(stream, x, weight, xs, ws, bias, residual, out, pre))
         if st != 0:
             raise GDError(st, "gd_linear_forward")
@@ -724,8 +783,9 @@ class Linear(_Handle):
 
         dbias: a tensor to write, True for a new one, or None for a layer without a bias.
         dz = dy act'(pre) in ``dtype`` is the gradient that the products take (dy itself without an
-        activation).  None for what is not needed; the gradient of the residual is dy.
+        activation).  None for what is not needed; the gradient of the residual is dy.  dz may be dy or pre.
         """
+        given_dz, given_dx = dz is not None, dx is not None
         io = _LinearGrad(accumulate=int(accumulate))
         rows, io.dy, io.dy_stride = self._matrix(dy, "dy", self.dtype, self.outf)
         io.rows = rows
@@ -754,10 +814,26 @@ class Linear(_Handle):
         if dbias is not None:
             dbias = _gradient(None if dbias is True else dbias, accumulate, (self.outf,), self.device, stream)
             io.dbias = self._tensor(dbias, "dbias", torch.float32, self.outf)
+        if rows and (given_dz or given_dx):
+            self._outputs_apart(io, given_dz, given_dx)
         st = _lib().gd_linear_backward(self._h, io, self._stream(stream, dy, x, weight, pre, dz, dx, dweight, dbias))
         if st != 0:
             raise GDError(st, "gd_linear_backward")
         return dx, dweight, dbias, dz
+
+    def _outputs_apart(self, io, dz, dx) -> None:
+        """A given dz or dx lies apart from what the call reads, and from the other."""
+        rows, k, n, size = io.rows, self.inf, self.outf, self.dtype.itemsize
+        others = {"dy": (io.dy, rows, io.dy_stride, n), "x": (io.x, rows, io.x_stride, k),
+                  "weight": (io.weight, n, io.weight_stride, k), "pre": (io.pre, rows, io.pre_stride, n),
+                  "dz": (io.dz, rows, io.dz_stride, n)}
+        others = {name: span for name, span in others.items() if span[0]}  # what the call was given
+        if dz and io.dz:
+            span = others.pop("dz")
+            _apart(size, "dz", span, others, ("dy", "pre"))
+            others["dz"] = span
+        if dx and io.dx:
+            _apart(size, "dx", (io.dx, rows, io.dx_stride, k), others)
 
 
 def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.cuda.Stream] = None):
