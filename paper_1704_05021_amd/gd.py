@@ -524,6 +524,13 @@ def _rows_on(device: int, t: torch.Tensor, name: str, dtype: torch.dtype, column
     return n, t.data_ptr(), down if n > 1 else columns
 
 
+def _untracked() -> RuntimeError:
+    """What a forward raises for tensors that autograd would have to follow: its results would come out cut off from
+    them, without a word."""
+    return RuntimeError("autograd does not follow the layers' calls: make them under torch.no_grad() or on detached "
+                        "tensors, and take gradients by their backward()")
+
+
 def _meet(a, b, size: int) -> bool:
     """Whether two matrices share memory: (address, rows, row stride, columns) in elements of ``size`` bytes."""
     (pa, na, sa, ca), (pb, nb, sb, cb) = a, b
@@ -574,7 +581,8 @@ class _Handle:
     """A library handle on one device, freed with the object.
 
     Outputs in the layer's type that the caller gives are checked to lie apart from the call's inputs and its other
-    outputs in that type, but where a call says that they may be the same rows.
+    outputs in that type, but where a call says that they may be the same rows.  Autograd does not follow the calls: a
+    layer's forward refuses tensors that require gradients while autograd records, and its backward gives the gradients.
     """
 
     _what = ""
@@ -654,6 +662,9 @@ class RMSNorm(_Handle):
             _, io.sum, io.sum_stride = self._matrix(h, "sum_out", self.dtype, self.dim, rows)
         if rows and (out is not None or sum_out is not None):
             self._outputs_apart(io, out is not None and not int8, sum_out is not None)
+        if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                        (residual is not None and residual.requires_grad)):
+            raise _untracked()
         st = _lib().gd_norm_forward(self._h, io, self._stream(stream, x, weight, residual, y, scale, h))
         if st != 0:
             raise GDError(st, "gd_norm_forward")
@@ -750,7 +761,7 @@ class Linear(_Handle):
             io.bias = self._tensor(bias, "bias", self.dtype, self.outf)
         if residual is not None:
             _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.outf, rows)
-        shape = (*x.shape[:-1], self.outf)
+        shape = (rows, self.outf) if x.dim() == 2 else (*x.shape[:-1], self.outf)
         given = out is not None
         if not given:
             out = _new(stream, x.new_empty, shape, dtype=self.dtype)
@@ -772,6 +783,10 @@ class Linear(_Handle):
                 _apart(size, "out", span, others, ("residual",))
             if pre is not None:
                 _apart(size, "pre", (io.pre, rows, io.pre_stride, n), {**others, "out": span})
+        if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                        (bias is not None and bias.requires_grad) or
+                                        (residual is not None and residual.requires_grad)):
+            raise _untracked()
         st = _lib().gd_linear_forward(self._h, io, self._stream(stream, x, weight, xs, ws, bias, residual, out, pre))
         if st != 0:
             raise GDError(st, "gd_linear_forward")
@@ -847,6 +862,8 @@ def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.
     rows, xp, xs = _rows_on(index, x, "x", x.dtype, columns)
     _, qp, qs = _rows_on(index, q, "out", torch.int8, columns, rows)
     sp = _flat_on(index, scale, "scale", torch.float32, rows)
+    if x.requires_grad and torch.is_grad_enabled():
+        raise _untracked()
     if torch.cuda.current_device() != index:
         with torch.cuda.device(index):
             st = _lib().gd_quantise_rows(xp, code, rows, columns, xs, qp, qs, sp, _stream_on(index, stream, x, q, scale))

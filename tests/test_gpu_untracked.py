@@ -1,0 +1,74 @@
+"""Autograd does not follow the layers: a forward of tensors that require gradients is refused while autograd records,
+so that no gradient is lost without a word, and works under no_grad and inside an autograd function."""
+import pytest
+import torch
+
+from paper_1704_05021_amd import gd
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+def draw(*shape):
+    return torch.randn(*shape, device="cuda")
+
+
+def test_forwards_refuse_what_autograd_would_follow():
+    x, w, b, r, gain = draw(4, 32), draw(48, 32), draw(48), draw(4, 48), draw(32)
+    layer, norm = gd.Linear(32, 48, torch.float32, "silu", max_rows=4), gd.RMSNorm(32, torch.float32)
+    q, s = gd.quantise_rows(x)
+    wq, ws = gd.quantise_rows(w)
+    calls = {
+        "linear": (lambda x, w, b, r: layer.forward(x, w, b, r), (x, w, b, r)),
+        "int8": (lambda b, r: layer.forward_int8(q, s, wq, ws, b, r), (b, r)),
+        "norm": (lambda x, g, r: norm.forward(x, g, r)[0], (x, gain, draw(4, 32))),
+        "norm_int8": (lambda x, g, r: norm.forward_int8(x, g, r)[0], (x, gain, draw(4, 32))),
+        "quantise": (lambda x: gd.quantise_rows(x)[0], (x,)),
+    }
+    for name, (call, args) in calls.items():
+        want = call(*args)
+        for i in range(len(args)):
+            tracked = [a.clone().requires_grad_(i == j) for j, a in enumerate(args)]
+            with pytest.raises(RuntimeError, match="autograd"):
+                call(*tracked)
+            with torch.no_grad():
+                assert torch.equal(call(*tracked), want), name
+            assert torch.equal(call(*[a.detach() for a in tracked]), want), name
+
+
+def test_inside_an_autograd_function():
+    layer = gd.Linear(32, 48, torch.float32, "gelu", max_rows=4)
+
+    class Layer(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, b):
+            y, pre = layer.forward(x, w, b, keep_pre=True)
+            ctx.save_for_backward(x, w, pre)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            return layer.backward(dy.contiguous(), *ctx.saved_tensors, dbias=True)[:3]
+
+    x, w, b, dy = (t.requires_grad_(t.shape != (4, 48)) for t in (draw(4, 32), draw(48, 32), draw(48), draw(4, 48)))
+    Layer.apply(x, w, b).backward(dy)
+    got = [t.grad for t in (x, w, b)]
+    with torch.no_grad():
+        _, pre = layer.forward(x, w, b, keep_pre=True)
+        want = layer.backward(dy, x, w, pre, dbias=True)[:3]
+    for g, v in zip(got, want):
+        assert torch.equal(g, v)
+
+
+def test_an_optimiser_step_takes_leaves():
+    p, g = draw(64).requires_grad_(), draw(64)
+    opt, q = gd.AdamW([0, 64]), p.detach().clone()
+    opt.step(p, g, opt.init_state(), 1, lr=1e-3)
+    opt.step(q, g, opt.init_state(), 1, lr=1e-3)
+    assert torch.equal(p.detach(), q)
