@@ -86,6 +86,17 @@ __device__ __forceinline__ uint32_t wave_max_bits(const float* x) {
     return lane_value(wave_incl_max(b), kWave - 1);
 }
 
+// What four codes of each moment stand for.
+__device__ __forceinline__ void decode4(uint32_t mc, uint32_t vc, float mu, float vu, Pack<float, 4>& m, Pack<float, 4>& v) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float q = (float)(int8_t)(mc >> 8 * j), r = (float)(vc >> 8 * j & 0xFFu);
+        m.v[j] = mu * (q * fabsf(q));
+        v.v[j] = vu * (r * r);
+        v.v[j] *= v.v[j];
+    }
+}
+
 // A wave's 256 elements: what it loads, and what becomes of it.  WHOLE: all 256 are there.
 template <typename G, typename C, bool CODES>
 struct AdamRun {
@@ -116,14 +127,9 @@ struct AdamRun {
         if (WHOLE) n = 4;
         float root[4];
         Pack<C, 4> copy;
+        if constexpr (CODES) decode4(mc, vc, mu, vu, m, v);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if constexpr (CODES) {
-                const float q = (float)(int8_t)(mc >> 8 * j), r = (float)(vc >> 8 * j & 0xFFu);
-                m.v[j] = mu * (q * fabsf(q));
-                v.v[j] = vu * (r * r);
-                v.v[j] *= v.v[j];
-            }
             const float gv = (float)g.v[j] * gs;
             m.v[j] = m.v[j] * a.beta1 + gv * a.one_beta1;
             v.v[j] = v.v[j] * a.beta2 + gv * gv * a.one_beta2;
@@ -240,16 +246,6 @@ __global__ __launch_bounds__(kBlock) void k_clip(const double* part, uint32_t pa
     scale[0] = (float)(x > max_norm ? grad_scale * (max_norm / x) : grad_scale);
     scale[1] = seen <= 3.4028234663852886e38f ? 0.0f : 1.0f;
     if (norm) *norm = seen;
-}
-
-__device__ __forceinline__ void decode4(uint32_t mc, uint32_t vc, float mu, float vu, Pack<float, 4>& m, Pack<float, 4>& v) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float q = (float)(int8_t)(mc >> 8 * j), r = (float)(vc >> 8 * j & 0xFFu);
-        m.v[j] = mu * (q * fabsf(q));
-        v.v[j] = vu * (r * r);
-        v.v[j] *= v.v[j];
-    }
 }
 
 __global__ __launch_bounds__(kBlock) void k_decode(const AdamChunk* chunks, uint32_t num_chunks, const uint8_t* m,
