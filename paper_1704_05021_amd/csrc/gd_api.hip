@@ -37,7 +37,10 @@ uint32_t sample_keys_for(uint64_t a, uint64_t b) {
 template <typename T>
 bool dev_alloc(gd_ctx* ctx, T** p, size_t count) {
     void* q = nullptr;
-    if (hipMalloc(&q, std::max<size_t>(count, 1) * sizeof(T)) != hipSuccess) return false;
+    if (hipMalloc(&q, std::max<size_t>(count, 1) * sizeof(T)) != hipSuccess) {
+        (void)hipGetLastError();  // the caller is told; the next launch must not find it
+        return false;
+    }
     ctx->allocations.push_back(q);
     *p = static_cast<T*>(q);
     return true;

@@ -46,7 +46,10 @@ struct DeviceMemory {
     bool alloc(T** p, size_t count) {
         void* q = nullptr;
         held.reserve(held.size() + 1);
-        if (hipMalloc(&q, std::max<size_t>(count, 1) * sizeof(T)) != hipSuccess) return false;
+        if (hipMalloc(&q, std::max<size_t>(count, 1) * sizeof(T)) != hipSuccess) {
+            (void)hipGetLastError();  // the caller is told; the next launch must not find it
+            return false;
+        }
         held.push_back(q);
         *p = static_cast<T*>(q);
         return true;
