@@ -306,7 +306,8 @@ gd_status gd_compress_static(const uint64_t* tensor_offsets, uint32_t num_tensor
  * formed with fused multiply-adds and matrix instructions; results are the
  * same on every run.  A handle holds a plan and device scratch, never a
  * caller's data, so layers of one shape may share one; one call at a time per
- * handle.  Nothing is allocated after create, so every call may be captured
+ * handle, on the GPU too (calls on different streams need an order between
+ * them, as their scratch is the same).  Nothing is allocated after create, so every call may be captured
  * into a graph (the numbers in the argument struct are captured by value).
  * Strides count elements between the starts of consecutive rows; within a row
  * elements are contiguous.  Pointers need the alignment of their element only.
@@ -430,10 +431,14 @@ gd_status gd_adamw_decode(gd_adamw* opt, const void* m, const void* v, const flo
  * and allocates their scratch: 32 MB for partial products, 1 KB per output for
  * the bias's gradient, and in 16 bits, where in or out is no multiple of 8,
  * room for padded copies of a product's operands, at most 512 MB (larger
- * products then take a slower form).  in and out are 1 to 2^22, max_rows at
+ * products then take a slower form).  Layers of one shape with two activations
+ * are two handles, each with its scratch.  in and out are 1 to 2^22, max_rows at
  * most 2^31 - 1.  The handle holds no weights.  Products are fastest where in
  * and out are multiples of 8 (16 for 8-bit operands) and operands start at
- * 16-byte boundaries.
+ * 16-byte boundaries.  Large products of such layers whose operands start
+ * elsewhere (a weight behind a bias of 10 in a flat buffer), and of 8-bit
+ * operands with in no multiple of 16, have no padded copies and take up to
+ * twice as long.
  */
 typedef struct gd_linear gd_linear;
 typedef enum {

@@ -15,9 +15,11 @@
 // contraction), so that their codes do not depend on this code's shape; the
 // parameter's update takes the hardware's reciprocal (one ulp).
 //
-// Measured over 137M elements: 719 us with 32-bit moments, 413 with 8-bit
-// ones (5.3 TB/s each, the rate of a large copy; one run a block of threads
-// took 474), decoding 239 us (5.7 TB/s); the norm adds 109 us (5.0 TB/s).
+// Measured over 137M elements, on several cards: 696 to 723 us with 32-bit
+// moments (5.3 to 5.5 TB/s, the rate of a large copy or above it), 366 to 413
+// with 8-bit ones (5.3 to 6.0 TB/s; one run a block of threads took 474),
+// decoding 215 to 268 us (5.1 to 6.4 TB/s); the norm adds 105 to 111 us (5.0
+// TB/s).
 
 #include <cmath>
 #include <new>

@@ -8,15 +8,21 @@
 // contiguous direction, so that a lane's four consecutive accumulators are
 // neighbours in memory.
 //
-// A tile of BI x BJ results takes one block.  Each step of 128 bytes of k is
-// loaded into registers while the step before is multiplied, then stored to
-// the other half of LDS: rows of eight 16-byte chunks, the chunk's place
+// A tile of BI x BJ results takes one block, in steps of 128 bytes of k that
+// pass through LDS: rows of eight 16-byte chunks, the chunk's place
 // exclusive-ored with bits of the row, so that neither the stores nor the
-// matrix fragments' reads of 16 rows pile onto a bank.  Operands that lie
-// across k are transposed in registers on their way (16-bit elements: one
-// byte permutation per two elements; 32-bit ones: none).  A matrix
-// instruction's lanes each take 16 bytes along k from one row; which k they
-// are does not matter as long as both operands agree.
+// matrix fragments' reads of 16 rows pile onto a bank.  A matrix instruction's
+// lanes each take 16 bytes along k from one row; which k they are does not
+// matter as long as both operands agree.  Two forms bring a step there:
+//
+// gemm_staged, for any operands: while step s is multiplied from one half of
+// LDS, step s + 1 goes from registers to the other half, and step s + 3 is
+// loaded into those registers (two steps are under way in them).  Operands
+// that lie across k are transposed in registers (16-bit elements: one byte
+// permutation per two elements; 32-bit ones: none).
+//
+// gemm_fetch, for 16- and 8-bit operands of whole 16-byte chunks: memory
+// instructions place a step in LDS, in no register (below).
 #pragma once
 
 #include "gd.h"
@@ -640,7 +646,7 @@ struct TileFetch {
                 fetch_far(k_of(n) < k_left ? (const void*)(from + off[n]) : &zero_chunk, to);
         }
     }
-    // This lane's part of the address of its fragment of 32 rows, 16 bytes of k each, number c of the step.
+    // This lane's part of the address of its fragment of 16 rows, 16 bytes of k a lane, number c of the step.
     static __device__ __forceinline__ uint32_t lane_at(int c) {
         const uint32_t l = lane_id();
         if constexpr (ACROSS) {
@@ -650,10 +656,10 @@ struct TileFetch {
         const uint32_t row = l & 15;
         return row * kStepBytes + (((c * 4 + (l >> 4)) ^ row_place(row)) << 4);
     }
-    // The fragment of rows row0 (a multiple of 32) on; lane is lane_at(c), the tile starts at `tile` in LDS.
+    // The fragment of rows row0 (a multiple of 16) on; lane is lane_at(c), the tile starts at `tile` in LDS.
     static __device__ __forceinline__ u4 fragment(const char* tile, uint32_t row0, uint32_t lane) {
         if constexpr (ACROSS) {
-            // rows 16 on are the next pair of chunks; a k's row is a power of two, so the exclusive-or keeps to it
+            // 16 rows are a pair of chunks; a k's row is a power of two of them, so the exclusive-or keeps to it
             typedef short s4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s4 lds_s4;
             const char* p = tile + (lane ^ (row0 / 16 << 5));

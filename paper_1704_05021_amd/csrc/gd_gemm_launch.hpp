@@ -38,7 +38,12 @@ bool pad(const void*& p, uint64_t& stride, uint64_t rows, uint32_t columns, Gemm
 // What a tile costs, in microseconds, measured on products in bfloat16 with k
 // of 4,096 (64 steps): a step of one tile alone on its compute unit, and of
 // each of several there at once (as many as LDS holds).  Every round of tiles
-// also takes about kRoundUs to fill the pipeline and write results.
+// also takes about kRoundUs to fill the pipeline and write results.  Products
+// in binary32, of 8 bits and through registers are planned with the same
+// figures, which are not theirs: their steps take longer (binary32 about four
+// times as long: 8192 x 4096 x 4096 is planned at 506 us and takes 1,970; through
+// registers in bfloat16 it takes 346), so the split of k and the join weigh
+// more in their plans than they should.
 struct TileCost {
     uint32_t bi, bj, threads, at_once;
     double alone_us, shared_us;
