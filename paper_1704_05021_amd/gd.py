@@ -852,7 +852,8 @@ class Linear(_Handle):
 
 
 def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.cuda.Stream] = None):
-    """(q, scale): rows of x in 8 bits, x = q * scale[row], scale[row] = max|x| / 127 (gd_quantise_rows)."""
+    """(q, scale): rows of x in 8 bits, x = q * scale[row], scale[row] = max|x| / 127 (gd_quantise_rows).  Codes carry
+    no gradient, so x may be one that requires it (a model's weight)."""
     code, index = _dtype_code(x.dtype), x.get_device()
     if index < 0 or x.dim() == 0 or x.size(-1) == 0:
         raise ValueError("x must be a GPU tensor of rows of at least one element")
@@ -862,8 +863,6 @@ def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.
     rows, xp, xs = _rows_on(index, x, "x", x.dtype, columns)
     _, qp, qs = _rows_on(index, q, "out", torch.int8, columns, rows)
     sp = _flat_on(index, scale, "scale", torch.float32, rows)
-    if x.requires_grad and torch.is_grad_enabled():
-        raise _untracked()
     if torch.cuda.current_device() != index:
         with torch.cuda.device(index):
             st = _lib().gd_quantise_rows(xp, code, rows, columns, xs, qp, qs, sp, _stream_on(index, stream, x, q, scale))

@@ -29,7 +29,6 @@ def test_forwards_refuse_what_autograd_would_follow():
         "int8": (lambda b, r: layer.forward_int8(q, s, wq, ws, b, r), (b, r)),
         "norm": (lambda x, g, r: norm.forward(x, g, r)[0], (x, gain, draw(4, 32))),
         "norm_int8": (lambda x, g, r: norm.forward_int8(x, g, r)[0], (x, gain, draw(4, 32))),
-        "quantise": (lambda x: gd.quantise_rows(x)[0], (x,)),
     }
     for name, (call, args) in calls.items():
         want = call(*args)
@@ -64,6 +63,12 @@ def test_inside_an_autograd_function():
         want = layer.backward(dy, x, w, pre, dbias=True)[:3]
     for g, v in zip(got, want):
         assert torch.equal(g, v)
+
+
+def test_rows_of_a_weight_are_quantised():
+    w = draw(48, 32)
+    for a, b in zip(gd.quantise_rows(w.clone().requires_grad_()), gd.quantise_rows(w)):
+        assert torch.equal(a, b) and not a.requires_grad
 
 
 def test_an_optimiser_step_takes_leaves():
