@@ -320,6 +320,55 @@ typedef enum {
     GD_F16 = 2   /* IEEE binary16 */
 } gd_dtype;
 
+typedef enum {
+    GD_I32 = 0, /* int32_t */
+    GD_I64 = 1  /* int64_t */
+} gd_index;
+
+/*
+ * gd_embed - rows of a weight by token, scaled, and the weight's gradient.
+ *   y[i] = scale * weight[t_i];  dweight[v] = scale * sum over i with t_i = v of dy[i]
+ * A token outside [0, vocab) is padding: its row of y is zeros, and its row of
+ * dy is not read.  dweight is written whole, rows of tokens that do not occur
+ * with zeros.  A token's rows are summed in their order, in binary32 within
+ * 16 to 64 of them and in 64 bits across those.
+ * gd_embed_create plans a vocabulary (1..2^31 - 1) of rows of dim (1..2^20)
+ * elements in `type` on the current device, for backward calls of at most
+ * max_rows (up to 2^24) rows, and allocates 16 bytes per row of those and
+ * 8 dim bytes per 64 of them (per 16 up to the 8,192nd) as scratch.  The
+ * forward call takes any number of rows.
+ */
+typedef struct gd_embed gd_embed;
+gd_status gd_embed_create(gd_embed** out, uint32_t vocab, uint32_t dim, gd_dtype type, uint64_t max_rows);
+void gd_embed_destroy(gd_embed* embed);
+
+typedef struct {
+    uint64_t rows;            /* 0: nothing is done */
+    const void* tokens;       /* [rows] of `index` */
+    const void* weight;       /* [vocab][dim] */
+    void* y;                  /* [rows][dim] */
+    uint64_t weight_stride, y_stride; /* at least dim */
+    float scale;              /* finite */
+    gd_index index;
+} gd_embed_io;
+
+/* GD_ERR_ARG for a NULL pointer, a stride below dim, a bad scale or index. */
+gd_status gd_embed_forward(gd_embed* embed, const gd_embed_io* io, void* stream);
+
+typedef struct {
+    uint64_t rows;            /* 0: dweight becomes 0 (accumulate: stays) */
+    const void* tokens;       /* [rows] of `index` */
+    const void* dy;           /* [rows][dim] in the type */
+    float* dweight;           /* [vocab][dim] in binary32 */
+    uint64_t dy_stride, dweight_stride; /* at least dim */
+    float scale;              /* finite */
+    gd_index index;
+    int accumulate;           /* not 0: dweight +=, and rows of tokens that do not occur stay */
+} gd_embed_grad;
+
+/* Errors as the forward call's, and GD_ERR_ARG for rows above max_rows. */
+gd_status gd_embed_backward(gd_embed* embed, const gd_embed_grad* io, void* stream);
+
 /*
  * gd_norm - root-mean-square norm of rows with the residual's addition.
  *   h = x + residual (or x);  y = h * weight / sqrt(mean(h^2) + eps)
@@ -366,6 +415,53 @@ typedef struct {
 } gd_norm_grad;
 
 gd_status gd_norm_backward(gd_norm* norm, const gd_norm_grad* io, void* stream);
+
+/*
+ * gd_layernorm - layer norm of rows with the residual's addition.
+ *   h = x + residual (or x);  c = h - mean(h)
+ *   y = c / sqrt(mean(c^2) + eps) * weight + bias
+ * A row's sums are formed in 64 bits; h is rounded where it is written, and y
+ * is formed from the sum as it was before that rounding.
+ * gd_layernorm_create plans rows of `dim` elements (1..32768) in `type` on the
+ * current device and allocates the scratch of the backward pass (4 KB per
+ * element of dim).
+ */
+typedef struct gd_layernorm gd_layernorm;
+gd_status gd_layernorm_create(gd_layernorm** out, uint32_t dim, gd_dtype type);
+void gd_layernorm_destroy(gd_layernorm* norm);
+
+typedef struct {
+    uint64_t rows;            /* 0: nothing is done */
+    const void* x;            /* [rows][dim] */
+    const void* residual;     /* [rows][dim], or NULL */
+    const void* weight;       /* [dim] */
+    const void* bias;         /* [dim], or NULL for zeros */
+    void* sum;                /* [rows][dim] receives h, or NULL; may be x or residual */
+    void* y;                  /* [rows][dim] in the type, or int8 when y_scale is given; in the type it may be x or
+                                 residual */
+    float* y_scale;           /* [rows], or NULL: as gd_norm_io's */
+    uint64_t x_stride, residual_stride, sum_stride, y_stride; /* at least dim */
+    float eps;                /* 0 or more */
+} gd_layernorm_io;
+
+/* GD_ERR_ARG for a NULL pointer, a stride below dim (0 is no stride) or a bad eps. */
+gd_status gd_layernorm_forward(gd_layernorm* norm, const gd_layernorm_io* io, void* stream);
+
+typedef struct {
+    uint64_t rows;            /* 0: dweight and dbias become 0 (accumulate: stay) */
+    const void* dy;           /* [rows][dim] gradient of y */
+    const void* x;            /* [rows][dim] what was normalised: sum of the forward call, or its x */
+    const void* weight;       /* [dim] */
+    const void* dsum;         /* [rows][dim] further gradient of the sum (down the residual stream), or NULL */
+    void* dx;                 /* [rows][dim] gradient of x and of residual; may be dy or dsum */
+    float* dweight;           /* [dim] in binary32, or NULL */
+    float* dbias;             /* [dim] in binary32, or NULL */
+    uint64_t dy_stride, x_stride, dsum_stride, dx_stride;
+    float eps;
+    int accumulate;           /* not 0: dweight and dbias += instead of = */
+} gd_layernorm_grad;
+
+gd_status gd_layernorm_backward(gd_layernorm* norm, const gd_layernorm_grad* io, void* stream);
 
 /*
  * gd_adamw - an AdamW step (Adam with decoupled weight decay; Kingma and Ba

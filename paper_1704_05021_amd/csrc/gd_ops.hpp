@@ -95,6 +95,26 @@ __device__ __forceinline__ void row_sums(double& a, double& b, double* lds_a, do
     }
 }
 
+// N such sums behind one barrier.
+template <int WAVES, int N, int LDS>
+__device__ __forceinline__ void row_sums(double (&v)[N], double (&lds)[N][LDS]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
+    if constexpr (WAVES > 1) {
+        const uint32_t w = wave_index();
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (lane_id() == 0) lds[k][w] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = 0.0;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) v[k] += lds[k][w / WAVES * WAVES + i];
+        }
+    }
+}
+
 // Largest of unsigned words over the threads of one row, likewise.
 template <int WAVES>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* lds) {

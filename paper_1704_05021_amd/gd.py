@@ -53,6 +53,14 @@ EXPORTS = [
     "gd_norm_destroy",
     "gd_norm_forward",
     "gd_norm_backward",
+    "gd_layernorm_create",
+    "gd_layernorm_destroy",
+    "gd_layernorm_forward",
+    "gd_layernorm_backward",
+    "gd_embed_create",
+    "gd_embed_destroy",
+    "gd_embed_forward",
+    "gd_embed_backward",
     "gd_adamw_create",
     "gd_adamw_destroy",
     "gd_adamw_blocks",
@@ -94,6 +102,15 @@ _NormIO = _struct("_NormIO", of=[(_u64, "rows"), (_vp, "x residual weight sum y 
 _NormGrad = _struct("_NormGrad", of=[(_u64, "rows"), (_vp, "dy x weight dsum dx dweight"),
                                      (_u64, "dy_stride x_stride dsum_stride dx_stride"), (_flt, "eps"),
                                      (_int, "accumulate")])
+_LayerNormIO = _struct("_LayerNormIO", of=[(_u64, "rows"), (_vp, "x residual weight bias sum y y_scale"),
+                                           (_u64, "x_stride residual_stride sum_stride y_stride"), (_flt, "eps")])
+_LayerNormGrad = _struct("_LayerNormGrad", of=[(_u64, "rows"), (_vp, "dy x weight dsum dx dweight dbias"),
+                                               (_u64, "dy_stride x_stride dsum_stride dx_stride"), (_flt, "eps"),
+                                               (_int, "accumulate")])
+_EmbedIO = _struct("_EmbedIO", of=[(_u64, "rows"), (_vp, "tokens weight y"), (_u64, "weight_stride y_stride"),
+                                   (_flt, "scale"), (_int, "index")])
+_EmbedGrad = _struct("_EmbedGrad", of=[(_u64, "rows"), (_vp, "tokens dy dweight"), (_u64, "dy_stride dweight_stride"),
+                                       (_flt, "scale"), (_int, "index accumulate")])
 _AdamWIO = _struct("_AdamWIO", of=[(_vp, "params grad m v m_unit v_unit copy norm"), (_int, "grad_type copy_type"),
                                    (_u64, "step"), (_dbl, "lr beta1 beta2 eps weight_decay max_norm grad_scale")])
 _LinearIO = _struct("_LinearIO", of=[(_u64, "rows"), (_vp, "x weight x_scale weight_scale bias residual y pre"),
@@ -150,12 +167,15 @@ def _lib() -> ctypes.CDLL:
     lib.gd_debug_state.restype = i32
     lib.gd_compress_static.argtypes = [vp, u32, vp, vp, vp, dbl, i32, i32, ctypes.POINTER(_Sparse), vp]
     lib.gd_compress_static.restype = i32
-    for what, args in (("norm", [ctypes.POINTER(vp), u32, i32]), ("linear", [ctypes.POINTER(vp), u32, u32, i32, i32, u64]),
+    for what, args in (("norm", [ctypes.POINTER(vp), u32, i32]), ("layernorm", [ctypes.POINTER(vp), u32, i32]),
+                       ("embed", [ctypes.POINTER(vp), u32, u32, i32, u64]), ("linear", [ctypes.POINTER(vp), u32, u32, i32, i32, u64]),
                        ("adamw", [ctypes.POINTER(vp), vp, u32, i32, vp])):
         create, destroy = getattr(lib, f"gd_{what}_create"), getattr(lib, f"gd_{what}_destroy")
         create.argtypes, create.restype = args, i32
         destroy.argtypes, destroy.restype = [vp], None
     for name, io in (("gd_norm_forward", _NormIO), ("gd_norm_backward", _NormGrad), ("gd_adamw_step", _AdamWIO),
+                     ("gd_layernorm_forward", _LayerNormIO), ("gd_layernorm_backward", _LayerNormGrad),
+                     ("gd_embed_forward", _EmbedIO), ("gd_embed_backward", _EmbedGrad),
                      ("gd_linear_forward", _LinearIO), ("gd_linear_backward", _LinearGrad)):
         getattr(lib, name).argtypes, getattr(lib, name).restype = [vp, ctypes.POINTER(io), vp], i32
     lib.gd_adamw_blocks.argtypes, lib.gd_adamw_blocks.restype = [vp], u64
@@ -718,6 +738,178 @@ def _gradient(given, accumulate, shape, device, stream):
     if accumulate:
         raise ValueError("accumulate needs the gradient to add to")
     return _new(stream, torch.empty, shape, dtype=torch.float32, device=device)
+
+
+class LayerNorm(_Handle):
+    """Layer norm of rows of ``dim`` elements with the residual's addition (gd_layernorm_*).
+
+    y = (h - mean(h)) / sqrt(var(h) + eps) * weight + bias, h = x + residual.  Tensors are [..., dim] in ``dtype``; one
+    object serves every layer of its shape on a stream.
+    """
+
+    _what = "layernorm"
+
+    def __init__(self, dim: int, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-5, device=None):
+        self.dim, self.dtype, self.eps = int(dim), dtype, float(eps)
+        if not 0 < self.dim < 1 << 32:
+            raise GDError(1, "LayerNorm")
+        self._create(device, self.dim, _dtype_code(dtype))
+
+    def forward(self, x, weight, bias=None, residual=None, out=None, sum_out=None, stream=None):
+        """(y, h); h is x itself without a residual.  ``sum_out`` and ``out`` may be x or residual."""
+        y, _, h = self._run(x, weight, bias, residual, out, None, False, sum_out, stream)
+        return y, h
+
+    def forward_int8(self, x, weight, bias=None, residual=None, out=None, scale=None, sum_out=None, stream=None):
+        """(q, scale, h): rows of y in 8 bits, y = q * scale[row], scale[row] = max|y| / 127."""
+        return self._run(x, weight, bias, residual, out, scale, True, sum_out, stream)
+
+    def _run(self, x, weight, bias, residual, out, scale, int8, sum_out, stream):
+        io = _LayerNormIO(eps=self.eps)
+        rows, io.x, io.x_stride = self._matrix(x, "x", self.dtype, self.dim)
+        io.rows = rows
+        io.weight = self._tensor(weight, "weight", self.dtype, self.dim)
+        if bias is not None:
+            io.bias = self._tensor(bias, "bias", self.dtype, self.dim)
+        y = out
+        if y is None:
+            y = (_new(stream, x.new_empty, x.shape, dtype=torch.int8) if int8
+                 else _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format))
+        _, io.y, io.y_stride = self._matrix(y, "out", torch.int8 if int8 else self.dtype, self.dim, rows)
+        if int8:
+            if scale is None:
+                scale = _new(stream, x.new_empty, x.shape[:-1], dtype=torch.float32)
+            io.y_scale = self._tensor(scale, "scale", torch.float32, rows)
+        h = x
+        if residual is not None:
+            _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.dim, rows)
+            h = _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format) if sum_out is None else sum_out
+        elif sum_out is not None:
+            h = sum_out
+        if h is not x or sum_out is not None:
+            _, io.sum, io.sum_stride = self._matrix(h, "sum_out", self.dtype, self.dim, rows)
+        if rows and (out is not None or sum_out is not None):
+            self._outputs_apart(io, out is not None and not int8, sum_out is not None)
+        if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                        (bias is not None and bias.requires_grad) or
+                                        (residual is not None and residual.requires_grad)):
+            raise _untracked()
+        st = _lib().gd_layernorm_forward(self._h, io, self._stream(stream, x, weight, bias, residual, y, scale, h))
+        if st != 0:
+            raise GDError(st, "gd_layernorm_forward")
+        return y, scale, h
+
+    def _outputs_apart(self, io, out, sum_out) -> None:
+        """A given out or sum_out lies apart from what the call reads, and from the other."""
+        rows, dim, size = io.rows, self.dim, self.dtype.itemsize
+        others = {"x": (io.x, rows, io.x_stride, dim), "weight": (io.weight, 1, dim, dim)}
+        if io.bias:
+            others["bias"] = (io.bias, 1, dim, dim)
+        if io.residual:
+            others["residual"] = (io.residual, rows, io.residual_stride, dim)
+        if sum_out:
+            _apart(size, "sum_out", (io.sum, rows, io.sum_stride, dim), others, ("x", "residual"))
+        if io.sum:
+            others["sum_out"] = (io.sum, rows, io.sum_stride, dim)
+        if out:
+            _apart(size, "out", (io.y, rows, io.y_stride, dim), others, ("x", "residual"))
+
+    def backward(self, dy, h, weight, dsum=None, dx=None, dweight=None, dbias=None, accumulate=False, stream=None):
+        """(dx, dweight, dbias): the gradient of x and of residual, and the weight's and the bias's in float32 (slices
+        of a flat gradient, say).  ``h`` is what forward returned, ``dsum`` a further gradient of h; dx may be dy or
+        dsum.  dbias False: a layer without a bias."""
+        io = _LayerNormGrad(eps=self.eps, accumulate=int(accumulate))
+        rows, io.dy, io.dy_stride = self._matrix(dy, "dy", self.dtype, self.dim)
+        io.rows = rows
+        _, io.x, io.x_stride = self._matrix(h, "h", self.dtype, self.dim, rows)
+        io.weight = self._tensor(weight, "weight", self.dtype, self.dim)
+        if dsum is not None:
+            _, io.dsum, io.dsum_stride = self._matrix(dsum, "dsum", self.dtype, self.dim, rows)
+        given = dx is not None
+        if not given:
+            dx = _new(stream, torch.empty_like, dy, memory_format=torch.contiguous_format)
+        _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.dim, rows)
+        dweight = _gradient(dweight, accumulate, (self.dim,), self.device, stream)
+        io.dweight = self._tensor(dweight, "dweight", torch.float32, self.dim)
+        if dbias is not False:
+            dbias = _gradient(dbias, accumulate, (self.dim,), self.device, stream)
+            io.dbias = self._tensor(dbias, "dbias", torch.float32, self.dim)
+        else:
+            dbias = None
+        if rows and given:
+            dim = self.dim
+            others = {"dy": (io.dy, rows, io.dy_stride, dim), "h": (io.x, rows, io.x_stride, dim),
+                      "weight": (io.weight, 1, dim, dim)}
+            if dsum is not None:
+                others["dsum"] = (io.dsum, rows, io.dsum_stride, dim)
+            _apart(self.dtype.itemsize, "dx", (io.dx, rows, io.dx_stride, dim), others, ("dy", "dsum"))
+        st = _lib().gd_layernorm_backward(self._h, io, self._stream(stream, dy, h, weight, dsum, dx, dweight, dbias))
+        if st != 0:
+            raise GDError(st, "gd_layernorm_backward")
+        return dx, dweight, dbias
+
+
+_INDEX = {torch.int32: 0, torch.int64: 1}
+
+
+def _ids_on(device: int, t: torch.Tensor, name: str, n: Optional[int] = None):
+    """(address, type code) of a contiguous tensor of token ids on the device."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _INDEX or t.get_device() != device or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous int32 or int64 tensor on cuda:{device}")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{name} has {t.numel()} elements, not {n}")
+    return t.data_ptr(), _INDEX[t.dtype]
+
+
+class Embedding(_Handle):
+    """Rows of a weight [vocab, dim] in ``dtype`` by token, times ``scale``, and the weight's gradient (gd_embed_*).
+
+    Tokens are int32 or int64 of any shape; one outside [0, vocab) is padding, whose rows are zeros and pass no
+    gradient.  ``max_rows``: the most tokens of a backward call.  The object holds no weights.
+    """
+
+    _what = "embed"
+
+    def __init__(self, vocab: int, dim: int, dtype: torch.dtype = torch.bfloat16, scale: float = 1.0,
+                 max_rows: int = 8192, device=None):
+        self.vocab, self.dim, self.dtype, self.scale = int(vocab), int(dim), dtype, float(scale)
+        if not (0 < self.vocab < 1 << 32 and 0 < self.dim < 1 << 32 and 0 <= int(max_rows) < 1 << 64):
+            raise GDError(1, "Embedding")
+        self._create(device, self.vocab, self.dim, _dtype_code(dtype), int(max_rows))
+
+    def forward(self, tokens, weight, out=None, stream=None):
+        """y [*tokens.shape, dim]."""
+        io = _EmbedIO(scale=self.scale)
+        io.tokens, io.index = _ids_on(self.device.index, tokens, "tokens")
+        rows = io.rows = tokens.numel()
+        _, io.weight, io.weight_stride = self._matrix(weight, "weight", self.dtype, self.dim, self.vocab)
+        given = out is not None
+        if not given:
+            out = _new(stream, weight.new_empty, (*tokens.shape, self.dim))
+        _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.dim, rows)
+        if given and rows:
+            _apart(self.dtype.itemsize, "out", (io.y, rows, io.y_stride, self.dim),
+                   {"weight": (io.weight, self.vocab, io.weight_stride, self.dim)})
+        if weight.requires_grad and torch.is_grad_enabled():
+            raise _untracked()
+        st = _lib().gd_embed_forward(self._h, io, self._stream(stream, tokens, weight, out))
+        if st != 0:
+            raise GDError(st, "gd_embed_forward")
+        return out
+
+    def backward(self, dy, tokens, dweight=None, accumulate=False, stream=None):
+        """dweight [vocab, dim] in float32 (a slice of a flat gradient, say), rows of tokens that do not occur zeros;
+        with ``accumulate`` it is added to, and those rows stay."""
+        io = _EmbedGrad(scale=self.scale, accumulate=int(accumulate))
+        io.tokens, io.index = _ids_on(self.device.index, tokens, "tokens")
+        rows = io.rows = tokens.numel()
+        _, io.dy, io.dy_stride = self._matrix(dy, "dy", self.dtype, self.dim, rows)
+        dweight = _gradient(dweight, accumulate, (self.vocab, self.dim), self.device, stream)
+        _, io.dweight, io.dweight_stride = self._matrix(dweight, "dweight", torch.float32, self.dim, self.vocab)
+        st = _lib().gd_embed_backward(self._h, io, self._stream(stream, dy, tokens, dweight))
+        if st != 0:
+            raise GDError(st, "gd_embed_backward")
+        return dweight
 
 
 class Linear(_Handle):
