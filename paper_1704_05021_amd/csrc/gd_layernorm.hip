@@ -30,86 +30,151 @@ constexpr uint32_t kLayerNormMaxBlocks = 1u << 20;
 struct RowStats {
     double mean;
     float rstd;
+    // h less the mean: in 64 bits and rounded once, as elementary operations give it, so that codes of 8 bits come out the
+    // same; or in 32 bits by the mean's two halves, two roundings, which is far below a 16-bit result's own.
+    __device__ __forceinline__ float centred(float h, float high, float low) const { return (h - high) - low; }
+    __device__ __forceinline__ float centred(float h) const { return (float)((double)h - mean); }
 };
-__device__ __forceinline__ RowStats row_stats(double pivot, double d, double dd, uint32_t dim, float eps) {
-    const double m = d / dim, var = dd / dim - m * m;
+__device__ __forceinline__ RowStats row_stats(double pivot, double d, double dd, double per_dim, float eps) {
+    const double m = d * per_dim, var = dd * per_dim - m * m;
     // a spread below the sums' rounding may come out a hair under zero; NaN stays
     return {pivot + m, (float)rsqrt((var < 0.0 ? 0.0 : var) + (double)eps)};
 }
 
-template <typename T, int WAVES, int V, bool INT8>
-__global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm(gd_layernorm_io io, uint32_t dim) {
+// How a row of dim elements divides into vectors of eight.
+enum RowEnds {
+    kShort = 0,  // dim is below 8: read element by element
+    kRagged = 1, // the last vector is the one that ends with the row; what it shares with the one before is left out
+    kWhole = 2
+};
+
+// The vector of eight elements that a thread takes of a row: where it lies, and which of its elements are the thread's.
+template <int ENDS>
+struct Place {
+    uint32_t at, dim, mine;  // mine: a bit for each
+    __device__ __forceinline__ Place(uint32_t e, uint32_t dim) : dim(dim) {
+        at = ENDS == kShort ? 0 : min(e, dim - 8);
+        if (ENDS == kWhole)
+            mine = e < dim ? 0xFF : 0;
+        else if (ENDS == kRagged)
+            mine = 0xFFu << min(e - at, 8u) & 0xFF;
+        else
+            mine = e ? 0 : (1u << dim) - 1;
+    }
+    // Every load is made, by every thread and whatever is asked for: loads behind conditions wait for one another
+    // (8192 x 4096 in bfloat16 forward took 88 us so).
+    template <typename T>
+    __device__ __forceinline__ Pack<T, 8> load(const T* row) const {
+        if constexpr (ENDS == kShort) {
+            Pack<T, 8> r;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r.v[j] = row[min((uint32_t)j, dim - 1)];
+            return r;
+        }
+        return load_pack<8>(row + at);
+    }
+    // In binary32, `rest` in place of what is not the thread's.
+    template <typename T>
+    __device__ __forceinline__ void get(float (&v)[8], const Pack<T, 8>& raw, float rest) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)raw.v[j];
+        if (mine == 0xFF) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = ENDS != kWhole && mine >> j & 1 ? v[j] : rest;
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, const Pack<T, 8>& r, bool on) const {
+        if (!on) return;
+        if (mine == 0xFF) {
+            if constexpr (sizeof(r) % 16 == 0)
+                store_stream<8>(row + at, r, 8);
+            else
+                store_pack<8>(row + at, r);
+        } else if (ENDS != kWhole) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (mine >> j & 1) row[at + j] = r.v[j];
+        }
+    }
+};
+
+template <typename T, int WAVES, int V, int ENDS, bool INT8>
+__global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm(gd_layernorm_io io, uint32_t dim, double per_dim) {
     using S = NormShape<WAVES>;
-    __shared__ double lds_d[S::kThreads / kWave], lds_dd[S::kThreads / kWave];
+    __shared__ double lds_sum[2][S::kThreads / kWave];
     __shared__ uint32_t lds_max[S::kThreads / kWave];
     const uint32_t t = threadIdx.x % S::kRow;
-    Pack<T, 8> w[V], b[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const uint32_t e = min((t + i * S::kRow) * 8, dim);
-        w[i] = load_some<8>((const T*)io.weight + e, (int)(dim - e));
-        b[i] = Pack<T, 8>{};
-        if (io.bias) b[i] = load_some<8>((const T*)io.bias + e, (int)(dim - e));
-    }
-    // every wave of a block takes the same number of turns (the last ones of rows past the end do nothing)
+    constexpr bool kOnce = INT8 || sizeof(T) == 4;  // c is rounded once, and not twice
+    const bool add = io.residual != nullptr, shift = io.bias != nullptr;
+    // every wave of a block takes the same number of turns (the last ones of rows past the end write nothing)
     for (uint64_t first = (uint64_t)blockIdx.x * S::kRows; first < io.rows; first += (uint64_t)gridDim.x * S::kRows) {
-        const uint64_t row = first + threadIdx.x / S::kRow;
+        const uint64_t row = first + threadIdx.x / S::kRow, from = min(row, io.rows - 1);
         const bool on = row < io.rows;
-        float h[V][8], pivot = on ? (float)((const T*)io.x)[row * io.x_stride] : 0.0f;
-        if (io.residual && on) pivot += (float)((const T*)io.residual)[row * io.residual_stride];
+        // without a residual or a bias what is there is read in their place, and not used
+        const T* x = (const T*)io.x + from * io.x_stride;
+        const T* r = add ? (const T*)io.residual + from * io.residual_stride : x;
+        const T* b = (const T*)(shift ? io.bias : io.weight);
+        const T x0 = *x, r0 = *r;
+        Pack<T, 8> xs[V], rs[V], ws[V], bs[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t e = (t + i * S::kRow) * 8;
-            const int n = on ? (int)(dim - min(e, dim)) : 0;
-            const Pack<T, 8> x = load_some<8>((const T*)io.x + row * io.x_stride + e, n);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[i][j] = (float)x.v[j];
-            if (io.residual) {
-                const Pack<T, 8> r = load_some<8>((const T*)io.residual + row * io.residual_stride + e, n);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[i][j] += (float)r.v[j];
-            }
+            const Place<ENDS> p((t + i * S::kRow) * 8, dim);
+            xs[i] = p.load(x);
+            rs[i] = p.load(r);
         }
-        double s = 0.0, ss = 0.0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t e = (t + i * S::kRow) * 8;
-            const int n = on ? (int)(dim - min(e, dim)) : 0;
+            const Place<ENDS> p((t + i * S::kRow) * 8, dim);
+            ws[i] = p.load((const T*)io.weight);
+            bs[i] = p.load(b);
+        }
+        // elements past the row's end are its first, which adds nothing to the sums
+        const float pivot = add ? (float)x0 + (float)r0 : (float)x0;
+        const double from_here = pivot;
+        float h[V][8];
+        double s[2] = {0.0, 0.0};  // of d and d^2
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const Place<ENDS> p((t + i * S::kRow) * 8, dim);
+            float rv[8];
+            p.get(h[i], xs[i], (float)x0);
+            p.get(rv, rs[i], (float)r0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const double d = j < n ? (double)h[i][j] - (double)pivot : 0.0;
-                s += d;
-                ss = fma(d, d, ss);
+                h[i][j] = add ? h[i][j] + rv[j] : h[i][j];
+                const double d = (double)h[i][j] - from_here;
+                s[0] += d;
+                s[1] = fma(d, d, s[1]);
             }
         }
-        row_sums<WAVES>(s, ss, lds_d, lds_dd);
-        const RowStats st = row_stats(pivot, s, ss, dim, io.eps);
+        row_sums<WAVES>(s, lds_sum);
+        const RowStats st = row_stats(from_here, s[0], s[1], per_dim, io.eps);
+        const float high = (float)st.mean, low = (float)(st.mean - (double)high);
         uint32_t big = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t e = (t + i * S::kRow) * 8;
-            const int n = on ? (int)(dim - min(e, dim)) : 0;
+            const Place<ENDS> p((t + i * S::kRow) * 8, dim);
             Pack<T, 8> sum, y;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 sum.v[j] = (T)h[i][j];
-                h[i][j] = (float)((double)h[i][j] - st.mean) * st.rstd * (float)w[i].v[j] + (float)b[i].v[j];
+                const float c = kOnce ? st.centred(h[i][j]) : st.centred(h[i][j], high, low);
+                h[i][j] = c * st.rstd * (float)ws[i].v[j] + (shift ? (float)bs[i].v[j] : 0.0f);
                 y.v[j] = (T)h[i][j];
-                if (j < n) big = max(big, __float_as_uint(h[i][j]) & 0x7FFFFFFFu);
+                if (INT8 && p.mine >> j & 1) big = max(big, __float_as_uint(h[i][j]) & 0x7FFFFFFFu);
             }
-            if (io.sum) store_stream<8>((T*)io.sum + row * io.sum_stride + e, sum, n);
-            if (!INT8) store_stream<8>((T*)io.y + row * io.y_stride + e, y, n);
+            if (io.sum) p.store((T*)io.sum + row * io.sum_stride, sum, on);
+            if (!INT8) p.store((T*)io.y + row * io.y_stride, y, on);
         }
         if constexpr (INT8) {
             const RowScale q = row_scale(row_max<WAVES>(big, lds_max));
             if (t == 0 && on) io.y_scale[row] = q.scale;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const uint32_t e = (t + i * S::kRow) * 8;
                 Pack<int8_t, 8> y;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y.v[j] = quantise(h[i][j], q.step);
-                store_some<8>((int8_t*)io.y + row * io.y_stride + e, y, on ? (int)(dim - min(e, dim)) : 0);
+                Place<ENDS>((t + i * S::kRow) * 8, dim).store((int8_t*)io.y + row * io.y_stride, y, on);
             }
         }
         if constexpr (WAVES > 1) __syncthreads();  // before the next row's sums
@@ -118,40 +183,41 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm(gd_lay
 
 // A block takes several rows, and loads each while it works on the one before;
 // its share of the sums over rows goes to part[blockIdx.x]: dweight's, then dbias's.
-template <typename T, int WAVES, int V>
-__global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm_back(gd_layernorm_grad io, uint32_t dim,
-                                                                               float* part) {
+template <typename T, int WAVES, int V, int ENDS>
+__global__ __launch_bounds__(NormShape<WAVES>::kThreads, 4) void k_layernorm_back(gd_layernorm_grad io, uint32_t dim,
+                                                                                  double per_dim, float* part) {
     using S = NormShape<WAVES>;
     __shared__ double lds_sum[2][4][S::kThreads / kWave];
     const uint32_t t = threadIdx.x % S::kRow;
     const uint64_t turn = (uint64_t)gridDim.x * S::kRows;
+    const bool add = io.dsum != nullptr;
     struct Row {
         Pack<T, 8> x[V], dy[V], dsum[V];
         T first;
     };
-    const auto here = [&](int i) { return (t + i * S::kRow) * 8; };
+    const auto place = [&](int i) { return Place<ENDS>((t + i * S::kRow) * 8, dim); };
     const auto load = [&](Row& r, uint64_t first) {
-        const uint64_t row = first + threadIdx.x / S::kRow;
-        r.first = row < io.rows ? ((const T*)io.x)[row * io.x_stride] : (T)0.0f;
+        const uint64_t row = min(first + threadIdx.x / S::kRow, io.rows - 1);
+        const T *x = (const T*)io.x + row * io.x_stride, *dy = (const T*)io.dy + row * io.dy_stride;
+        const T* dsum = add ? (const T*)io.dsum + row * io.dsum_stride : dy;
+        r.first = *x;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t e = here(i);
-            const int n = row < io.rows ? (int)(dim - min(e, dim)) : 0;
-            r.x[i] = load_some<8>((const T*)io.x + row * io.x_stride + e, n);
-            r.dy[i] = load_some<8>((const T*)io.dy + row * io.dy_stride + e, n);
-            if (io.dsum) r.dsum[i] = load_some<8>((const T*)io.dsum + row * io.dsum_stride + e, n);
+            r.x[i] = place(i).load(x);
+            r.dy[i] = place(i).load(dy);
+            r.dsum[i] = place(i).load(dsum);
         }
     };
     constexpr bool kAhead = V == 1;  // more elements a thread leave no registers for it
-    Pack<T, 8> w[V];
+    Pack<T, 8> ws[V];
     float dw[V][8], db[V][8];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const uint32_t e = min(here(i), dim);
-        w[i] = load_some<8>((const T*)io.weight + e, (int)(dim - e));
+        ws[i] = place(i).load((const T*)io.weight);
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.0f;
     }
+    const auto w = [&](int i, int j) { return (float)ws[i].v[j]; };  // not 0 past the row's end, but dy is
     Row next;
     uint64_t first = (uint64_t)blockIdx.x * S::kRows;
     if (kAhead) load(next, first);
@@ -161,15 +227,16 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm_back(g
         if (!kAhead) load(next, first);
         const Row r = next;
         if (kAhead && first + turn < io.rows) load(next, first + turn);
-        const double pivot = (float)r.first;
-        double s[4] = {0.0, 0.0, 0.0, 0.0};  // of d, d^2, a, a d
+        const double from_here = (float)r.first;
+        double s[4] = {0.0, 0.0, 0.0, 0.0};  // of d, d^2, a, a d: d and a are 0 past the row's end
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int n = on ? (int)(dim - min(here(i), dim)) : 0;
+            float x[8], g[8];
+            place(i).get(x, r.x[i], (float)r.first);
+            place(i).get(g, r.dy[i], 0.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const double d = j < n ? (double)(float)r.x[i].v[j] - pivot : 0.0;
-                const double a = (float)r.dy[i].v[j] * (float)w[i].v[j];
+                const double d = (double)x[j] - from_here, a = g[j] * w(i, j);
                 s[0] += d;
                 s[1] = fma(d, d, s[1]);
                 s[2] += a;
@@ -178,24 +245,25 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm_back(g
         }
         // the two turns' sums lie apart, so one barrier a row is enough
         row_sums<WAVES>(s, lds_sum[odd]);
-        const RowStats st = row_stats(pivot, s[0], s[1], dim, io.eps);
-        const float mean_a = (float)(s[2] / dim);
-        const float mean_ax = (float)((s[3] - s[2] * (s[0] / dim)) / dim * st.rstd);  // mean(a xhat)
+        const RowStats st = row_stats(from_here, s[0], s[1], per_dim, io.eps);
+        const float high = (float)st.mean, low = (float)(st.mean - (double)high);
+        const float mean_a = (float)(s[2] * per_dim);
+        const float mean_ax = (float)((s[3] - s[2] * (s[0] * per_dim)) * per_dim * st.rstd);  // mean(a xhat)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t e = here(i);
-            const int n = on ? (int)(dim - min(e, dim)) : 0;
+            float x[8], g[8];
+            place(i).get(x, r.x[i], (float)r.first);
+            place(i).get(g, r.dy[i], 0.0f);
             Pack<T, 8> d;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float g = (float)r.dy[i].v[j], xhat = (float)((double)(float)r.x[i].v[j] - st.mean) * st.rstd;
-                dw[i][j] += n > 0 ? g * xhat : 0.0f;
-                db[i][j] += g;
-                float v = st.rstd * (g * (float)w[i].v[j] - mean_a - xhat * mean_ax);
-                if (io.dsum) v += (float)r.dsum[i].v[j];
-                d.v[j] = (T)v;
+                const float xhat = st.centred(x[j], high, low) * st.rstd;
+                dw[i][j] += S::kRows == 1 || on ? g[j] * xhat : 0.0f;
+                db[i][j] += S::kRows == 1 || on ? g[j] : 0.0f;
+                const float v = st.rstd * (g[j] * w(i, j) - mean_a - xhat * mean_ax);
+                d.v[j] = (T)(add ? v + (float)r.dsum[i].v[j] : v);
             }
-            store_stream<8>((T*)io.dx + row * io.dx_stride + e, d, n);
+            place(i).store((T*)io.dx + row * io.dx_stride, d, on);
         }
     }
     if (!part) return;
@@ -221,23 +289,16 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm_back(g
                 }
     }
     const auto put = [&](float* out, float* partial, const float (&v)[V][8]) {
+        float* to = gridDim.x > 1 ? partial : out;  // few rows: the block's share is all of it
+        if (!to) return;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t e = min(here(i), dim);
-            const int n = (int)(dim - e);
+            const Place<ENDS> p = place(i);
             Pack<float, 8> d;
+            if (to == out && io.accumulate) d = p.load(to);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d.v[j] = v[i][j];
-            if (gridDim.x > 1) {
-                store_some<8>(partial + e, d, n);
-            } else if (out) {  // few rows: the block's share is all of it
-                if (io.accumulate) {
-                    const Pack<float, 8> was = load_some<8>(out + e, n);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d.v[j] += was.v[j];
-                }
-                store_some<8>(out + e, d, n);
-            }
+            for (int j = 0; j < 8; ++j) d.v[j] = to == out && io.accumulate ? d.v[j] + v[i][j] : v[i][j];
+            p.store(to, d, true);
         }
     };
     put(io.dweight, part + (uint64_t)blockIdx.x * 2 * dim, dw);
@@ -268,18 +329,18 @@ __global__ __launch_bounds__(kJoinColumns* kJoinGroups) void k_layernorm_join(co
     *out = (float)s;
 }
 
-template <typename T, int WAVES, int V>
+template <typename T, int WAVES, int V, int ENDS>
 hipError_t launch_layernorm(const gd_layernorm_io& io, uint32_t dim, hipStream_t st) {
     using S = NormShape<WAVES>;
     const uint32_t blocks = (uint32_t)std::min<uint64_t>((io.rows + S::kRows - 1) / S::kRows, kLayerNormMaxBlocks);
     if (io.y_scale)
-        k_layernorm<T, WAVES, V, true><<<dim3(blocks), dim3(S::kThreads), 0, st>>>(io, dim);
+        k_layernorm<T, WAVES, V, ENDS, true><<<dim3(blocks), dim3(S::kThreads), 0, st>>>(io, dim, 1.0 / dim);
     else
-        k_layernorm<T, WAVES, V, false><<<dim3(blocks), dim3(S::kThreads), 0, st>>>(io, dim);
+        k_layernorm<T, WAVES, V, ENDS, false><<<dim3(blocks), dim3(S::kThreads), 0, st>>>(io, dim, 1.0 / dim);
     return hipGetLastError();
 }
 
-template <typename T, int WAVES, int V>
+template <typename T, int WAVES, int V, int ENDS>
 hipError_t launch_layernorm_back(const gd_layernorm_grad& io, uint32_t dim, float* part, hipStream_t st) {
     using S = NormShape<WAVES>;
     const bool sums = io.dweight || io.dbias;
@@ -289,7 +350,7 @@ hipError_t launch_layernorm_back(const gd_layernorm_grad& io, uint32_t dim, floa
     const bool one = turns <= 4 && turns * dim <= 1u << 14;
     const uint32_t parts = one ? (turns != 0) : (uint32_t)std::min<uint64_t>(turns, most);
     if (parts) {
-        k_layernorm_back<T, WAVES, V><<<dim3(parts), dim3(S::kThreads), 0, st>>>(io, dim, sums ? part : nullptr);
+        k_layernorm_back<T, WAVES, V, ENDS><<<dim3(parts), dim3(S::kThreads), 0, st>>>(io, dim, 1.0 / dim, sums ? part : nullptr);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -297,6 +358,13 @@ hipError_t launch_layernorm_back(const gd_layernorm_grad& io, uint32_t dim, floa
     k_layernorm_join<<<dim3((2 * dim + kJoinColumns - 1) / kJoinColumns), dim3(kJoinColumns * kJoinGroups), 0, st>>>(
         part, parts, dim, io.dweight, io.dbias, io.accumulate != 0);
     return hipGetLastError();
+}
+
+template <int WAVES, typename F>
+hipError_t with_ends(uint32_t dim, F f) {
+    if constexpr (WAVES == 1)
+        if (dim < 8) return f(std::integral_constant<int, kShort>());
+    return dim % 8 ? f(std::integral_constant<int, kRagged>()) : f(std::integral_constant<int, kWhole>());
 }
 
 }  // namespace gd
@@ -351,7 +419,9 @@ gd_status gd_layernorm_forward(gd_layernorm* n, const gd_layernorm_io* io, void*
     if (!guard.ok) return GD_ERR_HIP;
     const hipError_t e = gd::with_type(n->type, [&](auto zero) {
         return gd::with_shape(n->dim, false, [&](auto waves, auto v) {
-            return gd::launch_layernorm<decltype(zero), waves(), v()>(*io, n->dim, (hipStream_t)stream);
+            return gd::with_ends<waves()>(n->dim, [&](auto ends) {
+                return gd::launch_layernorm<decltype(zero), waves(), v(), ends()>(*io, n->dim, (hipStream_t)stream);
+            });
         });
     });
     return e == hipSuccess ? GD_OK : GD_ERR_HIP;
@@ -366,7 +436,9 @@ gd_status gd_layernorm_backward(gd_layernorm* n, const gd_layernorm_grad* io, vo
     if (!guard.ok) return GD_ERR_HIP;
     const hipError_t e = gd::with_type(n->type, [&](auto zero) {
         return gd::with_shape(n->dim, true, [&](auto waves, auto v) {
-            return gd::launch_layernorm_back<decltype(zero), waves(), v()>(*io, n->dim, n->part, (hipStream_t)stream);
+            return gd::with_ends<waves()>(n->dim, [&](auto ends) {
+                return gd::launch_layernorm_back<decltype(zero), waves(), v(), ends()>(*io, n->dim, n->part, (hipStream_t)stream);
+            });
         });
     });
     return e == hipSuccess ? GD_OK : GD_ERR_HIP;

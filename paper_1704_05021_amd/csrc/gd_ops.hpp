@@ -95,22 +95,30 @@ __device__ __forceinline__ void row_sums(double& a, double& b, double* lds_a, do
     }
 }
 
-// N such sums behind one barrier.
+// Up to four such sums behind one barrier, each wave's shares joined by 16 lanes a sum (all of them read by every
+// thread would take 64 registers for four sums of eight waves).
 template <int WAVES, int N, int LDS>
 __device__ __forceinline__ void row_sums(double (&v)[N], double (&lds)[N][LDS]) {
+    static_assert(N <= 4 && WAVES <= 16);
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
     if constexpr (WAVES > 1) {
-        const uint32_t w = wave_index();
+        const uint32_t w = wave_index(), k = lane_id() / 16, from = lane_id() % 16;
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (lane_id() == 0) lds[k][w] = v[k];
+        for (int i = 0; i < N; ++i)
+            if (lane_id() == 0) lds[i][w] = v[i];
         __syncthreads();
+        double s = -0.0;
+        if (k < (uint32_t)N && from < (uint32_t)WAVES) s = lds[k][w / WAVES * WAVES + from];
+        s += dpp_f64<0x111, 0xF>(s);  // row_shr:1
+        s += dpp_f64<0x112, 0xF>(s);  // row_shr:2
+        s += dpp_f64<0x114, 0xF>(s);  // row_shr:4
+        s += dpp_f64<0x118, 0xF>(s);  // row_shr:8
+        const uint64_t bits = (uint64_t)__double_as_longlong(s);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            v[k] = 0.0;
-#pragma unroll
-            for (int i = 0; i < WAVES; ++i) v[k] += lds[k][w / WAVES * WAVES + i];
+        for (int i = 0; i < N; ++i) {
+            const uint32_t lo = lane_value((uint32_t)bits, i * 16 + 15), hi = lane_value((uint32_t)(bits >> 32), i * 16 + 15);
+            v[i] = __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
         }
     }
 }
