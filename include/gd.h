@@ -591,6 +591,119 @@ typedef struct {
 gd_status gd_linear_backward(gd_linear* layer, const gd_linear_grad* io, void* stream);
 
 /*
+ * gd_logprob - log probabilities of given tokens under logits over a
+ * vocabulary, with the entropy and the top alternatives, and their gradient.
+ *   z = scale * logits;  lse = log(sum_v exp(z_v));  p = exp(z - lse)
+ *   logp = z_t - lse;  entropy = -sum_v p_v log p_v
+ *   dlogits_v = scale * (dlogp (1[v = t] - p_v) - dentropy p_v (log p_v + entropy))
+ * A logit of minus infinity is masked: its p is 0, and it adds nothing to the
+ * entropy.  A row of which every logit is masked has log probabilities of minus
+ * infinity, entropy 0 and no gradient.  A token outside [0, vocab) is padding:
+ * its logp is 0, whatever dlogp is there passes no gradient; the row's entropy and
+ * alternatives are as every row's.  A row with plus infinity or a NaN has NaN,
+ * and where no gradient comes down to a row (padding, or dlogp of 0, and
+ * dentropy of 0) its gradient is 0 whatever it holds.
+ * gd_logprob_create plans rows of vocab (1..2^31 - 1) logits in `type` for
+ * calls of at most max_rows (up to 2^31 - 1) rows on the current device, and
+ * allocates 300 KB of scratch.
+ */
+typedef struct gd_logprob gd_logprob;
+gd_status gd_logprob_create(gd_logprob** out, uint32_t vocab, gd_dtype type, uint64_t max_rows);
+void gd_logprob_destroy(gd_logprob* score);
+
+typedef struct {
+    uint64_t rows;            /* 0: nothing is done */
+    const void* logits;       /* [rows][vocab] */
+    const void* tokens;       /* [rows] of `index` */
+    float* logp;              /* [rows], or NULL */
+    float* entropy;           /* [rows], or NULL */
+    float* stats;             /* [rows][2] receives the largest z and the log of the sum of exp(z - largest), whose sum
+                                 is lse, for a backward call; or NULL */
+    float* top_logp;          /* [rows][top] receives the log probabilities of the likeliest tokens, in falling order */
+    int64_t* top_id;          /* [rows][top] and their ids: of equal logits the lower id first, a NaN before all numbers */
+    uint64_t stride;          /* at least vocab */
+    float scale;              /* finite, above 0 */
+    gd_index index;
+    uint32_t top;             /* 0 (top_logp and top_id are not read) to 64, at most vocab */
+} gd_logprob_io;
+
+/* GD_ERR_ARG for a NULL pointer, rows above max_rows, a bad stride, scale, index or top. */
+gd_status gd_logprob_forward(gd_logprob* score, const gd_logprob_io* io, void* stream);
+
+typedef struct {
+    uint64_t rows;
+    const void* logits;       /* [rows][vocab] */
+    const void* tokens;       /* [rows] of `index` */
+    const float* dlogp;       /* [rows] */
+    const float* dentropy;    /* [rows], or NULL for zeros */
+    const float* stats;       /* [rows][2] of a forward call of the same logits and scale, or NULL: the call forms them */
+    const float* entropy;     /* [rows] of that forward call; needed with stats and dentropy */
+    void* dlogits;            /* [rows][vocab] in the type; may be logits, at the same stride */
+    float* logp_out;          /* [rows] as the forward call's, or NULL; without stats only */
+    float* entropy_out;       /* [rows] likewise */
+    uint64_t stride, dlogits_stride; /* at least vocab */
+    float scale;
+    gd_index index;
+} gd_logprob_grad;
+
+/* Errors as the forward call's, and GD_ERR_ARG for logp_out or entropy_out with stats. */
+gd_status gd_logprob_backward(gd_logprob* score, const gd_logprob_grad* io, void* stream);
+
+/*
+ * gd_distill - the distance of logits to a teacher's top logits, and its
+ * gradient.  For every row the teacher names `top` ids and its logits there:
+ *   w = softmax over j of scale * teacher_j;  q = softmax over v of scale * logits_v
+ *   loss = sum_j w_j (log w_j - log q_id_j)
+ *   dlogits_v = scale dloss (q_v - sum over j with id_j = v of w_j)
+ * An id outside [0, vocab) or a teacher's logit of minus infinity names
+ * nothing (weight 0); a row that names nothing has loss 0 and no gradient.  An
+ * id may stand twice: its weights add.  A named token whose logit is minus
+ * infinity makes the loss infinite; a row of which every logit is has no
+ * gradient.  Other conventions as gd_logprob's.
+ * gd_distill_create as gd_logprob_create; 20 KB of scratch.
+ */
+typedef struct gd_distill gd_distill;
+gd_status gd_distill_create(gd_distill** out, uint32_t vocab, gd_dtype type, uint64_t max_rows);
+void gd_distill_destroy(gd_distill* distill);
+
+typedef struct {
+    uint64_t rows;            /* 0: nothing is done */
+    const void* logits;       /* [rows][vocab], the student's */
+    const void* ids;          /* [rows][top] of `index` */
+    const void* teacher;      /* [rows][top] logits in teacher_type */
+    float* loss;              /* [rows], or NULL */
+    float* stats;             /* [rows][2] as gd_logprob_io's, or NULL */
+    uint64_t stride;          /* at least vocab */
+    uint64_t ids_stride, teacher_stride; /* at least top */
+    float scale;              /* finite, above 0 */
+    uint32_t top;             /* 1..256 */
+    gd_index index;
+    gd_dtype teacher_type;
+} gd_distill_io;
+
+/* GD_ERR_ARG for a NULL pointer, rows above max_rows, a bad stride, scale, index, type or top. */
+gd_status gd_distill_forward(gd_distill* distill, const gd_distill_io* io, void* stream);
+
+typedef struct {
+    uint64_t rows;
+    const void* logits;
+    const void* ids;
+    const void* teacher;
+    const float* dloss;       /* [rows] */
+    const float* stats;       /* [rows][2] of a forward call of the same logits and scale, or NULL: the call forms them */
+    void* dlogits;            /* [rows][vocab] in the type; may be logits, at the same stride */
+    float* loss_out;          /* [rows], or NULL; without stats only */
+    uint64_t stride, ids_stride, teacher_stride, dlogits_stride;
+    float scale;
+    uint32_t top;
+    gd_index index;
+    gd_dtype teacher_type;
+} gd_distill_grad;
+
+/* Errors as the forward call's, and GD_ERR_ARG for loss_out with stats. */
+gd_status gd_distill_backward(gd_distill* distill, const gd_distill_grad* io, void* stream);
+
+/*
  * Rows in 8 bits, as the 8-bit products take them: with max = max_j |x[i][j]|,
  * scale[i] = max / 127 and q = x * (127 * (1 / max)) rounded to the nearest
  * whole number (ties to even), every operation rounded to binary32.  So q is

@@ -61,6 +61,14 @@ EXPORTS = [
     "gd_embed_destroy",
     "gd_embed_forward",
     "gd_embed_backward",
+    "gd_logprob_create",
+    "gd_logprob_destroy",
+    "gd_logprob_forward",
+    "gd_logprob_backward",
+    "gd_distill_create",
+    "gd_distill_destroy",
+    "gd_distill_forward",
+    "gd_distill_backward",
     "gd_adamw_create",
     "gd_adamw_destroy",
     "gd_adamw_blocks",
@@ -111,6 +119,17 @@ _EmbedIO = _struct("_EmbedIO", of=[(_u64, "rows"), (_vp, "tokens weight y"), (_u
                                    (_flt, "scale"), (_int, "index")])
 _EmbedGrad = _struct("_EmbedGrad", of=[(_u64, "rows"), (_vp, "tokens dy dweight"), (_u64, "dy_stride dweight_stride"),
                                        (_flt, "scale"), (_int, "index accumulate")])
+_LogProbIO = _struct("_LogProbIO", of=[(_u64, "rows"), (_vp, "logits tokens logp entropy stats top_logp top_id"),
+                                       (_u64, "stride"), (_flt, "scale"), (_int, "index"), (ctypes.c_uint32, "top")])
+_LogProbGrad = _struct("_LogProbGrad", of=[(_u64, "rows"), (_vp, "logits tokens dlogp dentropy stats entropy dlogits "
+                                                                 "logp_out entropy_out"),
+                                           (_u64, "stride dlogits_stride"), (_flt, "scale"), (_int, "index")])
+_DistillIO = _struct("_DistillIO", of=[(_u64, "rows"), (_vp, "logits ids teacher loss stats"),
+                                       (_u64, "stride ids_stride teacher_stride"), (_flt, "scale"),
+                                       (ctypes.c_uint32, "top"), (_int, "index teacher_type")])
+_DistillGrad = _struct("_DistillGrad", of=[(_u64, "rows"), (_vp, "logits ids teacher dloss stats dlogits loss_out"),
+                                           (_u64, "stride ids_stride teacher_stride dlogits_stride"), (_flt, "scale"),
+                                           (ctypes.c_uint32, "top"), (_int, "index teacher_type")])
 _AdamWIO = _struct("_AdamWIO", of=[(_vp, "params grad m v m_unit v_unit copy norm"), (_int, "grad_type copy_type"),
                                    (_u64, "step"), (_dbl, "lr beta1 beta2 eps weight_decay max_norm grad_scale")])
 _LinearIO = _struct("_LinearIO", of=[(_u64, "rows"), (_vp, "x weight x_scale weight_scale bias residual y pre"),
@@ -168,7 +187,8 @@ def _lib() -> ctypes.CDLL:
     lib.gd_compress_static.argtypes = [vp, u32, vp, vp, vp, dbl, i32, i32, ctypes.POINTER(_Sparse), vp]
     lib.gd_compress_static.restype = i32
     for what, args in (("norm", [ctypes.POINTER(vp), u32, i32]), ("layernorm", [ctypes.POINTER(vp), u32, i32]),
-                       ("embed", [ctypes.POINTER(vp), u32, u32, i32, u64]), ("linear", [ctypes.POINTER(vp), u32, u32, i32, i32, u64]),
+                       ("embed", [ctypes.POINTER(vp), u32, u32, i32, u64]),
+                       ("logprob", [ctypes.POINTER(vp), u32, i32, u64]), ("distill", [ctypes.POINTER(vp), u32, i32, u64]), ("linear", [ctypes.POINTER(vp), u32, u32, i32, i32, u64]),
                        ("adamw", [ctypes.POINTER(vp), vp, u32, i32, vp])):
         create, destroy = getattr(lib, f"gd_{what}_create"), getattr(lib, f"gd_{what}_destroy")
         create.argtypes, create.restype = args, i32
@@ -176,6 +196,8 @@ def _lib() -> ctypes.CDLL:
     for name, io in (("gd_norm_forward", _NormIO), ("gd_norm_backward", _NormGrad), ("gd_adamw_step", _AdamWIO),
                      ("gd_layernorm_forward", _LayerNormIO), ("gd_layernorm_backward", _LayerNormGrad),
                      ("gd_embed_forward", _EmbedIO), ("gd_embed_backward", _EmbedGrad),
+                     ("gd_logprob_forward", _LogProbIO), ("gd_logprob_backward", _LogProbGrad),
+                     ("gd_distill_forward", _DistillIO), ("gd_distill_backward", _DistillGrad),
                      ("gd_linear_forward", _LinearIO), ("gd_linear_backward", _LinearGrad)):
         getattr(lib, name).argtypes, getattr(lib, name).restype = [vp, ctypes.POINTER(io), vp], i32
     lib.gd_adamw_blocks.argtypes, lib.gd_adamw_blocks.restype = [vp], u64
@@ -1041,6 +1063,199 @@ class Linear(_Handle):
             others["dz"] = span
         if dx and io.dx:
             _apart(size, "dx", (io.dx, rows, io.dx_stride, k), others)
+
+
+@dataclass
+class LogProbs:
+    """What TokenLogProbs.forward says of each row, in float32."""
+
+    logp: torch.Tensor  # of the given token
+    entropy: Optional[torch.Tensor] = None
+    stats: Optional[torch.Tensor] = None  # [..., 2]: the largest scaled logit, the log of the sum of exp relative to it
+    top_logp: Optional[torch.Tensor] = None  # [..., top], falling
+    top_ids: Optional[torch.Tensor] = None  # [..., top] int64
+
+
+class _Scores(_Handle):
+    """Rows of ``vocab`` logits in ``dtype``, multiplied by ``scale`` (one over a temperature) before all else, for
+    calls of at most ``max_rows`` rows."""
+
+    def __init__(self, vocab: int, dtype: torch.dtype = torch.bfloat16, scale: float = 1.0, max_rows: int = 8192,
+                 device=None):
+        self.vocab, self.dtype, self.scale = int(vocab), dtype, float(scale)
+        if not (0 < self.vocab < 1 << 32 and 0 <= int(max_rows) < 1 << 64):
+            raise GDError(1, type(self).__name__)
+        self._create(device, self.vocab, _dtype_code(dtype), int(max_rows))
+
+    def _logits(self, io, logits) -> int:
+        rows, io.logits, io.stride = self._matrix(logits, "logits", self.dtype, self.vocab)
+        io.rows, io.scale = rows, self.scale
+        return rows
+
+    def _dlogits(self, io, logits, out, stream, apart):
+        """The gradient's buffer: new, or a given one that is the logits themselves or lies apart from what is read."""
+        given = out is not None
+        if not given:
+            out = _new(stream, torch.empty_like, logits, memory_format=torch.contiguous_format)
+        _, io.dlogits, io.dlogits_stride = self._matrix(out, "out", self.dtype, self.vocab, io.rows)
+        if given and io.rows:
+            _apart(self.dtype.itemsize, "out", (io.dlogits, io.rows, io.dlogits_stride, self.vocab),
+                   {"logits": (io.logits, io.rows, io.stride, self.vocab), **apart}, ("logits",))
+        return out
+
+
+class TokenLogProbs(_Scores):
+    """Log probabilities of given tokens under rows of logits, the rows' entropy and top alternatives, and the gradient
+    (gd_logprob_*).
+
+    Logits are [..., vocab], tokens int32 or int64 of the shape before; a token outside [0, vocab) is padding, whose log
+    probability is 0 and passes no gradient.  A logit of minus infinity is masked.
+    """
+
+    _what = "logprob"
+
+    def forward(self, logits, tokens, top: int = 0, entropy: bool = True, out: Optional[LogProbs] = None, stream=None):
+        """LogProbs; ``top`` up to 64 alternatives, of equal logits the lower id first.  ``out``: one of an earlier call
+        of the same shape, to write again."""
+        io = _LogProbIO()
+        rows = self._logits(io, logits)
+        io.tokens, io.index = _ids_on(self.device.index, tokens, "tokens", rows)
+        io.top, shape = top, tokens.shape
+        if out is None:
+            made = functools.partial(_new, stream, logits.new_empty, dtype=torch.float32)
+            out = LogProbs(made(shape), made(shape) if entropy else None, made((*shape, 2)))
+            if top:
+                out.top_logp, out.top_ids = made((*shape, top)), _new(stream, logits.new_empty, (*shape, top), dtype=torch.int64)
+        io.logp = self._tensor(out.logp, "out.logp", torch.float32, rows)
+        io.stats = self._tensor(out.stats, "out.stats", torch.float32, 2 * rows)
+        if entropy:
+            io.entropy = self._tensor(out.entropy, "out.entropy", torch.float32, rows)
+        if top:
+            io.top_logp = self._tensor(out.top_logp, "out.top_logp", torch.float32, rows * top)
+            io.top_id = self._tensor(out.top_ids, "out.top_ids", torch.int64, rows * top)
+        if logits.requires_grad and torch.is_grad_enabled():
+            raise _untracked()
+        st = _lib().gd_logprob_forward(self._h, io, self._stream(stream, logits, tokens, out.logp, out.entropy, out.stats,
+                                                                 out.top_logp, out.top_ids))
+        if st != 0:
+            raise GDError(st, "gd_logprob_forward")
+        return out
+
+    def backward(self, logits, tokens, dlogp, dentropy=None, scores: Optional[LogProbs] = None, out=None, stream=None):
+        """dlogits, from the gradients of the log probabilities and (or None) of the entropies, float32.  ``scores``:
+        what forward returned for these logits, to spare a pass over them; ``out`` may be the logits."""
+        return self._back(logits, tokens, dlogp, dentropy, scores, out, stream, False)[1]
+
+    def forward_backward(self, logits, tokens, dlogp, dentropy=None, out=None, stream=None):
+        """(LogProbs, dlogits) in one call, where the gradients of the log probabilities are known before they are (a
+        mean's are): without stats and alternatives, and with the entropy where ``dentropy`` is given."""
+        return self._back(logits, tokens, dlogp, dentropy, None, out, stream, True)
+
+    def _back(self, logits, tokens, dlogp, dentropy, scores, out, stream, forward):
+        io = _LogProbGrad()
+        rows = self._logits(io, logits)
+        io.tokens, io.index = _ids_on(self.device.index, tokens, "tokens", rows)
+        io.dlogp = self._tensor(dlogp, "dlogp", torch.float32, rows)
+        result = None
+        if dentropy is not None:
+            io.dentropy = self._tensor(dentropy, "dentropy", torch.float32, rows)
+        if scores is not None:
+            io.stats = self._tensor(scores.stats, "scores.stats", torch.float32, 2 * rows)
+            if dentropy is not None:
+                io.entropy = self._tensor(scores.entropy, "scores.entropy", torch.float32, rows)
+        if forward:
+            made = functools.partial(_new, stream, logits.new_empty, tokens.shape, dtype=torch.float32)
+            result = LogProbs(made(), None if dentropy is None else made())
+            io.logp_out = result.logp.data_ptr()
+            if dentropy is not None:
+                io.entropy_out = result.entropy.data_ptr()
+        apart = {}
+        if self.dtype == torch.float32 and out is not None and rows:
+            apart = {name: (t.data_ptr(), 1, rows, rows) for name, t in (("dlogp", dlogp), ("dentropy", dentropy)) if t is not None}
+            if scores is not None:
+                apart["scores.stats"] = (io.stats, 1, 2 * rows, 2 * rows)
+                if io.entropy:
+                    apart["scores.entropy"] = (io.entropy, 1, rows, rows)
+        out = self._dlogits(io, logits, out, stream, apart)
+        if forward and logits.requires_grad and torch.is_grad_enabled():
+            raise _untracked()
+        st = _lib().gd_logprob_backward(self._h, io, self._stream(
+            stream, logits, tokens, dlogp, dentropy, out, *(() if scores is None else (scores.stats, scores.entropy)),
+            *((result.logp, result.entropy) if forward else ())))
+        if st != 0:
+            raise GDError(st, "gd_logprob_backward")
+        return result, out
+
+
+class Distill(_Scores):
+    """The distance of rows of logits to a teacher's top logits, and its gradient (gd_distill_*).
+
+    For every row the teacher names up to 256 ids, int32 or int64 [..., top], and its logits there [..., top] in float32,
+    bfloat16 or float16; both softmaxes are taken of logits times ``scale``.  loss = sum w (log w - log q) over what is
+    named.  An id outside [0, vocab) or a teacher's logit of minus infinity names nothing.
+    """
+
+    _what = "distill"
+
+    def forward(self, logits, ids, teacher, stream=None):
+        """(loss, stats): float32 [...], and what backward takes to spare a pass over the logits."""
+        io = _DistillIO()
+        rows = self._logits(io, logits)
+        self._named(io, ids, teacher, rows)
+        loss = _new(stream, logits.new_empty, logits.shape[:-1], dtype=torch.float32)
+        stats = _new(stream, logits.new_empty, (*logits.shape[:-1], 2), dtype=torch.float32)
+        io.loss, io.stats = loss.data_ptr(), stats.data_ptr()
+        if torch.is_grad_enabled() and (logits.requires_grad or teacher.requires_grad):
+            raise _untracked()
+        st = _lib().gd_distill_forward(self._h, io, self._stream(stream, logits, ids, teacher, loss, stats))
+        if st != 0:
+            raise GDError(st, "gd_distill_forward")
+        return loss, stats
+
+    def backward(self, logits, ids, teacher, dloss, stats=None, out=None, stream=None):
+        """dlogits; ``stats``: what forward returned for these logits; ``out`` may be the logits."""
+        return self._back(logits, ids, teacher, dloss, stats, out, stream, False)[1]
+
+    def forward_backward(self, logits, ids, teacher, dloss, out=None, stream=None):
+        """(loss, dlogits) in one call, where the gradients of the losses are known before they are (a mean's are)."""
+        return self._back(logits, ids, teacher, dloss, None, out, stream, True)
+
+    def _named(self, io, ids, teacher, rows) -> None:
+        if not isinstance(ids, torch.Tensor) or ids.dtype not in _INDEX:
+            raise TypeError("ids must be int32 or int64")
+        if ids.dim() == 0 or ids.size(-1) == 0:
+            raise ValueError("ids must have rows of at least one element")
+        io.top, io.index = ids.size(-1), _INDEX[ids.dtype]
+        _, io.ids, io.ids_stride = self._matrix(ids, "ids", ids.dtype, io.top, rows)
+        io.teacher_type = _dtype_code(teacher.dtype)
+        _, io.teacher, io.teacher_stride = self._matrix(teacher, "teacher", teacher.dtype, io.top, rows)
+
+    def _back(self, logits, ids, teacher, dloss, stats, out, stream, forward):
+        io = _DistillGrad()
+        rows = self._logits(io, logits)
+        self._named(io, ids, teacher, rows)
+        io.dloss = self._tensor(dloss, "dloss", torch.float32, rows)
+        if stats is not None:
+            io.stats = self._tensor(stats, "stats", torch.float32, 2 * rows)
+        loss = None
+        if forward:
+            loss = _new(stream, logits.new_empty, logits.shape[:-1], dtype=torch.float32)
+            io.loss_out = loss.data_ptr()
+        apart = {}
+        if out is not None and rows:
+            if teacher.dtype == self.dtype:
+                apart["teacher"] = (io.teacher, rows, io.teacher_stride, io.top)
+            if self.dtype == torch.float32:
+                apart["dloss"] = (io.dloss, 1, rows, rows)
+                if stats is not None:
+                    apart["stats"] = (io.stats, 1, 2 * rows, 2 * rows)
+        out = self._dlogits(io, logits, out, stream, apart)
+        if forward and torch.is_grad_enabled() and (logits.requires_grad or teacher.requires_grad):
+            raise _untracked()
+        st = _lib().gd_distill_backward(self._h, io, self._stream(stream, logits, ids, teacher, dloss, stats, out, loss))
+        if st != 0:
+            raise GDError(st, "gd_distill_backward")
+        return loss, out
 
 
 def quantise_rows(x: torch.Tensor, out=None, scale=None, stream: Optional[torch.cuda.Stream] = None):
