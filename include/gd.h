@@ -591,6 +591,53 @@ typedef struct {
 gd_status gd_linear_backward(gd_linear* layer, const gd_linear_grad* io, void* stream);
 
 /*
+ * gd_gated - a gated layer y = act(x Wg^T + bg) * (x Wu^T + bu), the first half
+ * of a gated feed-forward block (the second is a gd_linear), and its backward.
+ * weight [2 out][in] holds Wg's rows and then Wu's, bias [2 out] bg and then
+ * bu.  y is formed from both sums before they are rounded.
+ * gd_gated_create, its scratch and its limits are as gd_linear_create's with 2
+ * out for out (so out is at most 2^21); the same alignments are fastest.
+ */
+typedef struct gd_gated gd_gated;
+gd_status gd_gated_create(gd_gated** out, uint32_t in, uint32_t out_features, gd_dtype type, gd_act act,
+                          uint64_t max_rows);
+void gd_gated_destroy(gd_gated* layer);
+
+typedef struct {
+    uint64_t rows;            /* 0: nothing is done */
+    const void* x;            /* [rows][in] in the type, or int8 with both scales */
+    const void* weight;       /* [2 out][in] likewise */
+    const float* x_scale;     /* [rows] and [2 out], or both NULL, as gd_linear_io's */
+    const float* weight_scale;
+    const void* bias;         /* [2 out] in the type, or NULL */
+    void* y;                  /* [rows][out] in the type */
+    void* pre;                /* [rows][2 out] in the type receives both sums with their bias for the backward, or NULL */
+    uint64_t x_stride, weight_stride; /* at least in */
+    uint64_t y_stride, pre_stride;    /* at least out and 2 out; every stride at most 2^22 */
+} gd_gated_io;
+
+/* Errors as gd_linear_forward's. */
+gd_status gd_gated_forward(gd_gated* layer, const gd_gated_io* io, void* stream);
+
+typedef struct {
+    uint64_t rows;            /* 0: dweight and dbias become 0 (accumulate: stay) */
+    const void* dy;           /* [rows][out] gradient of y */
+    const void* x;            /* [rows][in]; needed for dweight */
+    const void* weight;       /* [2 out][in]; needed for dx */
+    const void* pre;          /* [rows][2 out] pre of the forward call: g and u */
+    void* dz;                 /* [rows][2 out] receives dy u act'(g) and dy act(g), rounded to the type, the gradient of
+                                 both sums that the products below are taken with; may be pre.  Under GD_ACT_RELU both
+                                 are 0 where g is not above 0, whatever dy is there. */
+    void* dx;                 /* [rows][in] receives dz weight, or NULL */
+    float* dweight;           /* [2 out][in] in binary32, rows at dweight_stride: dz^T x, or NULL */
+    float* dbias;             /* [2 out] in binary32: sum over rows of dz, or NULL */
+    uint64_t dy_stride, x_stride, weight_stride, pre_stride, dz_stride, dx_stride, dweight_stride;
+    int accumulate;           /* not 0: dweight and dbias += instead of = */
+} gd_gated_grad;
+
+gd_status gd_gated_backward(gd_gated* layer, const gd_gated_grad* io, void* stream);
+
+/*
  * gd_logprob - log probabilities of given tokens under logits over a
  * vocabulary, with the entropy and the top alternatives, and their gradient.
  *   z = scale * logits;  lse = log(sum_v exp(z_v));  p = exp(z - lse)

@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libgd.so")
 SOURCES = ["gd_select.hip", "gd_sampled.hip", "gd_dense.hip", "gd_layout.hip", "gd_cand.hip", "gd_direct.hip", "gd_quant.hip", "gd_apply.hip", "gd_api.hip", "gd_static.hip",
-           "gd_norm.hip", "gd_layernorm.hip", "gd_embed.hip", "gd_score.hip", "gd_adamw.hip", "gd_linear.hip", "gd_gemm_bf16.hip", "gd_gemm_f16.hip", "gd_gemm_f32.hip"]
+           "gd_norm.hip", "gd_layernorm.hip", "gd_embed.hip", "gd_score.hip", "gd_adamw.hip", "gd_linear.hip", "gd_gated.hip", "gd_gemm_bf16.hip", "gd_gemm_f16.hip", "gd_gemm_f32.hip"]
 HEADERS = ["gd_device.hpp", "gd_kernels.h", "gd_internal.h", "gd_host.hpp", "gd_ops.hpp", "gd_rows.hpp", "gd_gemm.hpp",
            "gd_gemm_launch.hpp"]
 

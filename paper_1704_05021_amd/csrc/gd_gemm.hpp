@@ -23,7 +23,16 @@
 //
 // gemm_fetch, for 16- and 8-bit operands of whole 16-byte chunks: memory
 // instructions place a step in LDS, in no register (below).
+//
+// PAIR, for gated layers: P holds 2 I rows, I that gate and then the I that are
+// gated, and result i is act(gate i) times gated i.  A tile takes both rows of
+// its results, 16 that gate and the 16 that they gate in turn: so the two sums
+// of a result are in the same lane's registers, two fragments apart, both
+// waves' shares of the operand come from one half each, and the products are
+// those of one product with 2 I rows.
 #pragma once
+
+#include <type_traits>
 
 #include "gd.h"
 #include "gd_ops.hpp"
@@ -155,6 +164,30 @@ __device__ __forceinline__ void activate(int act, float (&s)[N]) {
     }
 }
 
+// s act'(z) in place of s.  A choice of act is one branch for all of them: one
+// an element took longer than the memory.  ReLU chooses and does not multiply:
+// a unit that is off passes nothing, a gradient that is not finite neither.
+template <bool EXACT, int N>
+__device__ __forceinline__ void act_slope(int act, const float (&z)[N], float (&s)[N]) {
+    if (act == GD_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = z[j] > 0.0f ? s[j] : 0.0f;
+    } else if (act == GD_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float e;
+            const float cdf = normal<EXACT>(z[j], e);
+            s[j] *= cdf + z[j] * (e * 0.39894228040143268f);
+        }
+    } else if (act == GD_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float q = sigmoid<EXACT>(z[j]);
+            s[j] *= q * (1.0f + z[j] * (1.0f - q));
+        }
+    }
+}
+
 template <int N, typename O>
 __device__ __forceinline__ void store_result(O* p, const Pack<O, N>& r, int n, bool stream) {
     if constexpr (N * sizeof(O) % 16 == 0) {
@@ -205,6 +238,39 @@ __device__ __forceinline__ void finish(const Finish& f, const Columns<O, N>& col
     store_result((O*)f.out + j * f.out_stride + i, y, n, f.stream);
 }
 
+// The same for gated results i to i + N - 1 of `all`, from the sums of their two rows.
+template <typename O, int N>
+struct PairColumns {
+    Columns<O, N> gate, gated;
+    __device__ __forceinline__ PairColumns(const Finish& f, uint32_t i, uint32_t all, int n)
+        : gate(f, i, n), gated(f, i + all, n) {}
+};
+template <typename O, int N>
+__device__ __forceinline__ void finish_pair(const Finish& f, const PairColumns<O, N>& cols, uint64_t j, uint32_t i, uint32_t all,
+                                            float (&g)[N], float (&u)[N], int n) {
+    if (f.p_scale) {
+        const float qs = f.q_scale[j];
+#pragma unroll
+        for (int c = 0; c < N; ++c) g[c] *= qs * cols.gate.scale.v[c], u[c] *= qs * cols.gated.scale.v[c];
+    }
+    if (f.bias)
+#pragma unroll
+        for (int c = 0; c < N; ++c) g[c] += (float)cols.gate.bias.v[c], u[c] += (float)cols.gated.bias.v[c];
+    if (f.pre) {
+        Pack<O, N> a, b;
+#pragma unroll
+        for (int c = 0; c < N; ++c) a.v[c] = (O)g[c], b.v[c] = (O)u[c];
+        O* pre = (O*)f.pre + j * f.pre_stride + i;
+        store_result(pre, a, n, f.stream);
+        store_result(pre + all, b, n, f.stream);
+    }
+    activate<sizeof(O) == 4>(f.act, g);
+    Pack<O, N> y;
+#pragma unroll
+    for (int c = 0; c < N; ++c) y.v[c] = (O)(g[c] * u[c]);
+    store_result((O*)f.out + j * f.out_stride + i, y, n, f.stream);
+}
+
 constexpr int kStepBytes = 128;  // of k in a step
 constexpr int kRowChunks = kStepBytes / 16;
 
@@ -223,6 +289,11 @@ __device__ __forceinline__ u4 shift_down(u4 v, uint32_t bytes) {
     return u4{__builtin_amdgcn_alignbyte(v[1], v[0], by), __builtin_amdgcn_alignbyte(v[2], v[1], by),
               __builtin_amdgcn_alignbyte(v[3], v[2], by), __builtin_amdgcn_alignbyte(0u, v[3], by)};
 }
+
+// Row r of a tile of pairs, 16 rows that gate before the 16 that they gate, is its result pair_row(r)'s.  A wave carries
+// eight rows at a time, and every turn of four waves or eight starts at a multiple of 32: so all of its rows gate, or none.
+__device__ __forceinline__ uint32_t pair_row(uint32_t r) { return r / 32 * 16 + r % 16; }
+__device__ __forceinline__ uint32_t pair_half() { return wave_index() >> 1 & 1; }
 
 // A step's R rows of one operand on their way from memory to LDS, the
 // block's THREADS threads sharing them.  Where a row or k ends inside a
@@ -253,6 +324,14 @@ struct TileLoad<E, false, R, THREADS> {
             const uint32_t id = n * THREADS + threadIdx.x;
             off[n] = min(id / kRowChunks, rows - row0 - 1) * (uint32_t)stride + first_k(n);
         }
+    }
+    // Of a pair of operands `rows` apart: result row0 is the tile's first (see pair_row).
+    __device__ void start_pair(const void* p, uint64_t stride, uint32_t row0, uint32_t rows, uint32_t k0, uint32_t k) {
+        base = (const E*)p + ((uint64_t)row0 + (uint64_t)pair_half() * rows) * stride + k0;
+        few = k < (uint32_t)CE;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            off[n] = min(pair_row((n * THREADS + threadIdx.x) / kRowChunks), rows - row0 - 1) * (uint32_t)stride + first_k(n);
     }
     __device__ __forceinline__ bool always_whole() const { return true; }
     __device__ __forceinline__ void load_whole(Regs& g, uint32_t step) const {
@@ -404,16 +483,21 @@ __device__ __forceinline__ void tile_of(const GemmArgs& a, uint32_t b, uint32_t&
 
 // The block's sums to their results.  A wave's go through LDS, 16 rows j of
 // all its i at a time, so that it reads and writes whole runs of memory.
-template <typename E, typename O, typename TL>
+template <typename E, typename O, typename TL, bool PAIR = false>
 __device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::Sum (&acc)[TL::NI][TL::NJ], char* lds,
                                            uint32_t i0, uint32_t j0, uint32_t split) {
     const uint32_t wave = wave_index(), lane = lane_id(), wi = wave % TL::WI, wj = wave / TL::WI;
     constexpr int W = TL::NI * 16;  // results of a row
     float* rows = (float*)(lds + wave * (W * 16 * 4));
-    constexpr int kPer = 8, kLanes = W / kPer, kAtOnce = kWave / kLanes;
-    const uint32_t col = lane % kLanes * kPer, i = i0 + wi * W + col;
+    constexpr int kPer = 8, kResults = PAIR ? W / 2 : W, kLanes = kResults / kPer, kAtOnce = kWave / kLanes;
+    const uint32_t col = lane % kLanes * kPer, i = i0 + wi * kResults + col;
     const int n = i < a.I ? (int)min(a.I - i, (uint32_t)kPer) : 0;
-    const Columns<O, kPer> cols(a.fin, i, a.part ? 0 : n);
+    const std::conditional_t<PAIR, PairColumns<O, kPer>, Columns<O, kPer>> cols = [&] {
+        if constexpr (PAIR)
+            return PairColumns<O, kPer>(a.fin, i, a.I, a.part ? 0 : n);
+        else
+            return Columns<O, kPer>(a.fin, i, a.part ? 0 : n);
+    }();
 #pragma unroll
     for (int j = 0; j < TL::NJ; ++j) {
 #pragma unroll
@@ -425,22 +509,48 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::S
 #pragma unroll 1
         for (uint32_t r = lane / kLanes; r < 16; r += kAtOnce) {
             const uint32_t row = j0 + (wj * TL::NJ + j) * 16 + r;
+            const auto get = [&](uint32_t from, float (&s)[kPer]) {
+                const f4 lo = *(const f4*)(rows + r * W + (from ^ ((r & 7) << 2)));
+                const f4 hi = *(const f4*)(rows + r * W + ((from + 4) ^ ((r & 7) << 2)));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[c] = lo[c], s[c + 4] = hi[c];
+            };
+            const auto put = [&](const float (&s)[kPer], uint64_t to) {
+                Pack<float, kPer> v;
+#pragma unroll
+                for (int c = 0; c < kPer; ++c) v.v[c] = s[c];
+                store_some<kPer>(a.part + to, v, n);
+            };
+            const auto whole = [&](float (&s)[kPer]) {
+                if constexpr (sizeof(E) == 1)
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c) s[c] = (float)bits_as<int>(s[c]);
+            };
             float s[kPer];
-            const f4 lo = *(const f4*)(rows + r * W + (col ^ ((r & 7) << 2)));
-            const f4 hi = *(const f4*)(rows + r * W + ((col + 4) ^ ((r & 7) << 2)));
-#pragma unroll
-            for (int c = 0; c < 4; ++c) s[c] = lo[c], s[c + 4] = hi[c];
-            if (row < a.J && n > 0) {
-                if (a.part) {
-                    Pack<float, kPer> v;
-#pragma unroll
-                    for (int c = 0; c < kPer; ++c) v.v[c] = s[c];
-                    store_some<kPer>(a.part + ((uint64_t)split * a.J + row) * a.I + i, v, n);
-                } else {
-                    if constexpr (sizeof(E) == 1)
-#pragma unroll
-                        for (int c = 0; c < kPer; ++c) s[c] = (float)bits_as<int>(s[c]);
-                    finish<O, kPer>(a.fin, cols, row, i, s, n);
+            if constexpr (PAIR) {
+                float u[kPer];
+                get(col / 16 * 32 + col % 16, s);
+                get(col / 16 * 32 + col % 16 + 16, u);
+                if (row < a.J && n > 0) {
+                    if (a.part) {
+                        const uint64_t to = ((uint64_t)split * a.J + row) * 2 * a.I + i;
+                        put(s, to);
+                        put(u, to + a.I);
+                    } else {
+                        whole(s);
+                        whole(u);
+                        finish_pair<O, kPer>(a.fin, cols, row, i, a.I, s, u, n);
+                    }
+                }
+            } else {
+                get(col, s);
+                if (row < a.J && n > 0) {
+                    if (a.part) {
+                        put(s, ((uint64_t)split * a.J + row) * a.I + i);
+                    } else {
+                        whole(s);
+                        finish<O, kPer>(a.fin, cols, row, i, s, n);
+                    }
                 }
             }
         }
@@ -449,20 +559,23 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, typename Mma<E>::S
 }
 
 // Tile `block` of a product, its share `split` of k, through registers; lds holds TL::kLds bytes.
-template <typename E, typename O, bool PA, bool QA, typename TL, int SETS = 2>
+template <typename E, typename O, bool PA, bool QA, typename TL, bool PAIR = false, int SETS = 2>
 __device__ __forceinline__ void gemm_staged(const GemmArgs& a, uint32_t block, uint32_t split, char* lds) {
     using M = Mma<E>;
     constexpr uint32_t KE = kStepBytes / sizeof(E);
     uint32_t ti, tj;
     tile_of(a, block, ti, tj);
-    const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
+    const uint32_t i0 = ti * (PAIR ? TL::BI / 2 : TL::BI), j0 = tj * TL::BJ;
     const uint32_t k0 = split * a.steps * KE;
     const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * KE);
     const uint32_t steps = k_end > k0 ? (k_end - k0 + KE - 1) / KE : 0;
 
     TileLoad<E, PA, TL::BI, TL::kThreads> lp;
     TileLoad<E, QA, TL::BJ, TL::kThreads> lq;
-    lp.start(a.p, a.p_stride, i0, a.I, k0, a.K);
+    if constexpr (PAIR)
+        lp.start_pair(a.p, a.p_stride, i0, a.I, k0, a.K);
+    else
+        lp.start(a.p, a.p_stride, i0, a.I, k0, a.K);
     lq.start(a.q, a.q_stride, j0, a.J, k0, a.K);
     typename M::Sum acc[TL::NI][TL::NJ];
 #pragma unroll
@@ -539,13 +652,13 @@ __device__ __forceinline__ void gemm_staged(const GemmArgs& a, uint32_t block, u
             __syncthreads();
         }
 
-    store_tile<E, O, TL>(a, acc, lds, i0, j0, split);
+    store_tile<E, O, TL, PAIR>(a, acc, lds, i0, j0, split);
 }
 
-template <typename E, typename O, bool PA, bool QA, typename TL>
+template <typename E, typename O, bool PA, bool QA, typename TL, bool PAIR = false>
 __global__ __launch_bounds__(TL::kThreads, 2) void k_gemm(GemmArgs a) {
     __shared__ __align__(16) char lds[TL::kLds];
-    gemm_staged<E, O, PA, QA, TL>(a, blockIdx.x, blockIdx.y, lds);
+    gemm_staged<E, O, PA, QA, TL, PAIR>(a, blockIdx.x, blockIdx.y, lds);
 }
 
 // ---- The same product with operands that memory instructions place in LDS ----
@@ -634,6 +747,16 @@ struct TileFetch {
             off[n] = (ACROSS ? k_of(n) * stride + r : r * stride + k_of(n)) * (uint32_t)sizeof(E);
         }
     }
+    // Of a pair of operands `rows` apart, along k: result row0 is the tile's first (see pair_row).
+    __device__ void start_pair(const void* p, uint64_t st, uint32_t row0, uint32_t rows, uint32_t k0) {
+        static_assert(!ACROSS && THREADS % 256 == 0);
+        stride = (uint32_t)st;
+        base = (const E*)p + ((uint64_t)row0 + (uint64_t)pair_half() * rows) * st + k0;
+        per_step = KE * sizeof(E);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            off[n] = (min(pair_row(row_of(n)), rows - row0 - 1) * stride + k_of(n)) * (uint32_t)sizeof(E);
+    }
     template <bool WHOLE>
     __device__ __forceinline__ void issue(uint32_t step, uint32_t k_left, uint32_t lds_at) const {
         const char* from = (const char*)base + step * per_step;
@@ -688,7 +811,7 @@ __global__ __launch_bounds__(kBlock) void k_pad(const E* from, uint64_t stride, 
 }
 
 // Tile `block` of a product, its share `split` of k; lds holds TL::DEEP steps.
-template <typename E, typename O, bool PA, bool QA, typename TL>
+template <typename E, typename O, bool PA, bool QA, typename TL, bool PAIR = false>
 __device__ __forceinline__ void gemm_fetch(const GemmArgs& a, uint32_t block, uint32_t split, char* lds) {
     using M = Mma<E>;
     using FP = TileFetch<E, PA, TL::BI, TL::kThreads>;
@@ -697,13 +820,16 @@ __device__ __forceinline__ void gemm_fetch(const GemmArgs& a, uint32_t block, ui
     constexpr int DEEP = TL::DEEP, kLoads = FP::N + FQ::N;
     uint32_t ti, tj;
     tile_of(a, block, ti, tj);
-    const uint32_t i0 = ti * TL::BI, j0 = tj * TL::BJ;
+    const uint32_t i0 = ti * (PAIR ? TL::BI / 2 : TL::BI), j0 = tj * TL::BJ;
     const uint32_t k0 = split * a.steps * FP::KE;
     const uint32_t k_end = min((uint64_t)a.K, (uint64_t)k0 + (uint64_t)a.steps * FP::KE);
     const uint32_t left = k_end > k0 ? k_end - k0 : 0, steps = (left + FP::KE - 1) / FP::KE, whole = left / FP::KE;
     FP fp;
     FQ fq;
-    fp.start(a.p, a.p_stride, i0, a.I, k0);
+    if constexpr (PAIR)
+        fp.start_pair(a.p, a.p_stride, i0, a.I, k0);
+    else
+        fp.start(a.p, a.p_stride, i0, a.I, k0);
     fq.start(a.q, a.q_stride, j0, a.J, k0);
     typename M::Sum acc[TL::NI][TL::NJ];
 #pragma unroll
@@ -806,13 +932,13 @@ __device__ __forceinline__ void gemm_fetch(const GemmArgs& a, uint32_t block, ui
         }
     }
     __syncthreads();
-    store_tile<E, O, TL>(a, acc, lds, i0, j0, split);
+    store_tile<E, O, TL, PAIR>(a, acc, lds, i0, j0, split);
 }
 
-template <typename E, typename O, bool PA, bool QA, typename TL>
+template <typename E, typename O, bool PA, bool QA, typename TL, bool PAIR = false>
 __global__ __launch_bounds__(TL::kThreads) void k_gemm_fetch(GemmArgs a) {
     __shared__ __align__(1024) char lds[TL::DEEP * TL::kStage];
-    gemm_fetch<E, O, PA, QA, TL>(a, blockIdx.x, blockIdx.y, lds);
+    gemm_fetch<E, O, PA, QA, TL, PAIR>(a, blockIdx.x, blockIdx.y, lds);
 }
 
 // The two products of a small layer's backward pass in one launch: blocks
@@ -835,36 +961,45 @@ __global__ __launch_bounds__(TileSmall::kThreads, DIRECT ? 1 : 2) void k_gemm_pa
 }
 
 // Joins the splits' sums, four results a thread.
-template <typename E, typename O>
+template <typename E, typename O, bool PAIR = false>
 __global__ __launch_bounds__(kBlock) void k_join(GemmArgs a, uint32_t splits) {
     const uint32_t per_row = (a.I + 3) / 4;
-    const uint64_t all = (uint64_t)per_row * a.J;
+    const uint64_t all = (uint64_t)per_row * a.J, wide = PAIR ? 2ull * a.I : a.I;
     for (uint64_t t = (uint64_t)blockIdx.x * kBlock + threadIdx.x; t < all; t += (uint64_t)gridDim.x * kBlock) {
         const uint64_t j = t / per_row;
         const uint32_t i = (uint32_t)(t - j * per_row) * 4;
         const int n = (int)min(a.I - i, 4u);
-        const float* p = a.part + j * a.I + i;
-        float s[4];
-        if constexpr (sizeof(E) == 1) {
-            int v[4] = {0, 0, 0, 0};
-            for (uint32_t k = 0; k < splits; ++k) {
-                const Pack<float, 4> x = load_some<4>(p + (uint64_t)k * a.J * a.I, n);
+        const auto join = [&](const float* p, float (&s)[4]) {
+            if constexpr (sizeof(E) == 1) {
+                int v[4] = {0, 0, 0, 0};
+                for (uint32_t k = 0; k < splits; ++k) {
+                    const Pack<float, 4> x = load_some<4>(p + (uint64_t)k * a.J * wide, n);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] += bits_as<int>(x.v[c]);
-            }
+                    for (int c = 0; c < 4; ++c) v[c] += bits_as<int>(x.v[c]);
+                }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[c] = (float)v[c];
-        } else {
+                for (int c = 0; c < 4; ++c) s[c] = (float)v[c];
+            } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[c] = 0.0f;
+                for (int c = 0; c < 4; ++c) s[c] = 0.0f;
 #pragma unroll 4
-            for (uint32_t k = 0; k < splits; ++k) {
-                const Pack<float, 4> x = load_some<4>(p + (uint64_t)k * a.J * a.I, n);
+                for (uint32_t k = 0; k < splits; ++k) {
+                    const Pack<float, 4> x = load_some<4>(p + (uint64_t)k * a.J * wide, n);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) s[c] += x.v[c];
+                    for (int c = 0; c < 4; ++c) s[c] += x.v[c];
+                }
             }
+        };
+        const float* p = a.part + j * wide + i;
+        float s[4];
+        join(p, s);
+        if constexpr (PAIR) {
+            float u[4];
+            join(p + a.I, u);
+            finish_pair<O, 4>(a.fin, PairColumns<O, 4>(a.fin, i, a.I, n), j, i, a.I, s, u, n);
+        } else {
+            finish<O, 4>(a.fin, Columns<O, 4>(a.fin, i, n), j, i, s, n);
         }
-        finish<O, 4>(a.fin, Columns<O, 4>(a.fin, i, n), j, i, s, n);
     }
 }
 
@@ -872,61 +1007,90 @@ __global__ __launch_bounds__(kBlock) void k_join(GemmArgs a, uint32_t splits) {
 // waves a share of k each, straight from memory, and joins their sums.  Bound
 // by reading P once.
 constexpr int kThinRows = 16, kThinWaves = 8, kThinDeep = 8;
-template <typename E, typename O>
+template <typename E, typename O, bool PAIR = false>
 __global__ __launch_bounds__(kThinWaves* kWave) void k_thin(GemmArgs a) {
     using M = Mma<E>;
-    __shared__ f4 lds[kThinWaves][kWave];
+    constexpr int H = PAIR ? 2 : 1;  // rows of P of a result
+    __shared__ f4 lds[H][kThinWaves][kWave];
     constexpr uint32_t CE = 16 / sizeof(E), KE = 4 * CE;  // k of one instruction
     const uint32_t wave = wave_index(), lane = lane_id();
     const uint32_t i0 = blockIdx.x * kThinRows;
     const E* p = (const E*)a.p + (uint64_t)min(i0 + lane % 16, a.I - 1) * a.p_stride + lane / 16 * CE;
     const E* q = (const E*)a.q + (uint64_t)min(lane % 16, a.J - 1) * a.q_stride + lane / 16 * CE;
+    const uint64_t apart = (uint64_t)a.I * a.p_stride;
     const uint32_t whole = a.K / KE, share = (whole + kThinWaves - 1) / kThinWaves;
     uint32_t s = min(wave * share, whole);
     const uint32_t end = min(s + share, whole);
-    typename M::Sum acc = {0, 0, 0, 0};
-    for (; s + kThinDeep <= end; s += kThinDeep) {
-        u4 x[kThinDeep], y[kThinDeep];
+    typename M::Sum acc[H];
 #pragma unroll
-        for (int d = 0; d < kThinDeep; ++d) x[d] = bits_as<u4>(load_pack<CE>(p + (uint64_t)(s + d) * KE));
+    for (int h = 0; h < H; ++h) acc[h] = typename M::Sum{0, 0, 0, 0};
+    for (; s + kThinDeep <= end; s += kThinDeep) {
+        u4 x[H][kThinDeep], y[kThinDeep];
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int d = 0; d < kThinDeep; ++d) x[h][d] = bits_as<u4>(load_pack<CE>(p + h * apart + (uint64_t)(s + d) * KE));
 #pragma unroll
         for (int d = 0; d < kThinDeep; ++d) y[d] = bits_as<u4>(load_pack<CE>(q + (uint64_t)(s + d) * KE));
 #pragma unroll
-        for (int d = 0; d < kThinDeep; ++d) acc = M::multiply(x[d], y[d], acc);
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int d = 0; d < kThinDeep; ++d) acc[h] = M::multiply(x[h][d], y[d], acc[h]);
     }
-    for (; s < end; ++s)
-        acc = M::multiply(bits_as<u4>(load_pack<CE>(p + (uint64_t)s * KE)), bits_as<u4>(load_pack<CE>(q + (uint64_t)s * KE)),
-                       acc);
+    for (; s < end; ++s) {
+        const u4 y = bits_as<u4>(load_pack<CE>(q + (uint64_t)s * KE));
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            acc[h] = M::multiply(bits_as<u4>(load_pack<CE>(p + h * apart + (uint64_t)s * KE)), y, acc[h]);
+    }
     if (wave == kThinWaves - 1 && whole * KE < a.K) {  // what is left of k
         const int have = (int)(a.K - whole * KE) - (int)(lane / 16 * CE);
-        acc = M::multiply(bits_as<u4>(load_some<CE>(p + (uint64_t)whole * KE, have)),
-                       bits_as<u4>(load_some<CE>(q + (uint64_t)whole * KE, have)), acc);
+        const u4 y = bits_as<u4>(load_some<CE>(q + (uint64_t)whole * KE, have));
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            acc[h] = M::multiply(bits_as<u4>(load_some<CE>(p + h * apart + (uint64_t)whole * KE, have)), y, acc[h]);
     }
-    lds[wave][lane] = bits_as<f4>(acc);
+#pragma unroll
+    for (int h = 0; h < H; ++h) lds[h][wave][lane] = bits_as<f4>(acc[h]);
     __syncthreads();
     if (wave != 0) return;
     const uint32_t i = i0 + lane / 16 * 4, j = lane % 16;
     if (i >= a.I || j >= a.J) return;
-    float v[4];
-    if constexpr (sizeof(E) == 1) {
-        int t[4] = {0, 0, 0, 0};
+    const auto join = [&](int h, float (&v)[4]) {
+        if constexpr (sizeof(E) == 1) {
+            int t[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < kThinWaves; ++w)
+            for (int w = 0; w < kThinWaves; ++w)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) t[c] += bits_as<int>(lds[w][lane][c]);
+                for (int c = 0; c < 4; ++c) t[c] += bits_as<int>(lds[h][w][lane][c]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = (float)t[c];
-    } else {
+            for (int c = 0; c < 4; ++c) v[c] = (float)t[c];
+        } else {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = 0.0f;
+            for (int c = 0; c < 4; ++c) v[c] = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kThinWaves; ++w)
+            for (int w = 0; w < kThinWaves; ++w)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] += lds[w][lane][c];
-    }
+                for (int c = 0; c < 4; ++c) v[c] += lds[h][w][lane][c];
+        }
+    };
     const int n = (int)min(a.I - i, 4u);
-    finish<O, 4>(a.fin, Columns<O, 4>(a.fin, i, n), j, i, v, n);
+    float v[4];
+    join(0, v);
+    if constexpr (PAIR) {
+        float u[4];
+        join(1, u);
+        finish_pair<O, 4>(a.fin, PairColumns<O, 4>(a.fin, i, a.I, n), j, i, a.I, v, u, n);
+    } else {
+        finish<O, 4>(a.fin, Columns<O, 4>(a.fin, i, n), j, i, v, n);
+    }
 }
+
+// Limits and scratch of the layers that take these products.
+constexpr uint64_t kLinearRoom = 8ull << 20;  // floats of partial sums of a product
+constexpr uint32_t kLinearMaxDim = 1u << 22, kLinearMaxInt8 = 1u << 17;
+constexpr uint64_t kLinearPad = 512ull << 20; // bytes of padded copies, at most
+constexpr uint32_t kBiasParts = 256;          // partial sums of the bias's gradient
 
 // Which operands lie across k.
 enum GemmForm { kAlong = 0, kPAcross = 1, kBothAcross = 2 };
@@ -949,6 +1113,10 @@ inline bool product_fits(uint64_t I, uint64_t J) {
 // One product that fits.  Operand types: E is O's type, or int8 with kAlong.
 template <typename E, typename O, int FORM>
 hipError_t launch_gemm(GemmArgs a, const GemmRoom& room, hipStream_t st);
+
+// One product of a gated layer, both operands along k: I results of 2 I rows of P, whose product_fits.
+template <typename E, typename O>
+hipError_t launch_gated(const GemmArgs& a, const GemmRoom& room, hipStream_t st);
 
 // The products of a layer's backward pass in its type T, each where it is given.
 template <typename T>

@@ -82,10 +82,10 @@ inline TilePlan plan_tiles(const TileCost& c, uint64_t I, uint64_t J, uint64_t s
     return best;
 }
 
-template <typename E, typename O, int FORM, typename TL>
+template <typename E, typename O, int FORM, typename TL, bool PAIR = false>
 hipError_t launch_tiles(GemmArgs a, uint64_t splits, bool direct, hipStream_t st) {
-    constexpr uint32_t KE = kStepBytes / sizeof(E);
-    a.tiles_i = (a.I + TL::BI - 1) / TL::BI;
+    constexpr uint32_t KE = kStepBytes / sizeof(E), kResults = PAIR ? TL::BI / 2 : TL::BI;
+    a.tiles_i = (a.I + kResults - 1) / kResults;
     a.tiles_j = (a.J + TL::BJ - 1) / TL::BJ;
     const uint64_t tiles = (uint64_t)a.tiles_i * a.tiles_j, steps = ((uint64_t)a.K + KE - 1) / KE;
     a.steps = (uint32_t)((steps + splits - 1) / splits);
@@ -94,27 +94,27 @@ hipError_t launch_tiles(GemmArgs a, uint64_t splits, bool direct, hipStream_t st
     if (splits == 1) a.part = nullptr;
     const dim3 grid((uint32_t)tiles, (uint32_t)splits);
     if constexpr (sizeof(E) <= 2) {
-        if (direct) k_gemm_fetch<E, O, FORM >= kPAcross, FORM == kBothAcross, TL><<<grid, dim3(TL::kThreads), 0, st>>>(a);
+        if (direct) k_gemm_fetch<E, O, FORM >= kPAcross, FORM == kBothAcross, TL, PAIR><<<grid, dim3(TL::kThreads), 0, st>>>(a);
     }
     if constexpr (TL::kThreads <= kBlock) {
-        if (!direct) k_gemm<E, O, FORM >= kPAcross, FORM == kBothAcross, TL><<<grid, dim3(TL::kThreads), 0, st>>>(a);
+        if (!direct) k_gemm<E, O, FORM >= kPAcross, FORM == kBothAcross, TL, PAIR><<<grid, dim3(TL::kThreads), 0, st>>>(a);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     a.part = part;
     const uint64_t threads = (uint64_t)((a.I + 3) / 4) * a.J;
-    k_join<E, O><<<dim3((uint32_t)std::min<uint64_t>((threads + kBlock - 1) / kBlock, 1u << 16)), dim3(kBlock), 0, st>>>(
+    k_join<E, O, PAIR><<<dim3((uint32_t)std::min<uint64_t>((threads + kBlock - 1) / kBlock, 1u << 16)), dim3(kBlock), 0, st>>>(
         a, (uint32_t)splits);
     return hipGetLastError();
 }
 
-// The tile (0 the smallest) and the split of k of a product.
+// The tile (0 the smallest) and the split of k of a product with I rows of P.
 struct Choice {
     int tile;
     uint32_t splits;
 };
 template <typename E, int FORM>
-Choice choose(const GemmArgs& a, bool direct, uint64_t room) {
+Choice choose(const GemmArgs& a, uint64_t I, bool direct, uint64_t room) {
     constexpr uint32_t KE = kStepBytes / sizeof(E);
     const uint64_t steps = ((uint64_t)a.K + KE - 1) / KE;
     TilePlan best{1e300, 1};
@@ -122,38 +122,40 @@ Choice choose(const GemmArgs& a, bool direct, uint64_t room) {
     constexpr TileCost kCosts[] = {kSmallCost, kMidCost, kWideCost, kLongCost, kBigCost};
     for (int t = 0; t < (direct ? 5 : 2); ++t) {  // the larger tiles take operands placed in LDS only
         if (FORM == kBothAcross && t == 3) continue;  // rows of 192 across k would not be a power of two in LDS
-        if (!kCosts[t].fits(a.I, a.J)) continue;
-        const TilePlan p = plan_tiles(kCosts[t], a.I, a.J, steps, room);
+        if (!kCosts[t].fits(I, a.J)) continue;
+        const TilePlan p = plan_tiles(kCosts[t], I, a.J, steps, room);
         if (p.us < best.us) best = p, tile = t;
     }
     return {tile, best.splits};
 }
 
-template <typename E, typename O, int FORM>
-hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
+template <typename E, typename O, int FORM, bool PAIR>
+hipError_t launch_product(GemmArgs a, const GemmRoom& given, hipStream_t st) {
+    static_assert(!PAIR || FORM == kAlong);
+    const uint32_t rows_of_p = PAIR ? 2 * a.I : a.I;
     if constexpr (FORM == kAlong)
         if (a.J <= (uint32_t)kThinRows) {
-            k_thin<E, O><<<dim3((a.I + kThinRows - 1) / kThinRows), dim3(kThinWaves * kWave), 0, st>>>(a);
+            k_thin<E, O, PAIR><<<dim3((a.I + kThinRows - 1) / kThinRows), dim3(kThinWaves * kWave), 0, st>>>(a);
             return hipGetLastError();
         }
     // 32 MB is what the dies' L2 hold together (8192 x 4096 x 4096 in bfloat16: 197 us stored past them, 213 through)
     a.fin.stream = (uint64_t)a.I * a.J * sizeof(O) >= 32ull << 20;
     bool direct = false;
     if constexpr (sizeof(E) <= 2) {
-        const uint64_t p_rows = FORM >= kPAcross ? a.K : a.I, q_rows = FORM == kBothAcross ? a.K : a.J;
+        const uint64_t p_rows = FORM >= kPAcross ? a.K : rows_of_p, q_rows = FORM == kBothAcross ? a.K : a.J;
         const uint32_t p_cols = FORM >= kPAcross ? a.I : a.K, q_cols = FORM == kBothAcross ? a.J : a.K;
         const bool p_whole = whole_chunks<E>(a.p, a.p_stride, p_cols), q_whole = whole_chunks<E>(a.q, a.q_stride, q_cols);
         direct = p_whole && q_whole;
         GemmRoom room = given;
-        if (!direct && room.pad && a.K && (double)a.I * a.J * a.K >= pad_work(FORM)) {
+        if (!direct && room.pad && a.K && (double)rows_of_p * a.J * a.K >= pad_work(FORM)) {
             GemmArgs b = a;
             direct = (p_whole || pad<E>(b.p, b.p_stride, p_rows, p_cols, room, st)) &&
                      (q_whole || pad<E>(b.q, b.q_stride, q_rows, q_cols, room, st));
             if (direct) a = b;
         }
     }
-    const Choice best = choose<E, FORM>(a, direct, given.floats);
-    const auto run = [&](auto tl) { return launch_tiles<E, O, FORM, decltype(tl)>(a, best.splits, direct, st); };
+    const Choice best = choose<E, FORM>(a, rows_of_p, direct, given.floats);
+    const auto run = [&](auto tl) { return launch_tiles<E, O, FORM, decltype(tl), PAIR>(a, best.splits, direct, st); };
     const int tile = best.tile;
     if constexpr (sizeof(E) <= 2) {
         if (tile == 4) return run(TileBig());
@@ -164,6 +166,15 @@ hipError_t launch_gemm(GemmArgs a, const GemmRoom& given, hipStream_t st) {
     return tile == 1 ? run(TileMid()) : run(TileSmall());
 }
 
+template <typename E, typename O, int FORM>
+hipError_t launch_gemm(GemmArgs a, const GemmRoom& room, hipStream_t st) {
+    return launch_product<E, O, FORM, false>(a, room, st);
+}
+template <typename E, typename O>
+hipError_t launch_gated(const GemmArgs& a, const GemmRoom& room, hipStream_t st) {
+    return launch_product<E, O, kAlong, true>(a, room, st);
+}
+
 // Both products in one launch, where each takes the smallest tile and does
 // not split k (40 x 784 x 512: 11.6 us in place of 15.0).
 template <typename T>
@@ -171,7 +182,7 @@ bool pair_backward(GemmArgs dx, GemmArgs dw, const GemmRoom& room, hipStream_t s
     const bool direct = sizeof(T) == 2 && whole_chunks<T>(dx.p, dx.p_stride, dx.I) &&
                         whole_chunks<T>(dx.q, dx.q_stride, dx.K) && whole_chunks<T>(dw.p, dw.p_stride, dw.I);
     if (!direct && room.pad && (double)dx.I * dx.J * dx.K >= pad_work(kBothAcross)) return false;
-    const Choice a = choose<T, kPAcross>(dx, direct, room.floats), b = choose<T, kBothAcross>(dw, direct, room.floats);
+    const Choice a = choose<T, kPAcross>(dx, dx.I, direct, room.floats), b = choose<T, kBothAcross>(dw, dw.I, direct, room.floats);
     if (a.tile || b.tile || a.splits > 1 || b.splits > 1) return false;
     uint64_t blocks = 0, first = 0;
     for (GemmArgs* g : {&dx, &dw}) {

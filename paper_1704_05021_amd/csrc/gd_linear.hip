@@ -9,35 +9,6 @@
 
 namespace gd {
 
-constexpr uint64_t kLinearRoom = 8ull << 20;  // floats of partial sums of a product
-constexpr uint32_t kLinearMaxDim = 1u << 22, kLinearMaxInt8 = 1u << 17;
-constexpr uint64_t kLinearPad = 512ull << 20; // bytes of padded copies, at most
-constexpr uint32_t kBiasParts = 256;          // partial sums of the bias's gradient
-
-// s act'(z) in place of s.  A choice of act is one branch for all of them: one
-// an element took longer than the memory.  ReLU chooses and does not multiply:
-// a unit that is off passes nothing, a gradient that is not finite neither.
-template <bool EXACT, int N>
-__device__ __forceinline__ void act_slope(int act, const float (&z)[N], float (&s)[N]) {
-    if (act == GD_ACT_RELU) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) s[j] = z[j] > 0.0f ? s[j] : 0.0f;
-    } else if (act == GD_ACT_GELU) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            float e;
-            const float cdf = normal<EXACT>(z[j], e);
-            s[j] *= cdf + z[j] * (e * 0.39894228040143268f);
-        }
-    } else if (act == GD_ACT_SILU) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float q = sigmoid<EXACT>(z[j]);
-            s[j] *= q * (1.0f + z[j] * (1.0f - q));
-        }
-    }
-}
-
 // dz = dy act'(pre), rounded, and its sums over the block's rows.  A wave takes
 // 512 columns of a row at a time, a lane 8; the block's waves take rows in
 // turn.  Bound by memory: 6 bytes an element in 16 bits.

@@ -61,6 +61,10 @@ EXPORTS = [
     "gd_embed_destroy",
     "gd_embed_forward",
     "gd_embed_backward",
+    "gd_gated_create",
+    "gd_gated_destroy",
+    "gd_gated_forward",
+    "gd_gated_backward",
     "gd_logprob_create",
     "gd_logprob_destroy",
     "gd_logprob_forward",
@@ -119,6 +123,11 @@ _EmbedIO = _struct("_EmbedIO", of=[(_u64, "rows"), (_vp, "tokens weight y"), (_u
                                    (_flt, "scale"), (_int, "index")])
 _EmbedGrad = _struct("_EmbedGrad", of=[(_u64, "rows"), (_vp, "tokens dy dweight"), (_u64, "dy_stride dweight_stride"),
                                        (_flt, "scale"), (_int, "index accumulate")])
+_GatedIO = _struct("_GatedIO", of=[(_u64, "rows"), (_vp, "x weight x_scale weight_scale bias y pre"),
+                                   (_u64, "x_stride weight_stride y_stride pre_stride")])
+_GatedGrad = _struct("_GatedGrad", of=[(_u64, "rows"), (_vp, "dy x weight pre dz dx dweight dbias"),
+                                       (_u64, "dy_stride x_stride weight_stride pre_stride dz_stride dx_stride "
+                                              "dweight_stride"), (_int, "accumulate")])
 _LogProbIO = _struct("_LogProbIO", of=[(_u64, "rows"), (_vp, "logits tokens logp entropy stats top_logp top_id"),
                                        (_u64, "stride"), (_flt, "scale"), (_int, "index"), (ctypes.c_uint32, "top")])
 _LogProbGrad = _struct("_LogProbGrad", of=[(_u64, "rows"), (_vp, "logits tokens dlogp dentropy stats entropy dlogits "
@@ -189,6 +198,7 @@ def _lib() -> ctypes.CDLL:
     for what, args in (("norm", [ctypes.POINTER(vp), u32, i32]), ("layernorm", [ctypes.POINTER(vp), u32, i32]),
                        ("embed", [ctypes.POINTER(vp), u32, u32, i32, u64]),
                        ("logprob", [ctypes.POINTER(vp), u32, i32, u64]), ("distill", [ctypes.POINTER(vp), u32, i32, u64]), ("linear", [ctypes.POINTER(vp), u32, u32, i32, i32, u64]),
+                       ("gated", [ctypes.POINTER(vp), u32, u32, i32, i32, u64]),
                        ("adamw", [ctypes.POINTER(vp), vp, u32, i32, vp])):
         create, destroy = getattr(lib, f"gd_{what}_create"), getattr(lib, f"gd_{what}_destroy")
         create.argtypes, create.restype = args, i32
@@ -196,6 +206,7 @@ def _lib() -> ctypes.CDLL:
     for name, io in (("gd_norm_forward", _NormIO), ("gd_norm_backward", _NormGrad), ("gd_adamw_step", _AdamWIO),
                      ("gd_layernorm_forward", _LayerNormIO), ("gd_layernorm_backward", _LayerNormGrad),
                      ("gd_embed_forward", _EmbedIO), ("gd_embed_backward", _EmbedGrad),
+                     ("gd_gated_forward", _GatedIO), ("gd_gated_backward", _GatedGrad),
                      ("gd_logprob_forward", _LogProbIO), ("gd_logprob_backward", _LogProbGrad),
                      ("gd_distill_forward", _DistillIO), ("gd_distill_backward", _DistillGrad),
                      ("gd_linear_forward", _LinearIO), ("gd_linear_backward", _LinearGrad)):
@@ -1063,6 +1074,120 @@ class Linear(_Handle):
             others["dz"] = span
         if dx and io.dx:
             _apart(size, "dx", (io.dx, rows, io.dx_stride, k), others)
+
+
+class GatedLinear(_Handle):
+    """A gated layer y = act(x Wg^T + bg) * (x Wu^T + bu) (gd_gated_*), weight [2 out, in] in ``dtype``: Wg's rows, then
+    Wu's; bias [2 out] likewise.
+
+    act: "none", "relu", "gelu" (by erf) or "silu".  The object holds the plan and scratch of calls of at most
+    ``max_rows`` rows, no weights; one object serves every layer of its shape on a stream.
+    """
+
+    _what = "gated"
+
+    def __init__(self, in_features: int, out_features: int, dtype: torch.dtype = torch.bfloat16, act: str = "silu",
+                 max_rows: int = 8192, device=None):
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, not {act!r}")
+        self.inf, self.outf, self.dtype, self.act = int(in_features), int(out_features), dtype, act
+        if not (0 < self.inf < 1 << 32 and 0 < self.outf < 1 << 32 and 0 <= int(max_rows) < 1 << 64):
+            raise GDError(1, "GatedLinear")
+        self._create(device, self.inf, self.outf, _dtype_code(dtype), ACTIVATIONS[act], int(max_rows))
+
+    def forward(self, x, weight, bias=None, out=None, keep_pre=False, stream=None):
+        """y, or (y, pre) with ``keep_pre`` (True, or a tensor [..., 2 out] to write): both sums for the backward."""
+        return self._run(x, weight, None, None, bias, out, keep_pre, stream)
+
+    def forward_int8(self, q, scale, weight_q, weight_scale, bias=None, out=None, stream=None):
+        """y in ``dtype`` from 8-bit operands: rows of x are q * scale[row], rows of weight weight_q *
+        weight_scale[row], codes in -127..127 (see quantise_rows and the norms' forward_int8)."""
+        return self._run(q, weight_q, scale, weight_scale, bias, out, False, stream)
+
+    def _run(self, x, weight, xs, ws, bias, out, keep_pre, stream):
+        kind, both = self.dtype if xs is None else torch.int8, 2 * self.outf
+        io = _GatedIO()
+        rows, io.x, io.x_stride = self._matrix(x, "x", kind, self.inf)
+        io.rows = rows
+        _, io.weight, io.weight_stride = self._matrix(weight, "weight", kind, self.inf, both)
+        if xs is not None:
+            io.x_scale = self._tensor(xs, "scale", torch.float32, rows)
+            io.weight_scale = self._tensor(ws, "weight_scale", torch.float32, both)
+        if bias is not None:
+            io.bias = self._tensor(bias, "bias", self.dtype, both)
+        given = out is not None
+        if not given:
+            out = _new(stream, x.new_empty, (*x.shape[:-1], self.outf), dtype=self.dtype)
+        _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.outf, rows)
+        pre = None
+        if keep_pre is not False:
+            pre = _new(stream, x.new_empty, (*x.shape[:-1], both), dtype=self.dtype) if keep_pre is True else keep_pre
+            _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, both, rows)
+        if rows and (given or (pre is not None and keep_pre is not True)):
+            k, n, size, others = self.inf, self.outf, self.dtype.itemsize, {}
+            if xs is None:
+                others = {"x": (io.x, rows, io.x_stride, k), "weight": (io.weight, both, io.weight_stride, k)}
+            if bias is not None:
+                others["bias"] = (io.bias, 1, both, both)
+            span = (io.y, rows, io.y_stride, n)
+            if given:
+                _apart(size, "out", span, others)
+            if pre is not None:
+                _apart(size, "pre", (io.pre, rows, io.pre_stride, both), {**others, "out": span})
+        if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                        (bias is not None and bias.requires_grad)):
+            raise _untracked()
+        st = _lib().gd_gated_forward(self._h, io, self._stream(stream, x, weight, xs, ws, bias, out, pre))
+        if st != 0:
+            raise GDError(st, "gd_gated_forward")
+        return out if pre is None else (out, pre)
+
+    def backward(self, dy, x, weight, pre, dx=None, dweight=None, dbias=None, dz=None, need_dx=True, need_dweight=True,
+                 accumulate=False, stream=None):
+        """(dx, dweight, dbias, dz); dweight and dbias in float32 (slices of a flat gradient, say).
+
+        dbias: a tensor to write, True for a new one, or None for a layer without a bias.
+        dz [..., 2 out] in ``dtype`` is the gradient of both sums that the products take; it may be pre.  None for what
+        is not needed.
+        """
+        given_dz, given_dx, both = dz is not None, dx is not None, 2 * self.outf
+        io = _GatedGrad(accumulate=int(accumulate))
+        rows, io.dy, io.dy_stride = self._matrix(dy, "dy", self.dtype, self.outf)
+        io.rows = rows
+        _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, both, rows)
+        if not given_dz:
+            dz = _new(stream, torch.empty_like, pre, memory_format=torch.contiguous_format)
+        _, io.dz, io.dz_stride = self._matrix(dz, "dz", self.dtype, both, rows)
+        if need_dx:
+            _, io.weight, io.weight_stride = self._matrix(weight, "weight", self.dtype, self.inf, both)
+            if dx is None:
+                dx = _new(stream, dy.new_empty, (*dy.shape[:-1], self.inf))
+            _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.inf, rows)
+        else:
+            dx = None
+        if need_dweight:
+            _, io.x, io.x_stride = self._matrix(x, "x", self.dtype, self.inf, rows)
+            dweight = _gradient(dweight, accumulate, (both, self.inf), self.device, stream)
+            _, io.dweight, io.dweight_stride = self._matrix(dweight, "dweight", torch.float32, self.inf, both)
+        else:
+            dweight = None
+        if dbias is not None:
+            dbias = _gradient(None if dbias is True else dbias, accumulate, (both,), self.device, stream)
+            io.dbias = self._tensor(dbias, "dbias", torch.float32, both)
+        if rows and (given_dz or given_dx):
+            k, n, size = self.inf, self.outf, self.dtype.itemsize
+            others = {"dy": (io.dy, rows, io.dy_stride, n), "x": (io.x, rows, io.x_stride, k),
+                      "weight": (io.weight, both, io.weight_stride, k), "pre": (io.pre, rows, io.pre_stride, both)}
+            others = {name: span for name, span in others.items() if span[0]}  # what the call was given
+            span = (io.dz, rows, io.dz_stride, both)
+            if given_dz:
+                _apart(size, "dz", span, others, ("pre",))
+            if given_dx and dx is not None:
+                _apart(size, "dx", (io.dx, rows, io.dx_stride, k), {**others, "dz": span})
+        st = _lib().gd_gated_backward(self._h, io, self._stream(stream, dy, x, weight, pre, dz, dx, dweight, dbias))
+        if st != 0:
+            raise GDError(st, "gd_gated_backward")
+        return dx, dweight, dbias, dz
 
 
 @dataclass
