@@ -47,6 +47,13 @@ __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.
 constexpr float kFar = -200.0f;
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
+// The largest of three, NaN left out.  (Of fmaxf the compiler makes three instructions for a pair: it quiets both first.)
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 template <int CTRL, int MASK>
 __device__ __forceinline__ float dpp_f32(float v, float none) {
     return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL, MASK, 0xF, false));
@@ -155,13 +162,44 @@ struct Vec {
     }
 };
 
+// A thread's vectors of a row or a piece, t, t + ROW and so on, kScoreDeep of them at a time and the next ones on their
+// way: whole(raw, v) where all are whole, last(raw, v) for what is left.
+template <typename T, int ROW, typename Whole, typename Last>
+__device__ __forceinline__ void walk(const T* x, uint32_t t, uint32_t n, Whole whole, Last last) {
+    const uint32_t vecs = (n + 7) / 8, full = n / 8;
+    constexpr uint32_t kTurn = ROW * kScoreDeep;
+    Pack<T, 8> raw[kScoreDeep], next[kScoreDeep];
+    uint32_t v = t;
+    const auto fits = [&](uint32_t v) { return v + (kScoreDeep - 1) * ROW < full; };
+    if (fits(v)) {
+#pragma unroll
+        for (int k = 0; k < kScoreDeep; ++k) next[k] = load_pack<8>(x + (v + k * ROW) * 8);
+        do {
+#pragma unroll
+            for (int k = 0; k < kScoreDeep; ++k) raw[k] = next[k];
+            // past the end the first ones again: no load waits for a condition
+            const uint32_t ahead = fits(v + kTurn) ? v + kTurn : t;
+#pragma unroll
+            for (int k = 0; k < kScoreDeep; ++k) next[k] = load_pack<8>(x + (ahead + k * ROW) * 8);
+            whole(raw, v);
+            v += kTurn;
+        } while (fits(v));
+    }
+    if (v < vecs) {
+#pragma unroll
+        for (int k = 0; k < kScoreDeep; ++k) raw[k] = Vec(v + k * ROW, vecs, n).load(x, n);
+        last(raw, v);
+    }
+}
+
 // What the gradient at an element takes: dz = p (c + e (log p + H)), both with the scale in them.
 struct Slope {
-    float m, log_s, c, e, entropy;
+    float m, log_s, c, e, entropy, c_s;  // c_s: c over the sum of exp(z - m)
+    __device__ __forceinline__ float plain(float x, float scale) const { return exp_fast(fmaf(x, scale, -m)) * c_s; }
     __device__ __forceinline__ float at(float x, float scale) const {
+        if (e == 0.0f) return plain(x, scale);
         const float lp = fmaf(x, scale, -m) - log_s;  // log p
-        const float p = exp_fast(lp);
-        return e == 0.0f ? p * c : p * fmaf(e, fmaxf(lp, kFar) + entropy, c);
+        return exp_fast(lp) * fmaf(e, fmaxf(lp, kFar) + entropy, c);
     }
 };
 
@@ -359,40 +397,52 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
 
     Soft soft{-INFINITY, 0.0f, 0.0f};
     uint32_t best = 0;  // the thread's largest element
-    if (stats && !skip)
-        for (uint32_t v = t; v < vecs; v += S::kRow * kScoreDeep) {
-            Pack<T, 8> raw[kScoreDeep];
+    if (stats && !skip) {
+        const auto add = [&](const float (&z)[kScoreDeep][8]) {
+            float big = -INFINITY;
 #pragma unroll
-            for (int k = 0; k < kScoreDeep; ++k) raw[k] = Vec(v + k * S::kRow, vecs, n).load(x, n);
-            float big = soft.m, z[kScoreDeep][8];
+            for (int k = 0; k < kScoreDeep; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    big = max_of(big, z[k][j], z[k][j + 1]);
+                    if (KIND == kTop) best = max(best, max(order_of(z[k][j]), order_of(z[k][j + 1])));
+                }
+            big = fmaxf(soft.m, big * scale);
+            const float to = reference(big), f = exp_fast(soft.m - to);
+            float p[kScoreDeep] = {}, tt[kScoreDeep] = {};  // sums of a few, side by side
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < kScoreDeep; ++k) {
+                    const float d = fmaf(z[k][j], scale, -to), e = exp_fast(d);
+                    p[k] += e;
+                    if (entropy) tt[k] = fmaf(e, fmaxf(d, kFar), tt[k]);
+                }
+            float ps = 0.0f, ts = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kScoreDeep; ++k) ps += p[k], ts += tt[k];
+            if (entropy) soft.t = f * (soft.t + soft.s * fmaxf(reference(soft.m) - to, kFar)) + ts;
+            soft.s = fmaf(f, soft.s, ps);
+            soft.m = big;
+        };
+        walk<T, S::kRow>(x, t, n, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t) {
+            float z[kScoreDeep][8];
+#pragma unroll
+            for (int k = 0; k < kScoreDeep; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[k][j] = (float)raw[k].v[j];
+            add(z);
+        }, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t v) {
+            float z[kScoreDeep][8];
 #pragma unroll
             for (int k = 0; k < kScoreDeep; ++k) {
                 const uint32_t mine = Vec(v + k * S::kRow, vecs, n).mine;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[k][j] = (float)raw[k].v[j];
-                if (mine != 0xFF)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) z[k][j] = mine >> j & 1 ? z[k][j] : -INFINITY;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) big = fmaxf(big, z[k][j] * scale);
-                if (KIND == kTop)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) best = max(best, order_of(z[k][j]));
+                for (int j = 0; j < 8; ++j) z[k][j] = mine >> j & 1 ? (float)raw[k].v[j] : -INFINITY;
             }
-            const float to = reference(big), f = exp_fast(soft.m - to);
-            float s = 0.0f, tt = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kScoreDeep; ++k)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = fmaf(z[k][j], scale, -to), p = exp_fast(d);
-                    s += p;
-                    if (entropy) tt = fmaf(p, fmaxf(d, kFar), tt);
-                }
-            soft.t = f * (soft.t + soft.s * fmaxf(reference(soft.m) - to, kFar)) + tt;
-            soft.s = fmaf(f, soft.s, s);
-            soft.m = big;
-        }
+            add(z);
+        });
+    }
     if (stats) soft = row_soft<WAVES>(soft, lds_soft);
     if (TEACHER || GRAD) __syncthreads();
 
@@ -432,21 +482,25 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
         sl.entropy = stats ? sl.log_s - soft.t / soft.s : a.given_entropy ? a.given_entropy[row] : 0.0f;
         sl.c = held == 0.0f ? 0.0f : (TEACHER ? g : -g) * held * scale;
         sl.e = e;
+        sl.c_s = sl.c / (stats ? soft.s : expf(sl.log_s));
         T* d = (T*)a.dlogits + row * a.dstride + begin;
         // a row that no gradient comes down to has none, whatever it holds, nor has one of which every logit is minus infinity
         const bool zeros = (sl.c == 0.0f && sl.e == 0.0f) || (sl.m == -INFINITY && sl.log_s == -INFINITY);
-        if (on)
-            for (uint32_t v = t; v < vecs; v += S::kRow * kScoreDeep) {
-                Pack<T, 8> raw[kScoreDeep];
-                if (!zeros)
+        const auto write = [&](auto value) {  // of an element
+            const auto of = [&](const Pack<T, 8>& raw) {
+                Pack<T, 8> y;
 #pragma unroll
-                    for (int k = 0; k < kScoreDeep; ++k) raw[k] = Vec(v + k * S::kRow, vecs, n).load(x, n);
+                for (int j = 0; j < 8; ++j) y.v[j] = (T)value((float)raw.v[j]);
+                return y;
+            };
+            walk<T, S::kRow>(x, t, n, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t v) {
+#pragma unroll
+                for (int k = 0; k < kScoreDeep; ++k) store_stream<8>(d + (v + k * S::kRow) * 8, of(raw[k]), 8);
+            }, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t v) {
 #pragma unroll
                 for (int k = 0; k < kScoreDeep; ++k) {
                     const Vec p(v + k * S::kRow, vecs, n);
-                    Pack<T, 8> y;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y.v[j] = (T)(zeros ? 0.0f : sl.at((float)raw[k].v[j], scale));
+                    const Pack<T, 8> y = of(raw[k]);
                     if (p.mine == 0xFF)
                         store_stream<8>(d + p.at, y, 8);
                     else
@@ -454,7 +508,15 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
                         for (int j = 0; j < 8; ++j)
                             if (p.mine >> j & 1) d[p.at + j] = y.v[j];
                 }
-            }
+            });
+        };
+        if (on && zeros) {
+            for (uint32_t v = t; v < vecs; v += S::kRow) store_stream<8>(d + v * 8, Pack<T, 8>{}, (int)(n - v * 8));
+        } else if (on && sl.e == 0.0f) {
+            write([&](float v) { return sl.plain(v, scale); });
+        } else if (on) {
+            write([&](float v) { return sl.at(v, scale); });
+        }
         // the elements that are named are written anew, with their weights in them and rounded once, behind the others
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();

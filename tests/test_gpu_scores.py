@@ -166,8 +166,10 @@ def test_masks(kind, rows, vocab):
         for dh in (None, h):
             dx = op.backward(y, tokens, g, dh, scores=r)
             check_gradient(dx, y, tokens, g, dh, 1.0, "masked")
-            assert not bool(dx[0].any()) and torch.equal(dx, op.forward_backward(y, tokens, g, dh)[1]) or rows < 256
-            check_gradient(op.forward_backward(y, tokens, g, dh)[1], y, tokens, g, dh, 1.0, "masked")
+            # not the same bits: the one takes the sum of a row, the other the exponential of its log, as rounded
+            again = op.forward_backward(y, tokens, g, dh)[1]
+            check_gradient(again, y, tokens, g, dh, 1.0, "masked")
+            assert not bool(dx[0].any() or again[0].any())
 
 
 @pytest.mark.parametrize("rows,vocab", [(3, 30), (3, 2048), (2, 5000), (300, 9000), (2, 40_000)])
