@@ -36,7 +36,7 @@ constexpr uint32_t kScorePiece = 4096;       // elements of a piece, at least
 constexpr uint32_t kScoreMaxPieces = 64;     // a lane each where they are joined
 constexpr uint32_t kScoreTopRoom = 1024;     // alternatives that a row's pieces name, at most
 constexpr uint32_t kListRoom = 1024;         // elements that a row's list holds; a row of more is looked through K times
-constexpr int kScoreDeep = 4;                // vectors of a thread on their way at once
+constexpr int kScoreDeep = 2;                // vectors of a thread in a turn; the next turn's are on their way meanwhile
 
 // A share of a row: the largest z, and relative to it the sums of exp(z) and of exp(z) z.
 struct Soft {
@@ -162,42 +162,46 @@ struct Vec {
     }
 };
 
-// A thread's vectors of a row or a piece, t, t + ROW and so on, kScoreDeep of them at a time and the next ones on their
-// way: whole(raw, v) where all are whole, last(raw, v) for what is left.
-template <typename T, int ROW, typename Whole, typename Last>
-__device__ __forceinline__ void walk(const T* x, uint32_t t, uint32_t n, Whole whole, Last last) {
-    const uint32_t vecs = (n + 7) / 8, full = n / 8;
-    constexpr uint32_t kTurn = ROW * kScoreDeep;
-    Pack<T, 8> raw[kScoreDeep], next[kScoreDeep];
-    uint32_t v = t;
-    const auto fits = [&](uint32_t v) { return v + (kScoreDeep - 1) * ROW < full; };
-    if (fits(v)) {
+// A row or a piece in turns of kScoreDeep vectors a thread: `whole` of them, in which every vector is, and what is left.
+template <typename T, int ROW>
+struct Turns {
+    typedef Pack<T, 8> Turn[kScoreDeep];
+    static constexpr uint32_t kVectors = ROW * kScoreDeep;
+    const T* x;
+    uint32_t t, n, vecs, whole;
+    __device__ __forceinline__ Turns(const T* x, uint32_t t, uint32_t n) : x(x), t(t), n(n), vecs((n + 7) / 8), whole(n / (kVectors * 8)) {}
+    __device__ __forceinline__ uint32_t vector(uint32_t turn, int k) const { return turn * kVectors + k * ROW + t; }
+    __device__ __forceinline__ void load(Turn& raw, uint32_t turn) const {
 #pragma unroll
-        for (int k = 0; k < kScoreDeep; ++k) next[k] = load_pack<8>(x + (v + k * ROW) * 8);
-        do {
+        for (int k = 0; k < kScoreDeep; ++k) raw[k] = load_pack<8>(x + vector(turn, k) * 8);
+    }
+    __device__ __forceinline__ bool left() const { return whole * kVectors * 8 < n; }
+    __device__ __forceinline__ Vec left_vec(int k) const { return Vec(vector(whole, k), vecs, n); }
+    __device__ __forceinline__ void load_left(Turn& raw) const {
+#pragma unroll
+        for (int k = 0; k < kScoreDeep; ++k) raw[k] = left_vec(k).load(x, n);
+    }
+    // each(raw, turn) for the whole turns from `first` on, the next one's loads on their way meanwhile
+    template <typename Each>
+    __device__ __forceinline__ void walk(uint32_t first, Each each) const {
+        if (first >= whole) return;
+        Turn raw, next;
+        load(next, first);
+#pragma unroll 1
+        for (uint32_t i = first; i < whole; ++i) {
 #pragma unroll
             for (int k = 0; k < kScoreDeep; ++k) raw[k] = next[k];
-            // past the end the first ones again: no load waits for a condition
-            const uint32_t ahead = fits(v + kTurn) ? v + kTurn : t;
-#pragma unroll
-            for (int k = 0; k < kScoreDeep; ++k) next[k] = load_pack<8>(x + (ahead + k * ROW) * 8);
-            whole(raw, v);
-            v += kTurn;
-        } while (fits(v));
+            if (i + 1 < whole) load(next, i + 1);
+            each(raw, i);
+        }
     }
-    if (v < vecs) {
-#pragma unroll
-        for (int k = 0; k < kScoreDeep; ++k) raw[k] = Vec(v + k * ROW, vecs, n).load(x, n);
-        last(raw, v);
-    }
-}
+};
 
 // What the gradient at an element takes: dz = p (c + e (log p + H)), both with the scale in them.
 struct Slope {
     float m, log_s, c, e, entropy, c_s;  // c_s: c over the sum of exp(z - m)
     __device__ __forceinline__ float plain(float x, float scale) const { return exp_fast(fmaf(x, scale, -m)) * c_s; }
     __device__ __forceinline__ float at(float x, float scale) const {
-        if (e == 0.0f) return plain(x, scale);
         const float lp = fmaf(x, scale, -m) - log_s;  // log p
         return exp_fast(lp) * fmaf(e, fmaxf(lp, kFar) + entropy, c);
     }
@@ -288,12 +292,14 @@ struct Alternatives {
     uint32_t group[S::kThreads / kWave][kWave], bound[S::kRows], n[S::kRows];
     uint64_t list[S::kRows][kListRoom], best[S::kThreads / kWave];
 
+    // largest: this thread's, NaN left out.  odd: the row holds a NaN or plus infinity.
     template <typename Put>
-    __device__ __forceinline__ void find(const T* x, uint32_t begin, uint32_t len, uint32_t K, uint32_t largest, bool on, Put put) {
-        const uint32_t t = threadIdx.x % S::kRow, r = threadIdx.x / S::kRow, vecs = (len + 7) / 8;
+    __device__ __forceinline__ void find(const T* x, uint32_t begin, uint32_t len, uint32_t K, float largest, bool on, bool odd,
+                                         Put put) {
+        const uint32_t t = threadIdx.x % S::kRow, r = threadIdx.x / S::kRow;
         const uint32_t wave = wave_index(), wave0 = wave / WAVES * WAVES;
         // the bound: the K-th largest of 64 groups of threads
-        group[wave][lane_id()] = largest;
+        group[wave][lane_id()] = order_of(largest);
         if (t == 0) n[r] = 0;
         __syncthreads();
         if (t < (uint32_t)kWave) {
@@ -308,28 +314,38 @@ struct Alternatives {
             if (before == K - 1) bound[r] = mine;
         }
         __syncthreads();
-        const uint32_t least = bound[r];
-        if (on)
-            for (uint32_t v = t; v < vecs; v += S::kRow * kScoreDeep) {
-                Pack<T, 8> raw[kScoreDeep];
+        const float least = value_of(bound[r]);
+        const Turns<T, S::kRow> turns(x, t, len);
+        // one look a vector: hardly any holds an element that reaches the bound
+        const auto look = [&](const Pack<T, 8>& raw, uint32_t at, uint32_t mine) {
+            float v[8], top = -INFINITY;
 #pragma unroll
-                for (int k = 0; k < kScoreDeep; ++k) raw[k] = Vec(v + k * S::kRow, vecs, len).load(x, len);
+            for (int j = 0; j < 8; ++j) v[j] = (float)raw.v[j];
 #pragma unroll
-                for (int k = 0; k < kScoreDeep; ++k) {
-                    const Vec p(v + k * S::kRow, vecs, len);
+            for (int j = 0; j < 8; j += 2) top = max_of(top, v[j], v[j + 1]);
+            if (!(top >= least)) return;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t o = order_of((float)raw[k].v[j]);
-                        if (o >= least && p.mine >> j & 1) {
-                            const uint32_t place = atomicAdd(&n[r], 1u);
-                            if (place < kListRoom) list[r][place] = key_of_element(o, begin + p.at + j);
-                        }
-                    }
+            for (int j = 0; j < 8; ++j)
+                if (v[j] >= least && mine >> j & 1) {
+                    const uint32_t place = atomicAdd(&n[r], 1u);
+                    if (place < kListRoom) list[r][place] = key_of_element(order_of(v[j]), begin + at + j);
                 }
+        };
+        if (on && !odd) {
+            turns.walk(0, [&](const typename Turns<T, S::kRow>::Turn& raw, uint32_t turn) {
+#pragma unroll
+                for (int k = 0; k < kScoreDeep; ++k) look(raw[k], turns.vector(turn, k) * 8, 0xFF);
+            });
+            if (turns.left()) {
+                typename Turns<T, S::kRow>::Turn raw;
+                turns.load_left(raw);
+#pragma unroll
+                for (int k = 0; k < kScoreDeep; ++k) look(raw[k], turns.left_vec(k).at, turns.left_vec(k).mine);
             }
+        }
         __syncthreads();
         const uint32_t listed = n[r];
-        if (listed <= kListRoom) {
+        if (!odd && listed <= kListRoom) {
             if (!on) return;
             for (uint32_t i = t; i < listed; i += S::kRow) {
                 const uint64_t key = list[r][i];
@@ -340,7 +356,8 @@ struct Alternatives {
             for (uint32_t k = len + t; k < K; k += S::kRow) put(k, 0);  // a piece of fewer elements than K
             return;
         }
-        // more elements reach the bound than the list holds (a row of equal ones): the next largest, K times
+        // more elements reach the bound than the list holds (a row of equal ones), or not all are in order: the next
+        // largest, K times
         uint64_t last = ~0ull;
         for (uint32_t k = 0; k < K; ++k) {
             uint64_t most = 0;
@@ -364,14 +381,14 @@ struct Alternatives {
 };
 struct Nothing {};
 
-enum ScoreKind { kSums = 0, kTop = 1, kGrad = 2 };
-template <typename T, int WAVES, int KIND, bool TEACHER>
+enum ScoreKind { kSums = 0, kTop = 1, kGrad = 2, kGradEntropy = 3 };  // kGrad: no entropy is asked for, nor its gradient given
+template <typename T, int WAVES, int KIND, bool TEACHER, int HELD = 0>
 __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs a, uint32_t first_unit) {
     using S = NormShape<WAVES>;
     __shared__ Soft lds_soft[S::kThreads / kWave];
     __shared__ std::conditional_t<TEACHER, Named, Nothing> named[S::kRows];
     __shared__ std::conditional_t<KIND == kTop, Alternatives<T, WAVES>, Nothing> top;
-    static_assert(WAVES == 1 || S::kRows == 1);
+    static_assert(WAVES == 1 || S::kRows == 1);  // barriers are a row's own
     const uint32_t t = threadIdx.x % S::kRow, r = threadIdx.x / S::kRow, units = (uint32_t)a.rows * a.pieces;
     const bool on = blockIdx.x * S::kRows + r < units - first_unit;
     const uint32_t unit = on ? first_unit + blockIdx.x * S::kRows + r : units - 1;
@@ -379,7 +396,7 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
     const uint64_t row = unit / a.pieces;
     const T* x = (const T*)a.logits + row * a.stride + begin;
     const float scale = a.scale;
-    constexpr bool GRAD = KIND == kGrad;
+    constexpr bool GRAD = KIND >= kGrad;
 
     // the token and its logit, read before anything is written over it; a teacher's by the row's first wave
     int64_t token = -1;
@@ -390,24 +407,34 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
         token = id_at(a, row, 0);
         if (token >= 0) token_x = (float)((const T*)a.logits + row * a.stride)[token];
     }
-    const float g = GRAD ? a.g[row] : 0.0f, e = GRAD && a.h ? -a.h[row] * scale : 0.0f;
-    const bool stats = !GRAD || !a.given, entropy = a.entropy || (GRAD && a.h);
+    const float g = GRAD ? a.g[row] : 0.0f, e = KIND == kGradEntropy && a.h ? -a.h[row] * scale : 0.0f;
+    const bool stats = !GRAD || !a.given, entropy = KIND == kGradEntropy || (!GRAD && a.entropy);
     // padding with nothing to say of it: its logits are not read
     const bool skip = GRAD && !TEACHER && token < 0 && e == 0.0f && !a.entropy;
 
+    // The gradient's launch holds the row's first turns (HELD over the bytes of an element) and its last in registers
+    // between its two passes, and reads the others twice.
+    const Turns<T, S::kRow> turns(x, t, n);
+    typedef typename Turns<T, S::kRow>::Turn Turn;
+    constexpr int kHeld = GRAD ? HELD / (int)sizeof(T) : 0;
+    Turn kept[kHeld > 0 ? kHeld : 1], last;
+    const uint32_t held_turns = min((uint32_t)kHeld, turns.whole);
+    if (!skip) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (i < (int)held_turns) turns.load(kept[i], i);
+        if (turns.left()) turns.load_left(last);
+    }
+
     Soft soft{-INFINITY, 0.0f, 0.0f};
-    uint32_t best = 0;  // the thread's largest element
+    float most = -INFINITY;  // the thread's largest logit
     if (stats && !skip) {
         const auto add = [&](const float (&z)[kScoreDeep][8]) {
-            float big = -INFINITY;
 #pragma unroll
             for (int k = 0; k < kScoreDeep; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    big = max_of(big, z[k][j], z[k][j + 1]);
-                    if (KIND == kTop) best = max(best, max(order_of(z[k][j]), order_of(z[k][j + 1])));
-                }
-            big = fmaxf(soft.m, big * scale);
+                for (int j = 0; j < 8; j += 2) most = max_of(most, z[k][j], z[k][j + 1]);
+            const float big = most * scale;
             const float to = reference(big), f = exp_fast(soft.m - to);
             float p[kScoreDeep] = {}, tt[kScoreDeep] = {};  // sums of a few, side by side
 #pragma unroll
@@ -425,23 +452,28 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
             soft.s = fmaf(f, soft.s, ps);
             soft.m = big;
         };
-        walk<T, S::kRow>(x, t, n, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t) {
+        const auto add_whole = [&](const Turn& raw, uint32_t) {
             float z[kScoreDeep][8];
 #pragma unroll
             for (int k = 0; k < kScoreDeep; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) z[k][j] = (float)raw[k].v[j];
             add(z);
-        }, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t v) {
+        };
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (i < (int)held_turns) add_whole(kept[i], i);
+        turns.walk(held_turns, add_whole);
+        if (turns.left()) {
             float z[kScoreDeep][8];
 #pragma unroll
             for (int k = 0; k < kScoreDeep; ++k) {
-                const uint32_t mine = Vec(v + k * S::kRow, vecs, n).mine;
+                const uint32_t mine = turns.left_vec(k).mine;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[k][j] = mine >> j & 1 ? (float)raw[k].v[j] : -INFINITY;
+                for (int j = 0; j < 8; ++j) z[k][j] = mine >> j & 1 ? (float)last[k].v[j] : -INFINITY;
             }
             add(z);
-        });
+        }
     }
     if (stats) soft = row_soft<WAVES>(soft, lds_soft);
     if (TEACHER || GRAD) __syncthreads();
@@ -464,7 +496,7 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
     if constexpr (KIND == kTop) {
         const uint32_t K = a.top;
         const float log_s = logf(soft.s);
-        top.find(x, begin, n, K, best, on, [&](uint32_t rank, uint64_t key) {
+        top.find(x, begin, n, K, most, on, soft.s != soft.s, [&](uint32_t rank, uint64_t key) {
             if (!on) return;
             if (a.pieces > 1) {
                 a.part_key[(uint64_t)unit * K + rank] = key;
@@ -493,29 +525,34 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
                 for (int j = 0; j < 8; ++j) y.v[j] = (T)value((float)raw.v[j]);
                 return y;
             };
-            walk<T, S::kRow>(x, t, n, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t v) {
+            const auto write_whole = [&](const Turn& raw, uint32_t turn) {
 #pragma unroll
-                for (int k = 0; k < kScoreDeep; ++k) store_stream<8>(d + (v + k * S::kRow) * 8, of(raw[k]), 8);
-            }, [&](const Pack<T, 8> (&raw)[kScoreDeep], uint32_t v) {
+                for (int k = 0; k < kScoreDeep; ++k) store_stream<8>(d + turns.vector(turn, k) * 8, of(raw[k]), 8);
+            };
 #pragma unroll
-                for (int k = 0; k < kScoreDeep; ++k) {
-                    const Vec p(v + k * S::kRow, vecs, n);
-                    const Pack<T, 8> y = of(raw[k]);
-                    if (p.mine == 0xFF)
-                        store_stream<8>(d + p.at, y, 8);
-                    else
+            for (int i = 0; i < kHeld; ++i)
+                if (i < (int)held_turns) write_whole(kept[i], i);
+            turns.walk(held_turns, write_whole);
+            if (!turns.left()) return;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (p.mine >> j & 1) d[p.at + j] = y.v[j];
-                }
-            });
+            for (int k = 0; k < kScoreDeep; ++k) {
+                const Vec p = turns.left_vec(k);
+                const Pack<T, 8> y = of(last[k]);
+                if (p.mine == 0xFF)
+                    store_stream<8>(d + p.at, y, 8);
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (p.mine >> j & 1) d[p.at + j] = y.v[j];
+            }
         };
         if (on && zeros) {
             for (uint32_t v = t; v < vecs; v += S::kRow) store_stream<8>(d + v * 8, Pack<T, 8>{}, (int)(n - v * 8));
-        } else if (on && sl.e == 0.0f) {
-            write([&](float v) { return sl.plain(v, scale); });
         } else if (on) {
-            write([&](float v) { return sl.at(v, scale); });
+            if constexpr (KIND == kGradEntropy)
+                write([&](float v) { return sl.at(v, scale); });
+            else
+                write([&](float v) { return sl.plain(v, scale); });
         }
         // the elements that are named are written anew, with their weights in them and rounded once, behind the others
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -533,10 +570,10 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
                         first = first && k >= j;
                         w += q.w[k];
                     }
-                if (first) d[id] = (T)(sl.at(q.x[j], scale) - g * w * scale);
+                if (first) d[id] = (T)(sl.plain(q.x[j], scale) - g * w * scale);
             }
         } else if (t == 0 && token >= 0 && (uint64_t)token - begin < n) {
-            d[(uint64_t)token - begin] = (T)(sl.at(token_x, scale) + g * scale);
+            d[(uint64_t)token - begin] = (T)((KIND == kGradEntropy ? sl.at(token_x, scale) : sl.plain(token_x, scale)) + g * scale);
         }
     }
 }
@@ -575,36 +612,57 @@ __global__ __launch_bounds__(kScoreJoinThreads) void k_score_join(ScoreArgs a) {
     }
 }
 
-template <typename T, int WAVES>
-hipError_t launch_score_shape(const ScoreArgs& a, bool grad, hipStream_t st) {
+// Calls f(grid, first unit) until all units are covered: a dispatch holds less than 2^32 threads.
+template <int WAVES, typename F>
+hipError_t over_units(const ScoreArgs& a, F f) {
     using S = NormShape<WAVES>;
     const uint32_t units = (uint32_t)a.rows * a.pieces;
-    constexpr uint32_t kMost = 1u << 22;  // units of a launch: a dispatch holds less than 2^32 threads
+    constexpr uint32_t kMost = 1u << 22;
     for (uint32_t first = 0; first < units; first += std::min(units - first, kMost)) {
-        const dim3 grid((std::min(units - first, kMost) + S::kRows - 1) / S::kRows), block(S::kThreads);
-        if (a.teacher) {
-            if (grad)
-                k_score<T, WAVES, kGrad, true><<<grid, block, 0, st>>>(a, first);
-            else
-                k_score<T, WAVES, kSums, true><<<grid, block, 0, st>>>(a, first);
-        } else if (grad) {
-            k_score<T, WAVES, kGrad, false><<<grid, block, 0, st>>>(a, first);
-        } else if (a.top) {
-            k_score<T, WAVES, kTop, false><<<grid, block, 0, st>>>(a, first);
-        } else {
-            k_score<T, WAVES, kSums, false><<<grid, block, 0, st>>>(a, first);
-        }
+        f(dim3((std::min(units - first, kMost) + S::kRows - 1) / S::kRows), dim3(S::kThreads), first);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
+template <typename T, int WAVES>
+hipError_t launch_sums(const ScoreArgs& a, hipStream_t st) {
+    return over_units<WAVES>(a, [&](dim3 grid, dim3 block, uint32_t first) {
+        if (a.teacher)
+            k_score<T, WAVES, kSums, true><<<grid, block, 0, st>>>(a, first);
+        else if (a.top)
+            k_score<T, WAVES, kTop, false><<<grid, block, 0, st>>>(a, first);
+        else
+            k_score<T, WAVES, kSums, false><<<grid, block, 0, st>>>(a, first);
+    });
+}
+template <typename T, int WAVES, int HELD>
+hipError_t launch_gradient(const ScoreArgs& a, hipStream_t st) {
+    return over_units<WAVES>(a, [&](dim3 grid, dim3 block, uint32_t first) {
+        if (a.teacher)
+            k_score<T, WAVES, kGrad, true, HELD><<<grid, block, 0, st>>>(a, first);
+        else if (a.h || a.entropy)
+            k_score<T, WAVES, kGradEntropy, false, HELD><<<grid, block, 0, st>>>(a, first);
+        else
+            k_score<T, WAVES, kGrad, false, HELD><<<grid, block, 0, st>>>(a, first);
+    });
+}
+// Waves of a row, and turns that the gradient's launch holds.  Up to 8,192 elements one wave a row does best, as no
+// barrier stands between its passes (gradient of 20,000 x 4,000 in bfloat16: 79 us, with four waves 186; of 9,000 x
+// 8,000 63 and 75; of 5,000 x 16,000 80 and 69), where there are rows enough to fill the chip so.  Turns held spare a
+// second reading but leave room for fewer waves: 3,000 x 85,000 take 220 us with six turns of four waves, 241 with two;
+// 5,000 x 16,000 take 83 and 69; four waves in place of eight 248 and 262.
 template <typename T>
 hipError_t launch_score_type(const ScoreArgs& a, bool grad, hipStream_t st) {
     const uint32_t n = std::min(a.vocab, a.piece);
-    if (n <= 2048) return launch_score_shape<T, 1>(a, grad, st);
-    if (n <= 8192) return launch_score_shape<T, 4>(a, grad, st);
-    return launch_score_shape<T, 8>(a, grad, st);
+    if (grad) {
+        if (n <= 2048 || (n <= 8192 && a.rows * a.pieces >= 1024)) return launch_gradient<T, 1, 4>(a, st);
+        if (n <= 80'000 / sizeof(T)) return launch_gradient<T, 4, 4>(a, st);
+        return launch_gradient<T, 4, 12>(a, st);
+    }
+    if (n <= 2048 || (n <= 8192 && a.rows * a.pieces >= 1024)) return launch_sums<T, 1>(a, st);
+    if (n <= 200'000 / sizeof(T)) return launch_sums<T, 4>(a, st);
+    return launch_sums<T, 8>(a, st);
 }
 hipError_t launch_score(const ScoreArgs& a, int type, bool grad, hipStream_t st) {
     return with_type(type, [&](auto zero) { return launch_score_type<decltype(zero)>(a, grad, st); });
