@@ -619,6 +619,11 @@ def _new(stream: Optional[torch.cuda.Stream], make, *args, **kwargs) -> torch.Te
     return t
 
 
+def _fresh(stream: Optional[torch.cuda.Stream], like: torch.Tensor, shape, dtype: torch.dtype) -> torch.Tensor:
+    """A contiguous tensor on the device of ``like`` that a call on ``stream`` writes."""
+    return like.new_empty(shape, dtype=dtype) if stream is None else _new(stream, like.new_empty, shape, dtype=dtype)
+
+
 def _stream_on(device: int, stream: Optional[torch.cuda.Stream], *tensors) -> Optional[int]:
     """The stream's handle.  Tensors used on a stream that is not the current one are kept from reuse until its work so
     far is done; that the work before them is done is the caller's to see to."""
@@ -798,29 +803,33 @@ class LayerNorm(_Handle):
         return self._run(x, weight, bias, residual, out, scale, True, sum_out, stream)
 
     def _run(self, x, weight, bias, residual, out, scale, int8, sum_out, stream):
-        io = _LayerNormIO(eps=self.eps)
-        rows, io.x, io.x_stride = self._matrix(x, "x", self.dtype, self.dim)
+        io, dim = _LayerNormIO(eps=self.eps), self.dim
+        rows, io.x, io.x_stride = self._matrix(x, "x", self.dtype, dim)
         io.rows = rows
-        io.weight = self._tensor(weight, "weight", self.dtype, self.dim)
+        io.weight = self._tensor(weight, "weight", self.dtype, dim)
         if bias is not None:
-            io.bias = self._tensor(bias, "bias", self.dtype, self.dim)
-        y = out
-        if y is None:
-            y = (_new(stream, x.new_empty, x.shape, dtype=torch.int8) if int8
-                 else _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format))
-        _, io.y, io.y_stride = self._matrix(y, "out", torch.int8 if int8 else self.dtype, self.dim, rows)
+            io.bias = self._tensor(bias, "bias", self.dtype, dim)
+        if out is None:  # what is made here needs no check
+            y = _fresh(stream, x, x.shape, torch.int8 if int8 else self.dtype)
+            io.y, io.y_stride = y.data_ptr(), dim
+        else:
+            y = out
+            _, io.y, io.y_stride = self._matrix(y, "out", torch.int8 if int8 else self.dtype, dim, rows)
         if int8:
             if scale is None:
-                scale = _new(stream, x.new_empty, x.shape[:-1], dtype=torch.float32)
-            io.y_scale = self._tensor(scale, "scale", torch.float32, rows)
+                scale = _fresh(stream, x, x.shape[:-1], torch.float32)
+                io.y_scale = scale.data_ptr()
+            else:
+                io.y_scale = self._tensor(scale, "scale", torch.float32, rows)
         h = x
         if residual is not None:
-            _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, self.dim, rows)
-            h = _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format) if sum_out is None else sum_out
-        elif sum_out is not None:
+            _, io.residual, io.residual_stride = self._matrix(residual, "residual", self.dtype, dim, rows)
+            if sum_out is None:
+                h = _fresh(stream, x, x.shape, self.dtype)
+                io.sum, io.sum_stride = h.data_ptr(), dim
+        if sum_out is not None:
             h = sum_out
-        if h is not x or sum_out is not None:
-            _, io.sum, io.sum_stride = self._matrix(h, "sum_out", self.dtype, self.dim, rows)
+            _, io.sum, io.sum_stride = self._matrix(h, "sum_out", self.dtype, dim, rows)
         if rows and (out is not None or sum_out is not None):
             self._outputs_apart(io, out is not None and not int8, sum_out is not None)
         if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
@@ -859,9 +868,11 @@ class LayerNorm(_Handle):
         if dsum is not None:
             _, io.dsum, io.dsum_stride = self._matrix(dsum, "dsum", self.dtype, self.dim, rows)
         given = dx is not None
-        if not given:
-            dx = _new(stream, torch.empty_like, dy, memory_format=torch.contiguous_format)
-        _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.dim, rows)
+        if given:
+            _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.dim, rows)
+        else:
+            dx = _fresh(stream, dy, dy.shape, self.dtype)
+            io.dx, io.dx_stride = dx.data_ptr(), self.dim
         dweight = _gradient(dweight, accumulate, (self.dim,), self.device, stream)
         io.dweight = self._tensor(dweight, "dweight", torch.float32, self.dim)
         if dbias is not False:
@@ -916,13 +927,14 @@ class Embedding(_Handle):
         io.tokens, io.index = _ids_on(self.device.index, tokens, "tokens")
         rows = io.rows = tokens.numel()
         _, io.weight, io.weight_stride = self._matrix(weight, "weight", self.dtype, self.dim, self.vocab)
-        given = out is not None
-        if not given:
-            out = _new(stream, weight.new_empty, (*tokens.shape, self.dim))
-        _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.dim, rows)
-        if given and rows:
-            _apart(self.dtype.itemsize, "out", (io.y, rows, io.y_stride, self.dim),
-                   {"weight": (io.weight, self.vocab, io.weight_stride, self.dim)})
+        if out is None:
+            out = _fresh(stream, weight, (*tokens.shape, self.dim), self.dtype)
+            io.y, io.y_stride = out.data_ptr(), self.dim
+        else:
+            _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.dim, rows)
+            if rows:
+                _apart(self.dtype.itemsize, "out", (io.y, rows, io.y_stride, self.dim),
+                       {"weight": (io.weight, self.vocab, io.weight_stride, self.dim)})
         if weight.requires_grad and torch.is_grad_enabled():
             raise _untracked()
         st = _lib().gd_embed_forward(self._h, io, self._stream(stream, tokens, weight, out))
@@ -1116,12 +1128,17 @@ class GatedLinear(_Handle):
         if bias is not None:
             io.bias = self._tensor(bias, "bias", self.dtype, both)
         given = out is not None
-        if not given:
-            out = _new(stream, x.new_empty, (*x.shape[:-1], self.outf), dtype=self.dtype)
-        _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.outf, rows)
+        if given:
+            _, io.y, io.y_stride = self._matrix(out, "out", self.dtype, self.outf, rows)
+        else:
+            out = _fresh(stream, x, (*x.shape[:-1], self.outf), self.dtype)
+            io.y, io.y_stride = out.data_ptr(), self.outf
         pre = None
-        if keep_pre is not False:
-            pre = _new(stream, x.new_empty, (*x.shape[:-1], both), dtype=self.dtype) if keep_pre is True else keep_pre
+        if keep_pre is True:
+            pre = _fresh(stream, x, (*x.shape[:-1], both), self.dtype)
+            io.pre, io.pre_stride = pre.data_ptr(), both
+        elif keep_pre is not False:
+            pre = keep_pre
             _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, both, rows)
         if rows and (given or (pre is not None and keep_pre is not True)):
             k, n, size, others = self.inf, self.outf, self.dtype.itemsize, {}
@@ -1155,14 +1172,18 @@ class GatedLinear(_Handle):
         rows, io.dy, io.dy_stride = self._matrix(dy, "dy", self.dtype, self.outf)
         io.rows = rows
         _, io.pre, io.pre_stride = self._matrix(pre, "pre", self.dtype, both, rows)
-        if not given_dz:
-            dz = _new(stream, torch.empty_like, pre, memory_format=torch.contiguous_format)
-        _, io.dz, io.dz_stride = self._matrix(dz, "dz", self.dtype, both, rows)
+        if given_dz:
+            _, io.dz, io.dz_stride = self._matrix(dz, "dz", self.dtype, both, rows)
+        else:
+            dz = _fresh(stream, pre, pre.shape, self.dtype)
+            io.dz, io.dz_stride = dz.data_ptr(), both
         if need_dx:
             _, io.weight, io.weight_stride = self._matrix(weight, "weight", self.dtype, self.inf, both)
-            if dx is None:
-                dx = _new(stream, dy.new_empty, (*dy.shape[:-1], self.inf))
-            _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.inf, rows)
+            if given_dx:
+                _, io.dx, io.dx_stride = self._matrix(dx, "dx", self.dtype, self.inf, rows)
+            else:
+                dx = _fresh(stream, dy, (*dy.shape[:-1], self.inf), self.dtype)
+                io.dx, io.dx_stride = dx.data_ptr(), self.inf
         else:
             dx = None
         if need_dweight:
@@ -1219,11 +1240,12 @@ class _Scores(_Handle):
 
     def _dlogits(self, io, logits, out, stream, apart):
         """The gradient's buffer: new, or a given one that is the logits themselves or lies apart from what is read."""
-        given = out is not None
-        if not given:
-            out = _new(stream, torch.empty_like, logits, memory_format=torch.contiguous_format)
+        if out is None:
+            out = _fresh(stream, logits, logits.shape, self.dtype)
+            io.dlogits, io.dlogits_stride = out.data_ptr(), self.vocab
+            return out
         _, io.dlogits, io.dlogits_stride = self._matrix(out, "out", self.dtype, self.vocab, io.rows)
-        if given and io.rows:
+        if io.rows:
             _apart(self.dtype.itemsize, "out", (io.dlogits, io.rows, io.dlogits_stride, self.vocab),
                    {"logits": (io.logits, io.rows, io.stride, self.vocab), **apart}, ("logits",))
         return out
@@ -1239,25 +1261,34 @@ class TokenLogProbs(_Scores):
 
     _what = "logprob"
 
-    def forward(self, logits, tokens, top: int = 0, entropy: bool = True, out: Optional[LogProbs] = None, stream=None):
-        """LogProbs; ``top`` up to 64 alternatives, of equal logits the lower id first.  ``out``: one of an earlier call
-        of the same shape, to write again."""
+    def forward(self, logits, tokens, top: int = 0, entropy: bool = True, keep_stats: bool = False,
+                out: Optional[LogProbs] = None, stream=None):
+        """LogProbs; ``top`` up to 64 alternatives, of equal logits the lower id first; ``keep_stats`` for backward.
+        ``out``: one of an earlier call of the same shape and wishes, to write again."""
         io = _LogProbIO()
         rows = self._logits(io, logits)
         io.tokens, io.index = _ids_on(self.device.index, tokens, "tokens", rows)
         io.top, shape = top, tokens.shape
         if out is None:
-            made = functools.partial(_new, stream, logits.new_empty, dtype=torch.float32)
-            out = LogProbs(made(shape), made(shape) if entropy else None, made((*shape, 2)))
+            f32 = torch.float32
+            out = LogProbs(_fresh(stream, logits, shape, f32), _fresh(stream, logits, shape, f32) if entropy else None,
+                           _fresh(stream, logits, (*shape, 2), f32) if keep_stats else None)
             if top:
-                out.top_logp, out.top_ids = made((*shape, top)), _new(stream, logits.new_empty, (*shape, top), dtype=torch.int64)
-        io.logp = self._tensor(out.logp, "out.logp", torch.float32, rows)
-        io.stats = self._tensor(out.stats, "out.stats", torch.float32, 2 * rows)
+                out.top_logp = _fresh(stream, logits, (*shape, top), f32)
+                out.top_ids = _fresh(stream, logits, (*shape, top), torch.int64)
+        else:
+            for name, n in (("logp", rows), ("entropy", rows * entropy), ("stats", 2 * rows * keep_stats), ("top_logp", rows * top)):
+                if n:
+                    self._tensor(getattr(out, name), "out." + name, torch.float32, n)
+            if top:
+                self._tensor(out.top_ids, "out.top_ids", torch.int64, rows * top)
+        io.logp = out.logp.data_ptr()
         if entropy:
-            io.entropy = self._tensor(out.entropy, "out.entropy", torch.float32, rows)
+            io.entropy = out.entropy.data_ptr()
+        if keep_stats:
+            io.stats = out.stats.data_ptr()
         if top:
-            io.top_logp = self._tensor(out.top_logp, "out.top_logp", torch.float32, rows * top)
-            io.top_id = self._tensor(out.top_ids, "out.top_ids", torch.int64, rows * top)
+            io.top_logp, io.top_id = out.top_logp.data_ptr(), out.top_ids.data_ptr()
         if logits.requires_grad and torch.is_grad_enabled():
             raise _untracked()
         st = _lib().gd_logprob_forward(self._h, io, self._stream(stream, logits, tokens, out.logp, out.entropy, out.stats,
@@ -1268,7 +1299,7 @@ class TokenLogProbs(_Scores):
 
     def backward(self, logits, tokens, dlogp, dentropy=None, scores: Optional[LogProbs] = None, out=None, stream=None):
         """dlogits, from the gradients of the log probabilities and (or None) of the entropies, float32.  ``scores``:
-        what forward returned for these logits, to spare a pass over them; ``out`` may be the logits."""
+        what forward returned for these logits, with its stats, to spare a pass over them; ``out`` may be the logits."""
         return self._back(logits, tokens, dlogp, dentropy, scores, out, stream, False)[1]
 
     def forward_backward(self, logits, tokens, dlogp, dentropy=None, out=None, stream=None):
@@ -1289,8 +1320,8 @@ class TokenLogProbs(_Scores):
             if dentropy is not None:
                 io.entropy = self._tensor(scores.entropy, "scores.entropy", torch.float32, rows)
         if forward:
-            made = functools.partial(_new, stream, logits.new_empty, tokens.shape, dtype=torch.float32)
-            result = LogProbs(made(), None if dentropy is None else made())
+            result = LogProbs(_fresh(stream, logits, tokens.shape, torch.float32),
+                              None if dentropy is None else _fresh(stream, logits, tokens.shape, torch.float32))
             io.logp_out = result.logp.data_ptr()
             if dentropy is not None:
                 io.entropy_out = result.entropy.data_ptr()
@@ -1322,14 +1353,17 @@ class Distill(_Scores):
 
     _what = "distill"
 
-    def forward(self, logits, ids, teacher, stream=None):
-        """(loss, stats): float32 [...], and what backward takes to spare a pass over the logits."""
+    def forward(self, logits, ids, teacher, keep_stats: bool = False, stream=None):
+        """(loss, stats): float32 [...], and with ``keep_stats`` (else None) what backward takes to spare a pass over the
+        logits."""
         io = _DistillIO()
         rows = self._logits(io, logits)
         self._named(io, ids, teacher, rows)
-        loss = _new(stream, logits.new_empty, logits.shape[:-1], dtype=torch.float32)
-        stats = _new(stream, logits.new_empty, (*logits.shape[:-1], 2), dtype=torch.float32)
-        io.loss, io.stats = loss.data_ptr(), stats.data_ptr()
+        loss, stats = _fresh(stream, logits, logits.shape[:-1], torch.float32), None
+        io.loss = loss.data_ptr()
+        if keep_stats:
+            stats = _fresh(stream, logits, (*logits.shape[:-1], 2), torch.float32)
+            io.stats = stats.data_ptr()
         if torch.is_grad_enabled() and (logits.requires_grad or teacher.requires_grad):
             raise _untracked()
         st = _lib().gd_distill_forward(self._h, io, self._stream(stream, logits, ids, teacher, loss, stats))
@@ -1364,7 +1398,7 @@ class Distill(_Scores):
             io.stats = self._tensor(stats, "stats", torch.float32, 2 * rows)
         loss = None
         if forward:
-            loss = _new(stream, logits.new_empty, logits.shape[:-1], dtype=torch.float32)
+            loss = _fresh(stream, logits, logits.shape[:-1], torch.float32)
             io.loss_out = loss.data_ptr()
         apart = {}
         if out is not None and rows:

@@ -120,7 +120,7 @@ def test_tokens_over_sizes(kind, rows, vocab):
         scale32 = float(torch.tensor(scale, dtype=torch.float32))
         what = f"{kind} {rows}x{vocab} {padded}"
         for top in sorted({0, 1, min(5, vocab), min(64, vocab)}):
-            r = op.forward(x, tokens, top=top)
+            r = op.forward(x, tokens, top=top, keep_stats=True)
             check_scores(r, x, tokens, scale32, top, what)
         assert op.forward(x, tokens.int() if not padded else tokens, entropy=False).entropy is None
         g, h = draw(3, rows), draw(4, rows)
@@ -159,7 +159,7 @@ def test_masks(kind, rows, vocab):
         if y is not x:
             y[3] = torch.finfo(t).min  # as likely as one another
             y[4].masked_fill_(y[4] == -math.inf, torch.finfo(t).min)
-        r = op.forward(y, tokens, top=min(64, vocab))
+        r = op.forward(y, tokens, top=min(64, vocab), keep_stats=True)
         check_scores(r, y, tokens, 1.0, min(64, vocab), "masked")
         assert float(r.logp[0]) == -math.inf and float(r.logp[1]) == 0.0 and float(r.entropy[:2].abs().sum()) == 0
         assert float(r.logp[2]) == -math.inf
@@ -195,7 +195,7 @@ def test_values_that_are_not_finite(vocab):
     x[0, 3], x[2, 7], x[4, 9] = math.nan, math.inf, math.nan
     x[4] = math.nan
     op = gd.TokenLogProbs(vocab, torch.float32, max_rows=rows)
-    r, want = op.forward(x, tokens, top=5), op.forward(clean, tokens, top=5)
+    r, want = op.forward(x, tokens, top=5, keep_stats=True), op.forward(clean, tokens, top=5, keep_stats=True)
     g, h = torch.ones(rows, device="cuda"), torch.ones(rows, device="cuda")
     dx, dwant = op.backward(x, tokens, g, h, scores=r), op.backward(clean, tokens, g, h, scores=want)
     for row in range(rows):
@@ -266,7 +266,7 @@ def test_teacher_over_sizes(kind, rows, vocab, top):
                 ids[1, 0], teacher[1, 0] = 0, 1.0
         op = gd.Distill(vocab, t, scale=scale, max_rows=rows)
         what = f"{kind} {rows} {vocab} {top} {case}"
-        loss, stats = op.forward(x, ids, teacher)
+        loss, stats = op.forward(x, ids, teacher, keep_stats=True)
         dx = op.backward(x, ids, teacher, g, stats=stats)
         check_distill(loss, dx, x, ids, teacher, g, scale, what)
         loss2, dx2 = op.forward_backward(x, ids.int() if case == "plain" else ids, teacher, g)
@@ -291,7 +291,7 @@ def test_teacher_with_masks(vocab):
     teacher[3, 1] = -math.inf
     x[3, ids[3, 1]] = -math.inf  # masked, but not named either
     op = gd.Distill(vocab, torch.float32, max_rows=rows)
-    loss, stats = op.forward(x, ids, teacher)
+    loss, stats = op.forward(x, ids, teacher, keep_stats=True)
     assert float(loss[0]) == math.inf and float(loss[1]) == math.inf and bool(loss[2].isnan()) and bool(loss[3:].isfinite().all())
     for dx in (op.backward(x, ids, teacher, g, stats=stats), op.forward_backward(x, ids, teacher, g)[1]):
         assert not bool(dx[0].any()) and bool(dx[2].isnan().any()) and bool(dx[[1, 3, 4]].isfinite().all())
@@ -340,7 +340,7 @@ def test_strides_and_shapes(kind, vocab):
     before = wide.clone()
     op.backward(x, tokens, g, out=x)
     assert torch.equal(x, dwant) and torch.equal(wide[:, :3], before[:, :3]) and torch.equal(wide[:, 3 + vocab:], before[:, 3 + vocab:])
-    shaped = op.forward(before[:, 3:3 + vocab].contiguous().view(2, 3, vocab), tokens.view(2, 3), top=4)
+    shaped = op.forward(before[:, 3:3 + vocab].contiguous().view(2, 3, vocab), tokens.view(2, 3), top=4, keep_stats=True)
     assert shaped.logp.shape == (2, 3) and shaped.stats.shape == (2, 3, 2) and shaped.top_ids.shape == (2, 3, 4)
     assert torch.equal(shaped.logp.view(-1), want.logp) and torch.equal(shaped.top_ids.view(6, 4), want.top_ids[:, :4])
     again = op.forward(before[:, 3:3 + vocab], tokens, top=9, out=r)
@@ -378,9 +378,9 @@ def test_another_stream_and_graph_replays(rows, vocab):
     op, ds = gd.TokenLogProbs(vocab), gd.Distill(vocab)
 
     def everything(stream=None):
-        r = op.forward(x, tokens, top=3, stream=stream)
+        r = op.forward(x, tokens, top=3, keep_stats=True, stream=stream)
         r2, dx = op.forward_backward(x, tokens, g, h, stream=stream)
-        loss, stats = ds.forward(x, ids, teacher, stream=stream)
+        loss, stats = ds.forward(x, ids, teacher, keep_stats=True, stream=stream)
         return [r.logp, r.entropy, r.stats, r.top_logp, r.top_ids, r2.logp, r2.entropy, dx, loss,
                 op.backward(x, tokens, g, h, scores=r, stream=stream), ds.backward(x, ids, teacher, g, stats=stats, stream=stream),
                 *ds.forward_backward(x, ids, teacher, g, stream=stream)]
@@ -416,8 +416,9 @@ def test_refusals():
     op, ds = gd.TokenLogProbs(vocab, torch.float32, max_rows=rows), gd.Distill(vocab, torch.float32, max_rows=rows)
     x, tokens, g = draw(1, rows, vocab), ids_of(2, vocab, rows), draw(3, rows)
     ids, teacher = ids_of(4, vocab, rows, 3), draw(5, rows, 3)
-    r = op.forward(x, tokens)
-    for bad in (lambda: op.forward(x.bfloat16(), tokens), lambda: op.forward(x, tokens.float()), lambda: op.forward(x, tokens.cpu()),
+    r = op.forward(x, tokens, keep_stats=True)
+    assert op.forward(x, tokens).stats is None and ds.forward(x, ids, teacher)[1] is None
+    for bad in (lambda: op.backward(x, tokens, g, scores=op.forward(x, tokens)), lambda: op.forward(x.bfloat16(), tokens), lambda: op.forward(x, tokens.float()), lambda: op.forward(x, tokens.cpu()),
                 lambda: op.backward(x, tokens, g.double()), lambda: op.backward(x, tokens, g, g, scores=gd.LogProbs(r.logp, None, r.stats)),
                 lambda: ds.forward(x, ids.float(), teacher), lambda: ds.forward(x, ids, teacher.double())):
         with pytest.raises(TypeError):
