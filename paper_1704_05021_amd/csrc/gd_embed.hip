@@ -22,15 +22,18 @@ namespace gd {
 
 constexpr uint32_t kEmbedMaxDim = 1u << 20, kEmbedMaxRows = 1u << 24;
 constexpr uint32_t kNoToken = 0xFFFFFFFFu;  // padding: sorted behind every token
-constexpr uint32_t kSortChunk = 2048, kSortThreads = 1024;
+constexpr uint32_t kPadding = 0x7FFFFFFFu;  // what stands for it where tokens are compared: above them all, below 2^32 - 1
+constexpr uint32_t kSortChunk = 4096, kSortThreads = 1024;
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 // Sorted rows a unit holds, by the number of rows: few rows make many small units for the sake of parallel work, many
-// make larger ones, of which fewer partial sums are written.
-__host__ __device__ constexpr uint32_t unit_rows(uint64_t rows) { return rows <= 4096 ? 16 : rows <= 16384 ? 32 : 64; }
+// make larger ones, of which fewer partial sums are written (3,000 rows of 500 in binary32 for 85,000 words: 52 us with
+// units of 8, 57 with 16).
+__host__ __device__ constexpr uint32_t unit_rows(uint64_t rows) { return rows <= 4096 ? 8 : rows <= 16384 ? 32 : 64; }
 constexpr uint64_t unit_count(uint64_t rows) { return (rows + unit_rows(rows) - 1) / unit_rows(rows); }
 // The most units that any number of rows up to this one makes.
-constexpr uint64_t most_units(uint64_t rows) { return std::max<uint64_t>(std::min<uint64_t>((rows + 15) / 16, 512), (rows + 63) / 64); }
-static_assert(unit_count(4096) == 256 && unit_count(16384) == 512 && unit_count(16385) == 257);
+constexpr uint64_t most_units(uint64_t rows) { return std::max<uint64_t>(std::min<uint64_t>((rows + 7) / 8, 512), (rows + 63) / 64); }
+static_assert(unit_count(4096) == 512 && unit_count(16384) == 512 && unit_count(16385) == 257);
 
 // The token of row i: kNoToken for ids outside the vocabulary.
 __device__ __forceinline__ uint32_t token_at(const void* tokens, bool wide, uint64_t i, uint32_t vocab) {
@@ -66,78 +69,83 @@ __global__ __launch_bounds__(kBlock) void k_embed(gd_embed_io io, uint32_t vocab
     }
 }
 
-// Zeros over [rows][dim] at `stride`, the blocks `block` of `blocks` sharing it.
-__device__ __forceinline__ void fill_zeros(float* out, uint64_t rows, uint64_t dim, uint64_t stride, uint64_t block,
-                                           uint64_t blocks) {
+// Zeros over [rows][dim] at `stride`, shared by `blocks` blocks of kSortThreads, a 16-byte vector a thread and turn.  There are
+// as many blocks as such turns, up to kFillBlocks: 85,000 x 500 take 26 us so, 34 with 512 blocks that go round.
+constexpr uint32_t kFillBlocks = 1u << 20;
+__device__ __forceinline__ void fill_zeros(float* out, uint32_t rows, uint32_t dim, uint64_t stride, uint32_t block, uint32_t blocks) {
     const Pack<float, 4> zeros = {};
-    if (stride == dim) {  // one run
-        const uint64_t all = rows * dim;
-        for (uint64_t e = (block * kSortThreads + threadIdx.x) * 4; e < all; e += blocks * kSortThreads * 4)
-            store_stream<4>(out + e, zeros, (int)min(all - e, (uint64_t)4));
-        return;
+    const uint32_t per_row = (dim + 3) / 4;
+    const bool one_run = stride == dim;
+    const uint64_t all = one_run ? (uint64_t)rows * dim : (uint64_t)rows * per_row;
+    for (uint64_t v = (uint64_t)block * kSortThreads + threadIdx.x; one_run ? v * 4 < all : v < all; v += (uint64_t)blocks * kSortThreads) {
+        if (one_run) {
+            store_stream<4>(out + v * 4, zeros, (int)min(all - v * 4, (uint64_t)4));
+        } else {
+            const uint64_t row = v / per_row;
+            const uint32_t e = (uint32_t)(v - row * per_row) * 4;
+            store_stream<4>(out + row * stride + e, zeros, (int)(dim - e));
+        }
     }
-    for (uint64_t row = block * (kSortThreads / kWave) + wave_index(); row < rows; row += blocks * (kSortThreads / kWave))
-        for (uint64_t e = lane_id() * 4; e < dim; e += kWave * 4)
-            store_stream<4>(out + row * stride + e, zeros, (int)min(dim - e, (uint64_t)4));
+}
+uint32_t fill_blocks(uint32_t rows, uint32_t dim) {
+    return (uint32_t)std::min<uint64_t>(((uint64_t)rows * ((dim + 3ull) / 4) + kSortThreads - 1) / kSortThreads, kFillBlocks);
 }
 
-// Blocks below `chunks` sort 2,048 rows each by (token, row), bitonic: element
-// e 1024 + t is thread t's, so that exchanges at a distance below 64 stay
-// within a wave, the farthest within a thread, and the others pass through LDS.
-// The other blocks write zeros.
+// Sorts chunks of 4,096 rows by (token, row): an element's place is the number
+// of those before it, counted.  A block takes 64 elements, one a lane, and its
+// sixteen waves a share each of the chunk's tokens, four at a time from LDS.
+// (Sorted by exchanges, 2,048 in a block, 3,000 rows took 22 us.)  Blocks from
+// `sorts` on write zeros over the first `filled` rows.
+constexpr uint32_t kSortWaves = kSortThreads / kWave, kChunkBlocks = kSortChunk / kWave;
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(gd_embed_grad io, uint32_t vocab, uint32_t dim, bool wide,
-                                                             uint32_t chunks, uint64_t* out) {
-    if (blockIdx.x >= chunks) {
-        fill_zeros(io.dweight, vocab, dim, io.dweight_stride, blockIdx.x - chunks, gridDim.x - chunks);
+                                                             uint32_t sorts, uint64_t* out, uint32_t filled) {
+    if (blockIdx.x >= sorts) {
+        fill_zeros(io.dweight, filled, dim, io.dweight_stride, blockIdx.x - sorts, gridDim.x - sorts);
         return;
     }
-    __shared__ uint64_t lds[kSortChunk];
-    const uint64_t first = (uint64_t)blockIdx.x * kSortChunk;
-    const uint32_t n = (uint32_t)min(io.rows - first, (uint64_t)kSortChunk);
-    uint64_t key[2];
+    __shared__ __align__(16) uint32_t lds[kSortChunk];
+    __shared__ uint32_t counts[kSortWaves][kWave];
+    const uint64_t first = (uint64_t)(blockIdx.x / kChunkBlocks) * kSortChunk;
+    const uint32_t n = (uint32_t)min(io.rows - first, (uint64_t)kSortChunk), padded = (n + kWave - 1) / kWave * kWave;
+    for (uint32_t i = threadIdx.x; i < padded; i += kSortThreads)
+        lds[i] = i < n ? min(token_at(io.tokens, wide, first + i, vocab), kPadding) : 0xFFFFFFFFu;
+    __syncthreads();
+    const uint32_t i0 = blockIdx.x % kChunkBlocks * kWave, i = i0 + lane_id();
+    if (i0 >= n) return;
+    const uint32_t mine = lds[i], share = (padded / kWave + kSortWaves - 1) / kSortWaves * kWave;
+    uint32_t j = min(wave_index() * share, padded);
+    const uint32_t end = min(j + share, padded);
+    uint32_t before = 0;
+    const auto count = [&](uint32_t stop, uint32_t bound) {  // tokens below the bound
+#pragma unroll 4
+        for (; j < stop; j += 4) {
+            const u4 t = *(const u4*)(lds + j);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const uint32_t i = e * kSortThreads + threadIdx.x;
-        key[e] = ~0ull;
-        if (i < n) key[e] = (uint64_t)token_at(io.tokens, wide, first + i, vocab) << 32 | (uint32_t)(first + i);
-    }
-    uint32_t all = 2;  // a power of two that holds them: what lies behind is not looked at
-    while (all < n) all *= 2;
-    for (uint32_t k = 2; k <= all; k *= 2)
-        for (uint32_t d = k / 2; d; d /= 2) {
-            if (d == kSortThreads) {  // k is the whole chunk: ascending
-                const uint64_t lo = min(key[0], key[1]), hi = max(key[0], key[1]);
-                key[0] = lo, key[1] = hi;
-                continue;
-            }
-            uint64_t other[2];
-            if (d >= (uint32_t)kWave) {
-                __syncthreads();
-                lds[threadIdx.x] = key[0], lds[kSortThreads + threadIdx.x] = key[1];
-                __syncthreads();
-                other[0] = lds[threadIdx.x ^ d], other[1] = lds[(kSortThreads + threadIdx.x) ^ d];
-            } else {
-                other[0] = __shfl_xor((unsigned long long)key[0], (int)d);
-                other[1] = __shfl_xor((unsigned long long)key[1], (int)d);
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t i = e * kSortThreads + threadIdx.x;
-                key[e] = ((i & d) == 0) == ((i & k) == 0) ? min(key[e], other[e]) : max(key[e], other[e]);
-            }
+            for (int k = 0; k < 4; ++k) before += t[k] < bound;
         }
+    };
+    count(min(end, i0), mine + 1);  // equal ones of lower rows are before it
+    for (const uint32_t stop = min(end, i0 + kWave); j < stop; ++j) before += lds[j] < mine + (j < i);
+    count(end, mine);
+    counts[wave_index()][lane_id()] = before;
+    __syncthreads();
+    if (wave_index() || i >= n) return;
+    before = 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const uint32_t i = e * kSortThreads + threadIdx.x;
-        if (i < n) out[first + i] = key[e];
-    }
+    for (uint32_t w = 0; w < kSortWaves; ++w) before += counts[w][lane_id()];
+    out[first + before] = (uint64_t)(mine == kPadding ? kNoToken : mine) << 32 | (uint32_t)(first + i);
 }
 
 // The sorted chunks in one order: an element's place is the number of smaller
-// ones, a binary search in each other chunk, four of them at a time.
-__global__ __launch_bounds__(kBlock) void k_embed_rank(const uint64_t* chunk, uint32_t rows, uint32_t chunks,
-                                                       uint64_t* order) {
-    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+// ones, a binary search in each other chunk, four of them at a time.  Blocks
+// from `ranks` on write zeros over `fill` rows.
+__global__ __launch_bounds__(kSortThreads) void k_embed_rank(const uint64_t* chunk, uint32_t rows, uint32_t chunks, uint64_t* order,
+                                                       uint32_t ranks, float* out, uint32_t fill, uint32_t dim, uint64_t stride) {
+    if (blockIdx.x >= ranks) {
+        fill_zeros(out, fill, dim, stride, blockIdx.x - ranks, gridDim.x - ranks);
+        return;
+    }
+    const uint32_t i = blockIdx.x * kSortThreads + threadIdx.x;
     if (i >= rows) return;
     const uint64_t key = chunk[i];
     const uint32_t own = i / kSortChunk;
@@ -368,17 +376,20 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
     if (!guard.ok) return GD_ERR_HIP;
     const hipStream_t st = (hipStream_t)stream;
     const uint32_t chunks = (uint32_t)((io->rows + gd::kSortChunk - 1) / gd::kSortChunk);
-    // blocks of zeros: two a compute unit, fewer where there is less to write
-    const uint64_t zeros = io->accumulate ? 0 : ((uint64_t)e->vocab * e->dim + 4 * gd::kSortThreads - 1) / (4 * gd::kSortThreads);
-    const uint32_t fill = (uint32_t)std::min<uint64_t>(zeros, 512);
-    gd::k_embed_sort<<<dim3(chunks + fill), dim3(gd::kSortThreads), 0, st>>>(*io, e->vocab, e->dim, wide == GD_I64, chunks,
-                                                                            chunks > 1 ? e->chunk : e->order);
+    // The zeros are written beside the sort, and where its chunks are joined most of them beside that: each of the two
+    // launches waits on memory for some microseconds, of which the zeros need not be waited for.
+    const uint32_t first = io->accumulate ? 0 : chunks > 1 ? e->vocab / 4 : e->vocab, rest = io->accumulate ? 0 : e->vocab - first;
+    const uint32_t sorts = chunks * gd::kChunkBlocks;
+    gd::k_embed_sort<<<dim3(sorts + gd::fill_blocks(first, e->dim)), dim3(gd::kSortThreads), 0, st>>>(
+        *io, e->vocab, e->dim, wide == GD_I64, sorts, chunks > 1 ? e->chunk : e->order, first);
     hipError_t r = hipGetLastError();
     if (r != hipSuccess) return GD_ERR_HIP;
     if (!io->rows) return GD_OK;
     if (chunks > 1) {
-        gd::k_embed_rank<<<dim3((uint32_t)((io->rows + gd::kBlock - 1) / gd::kBlock)), dim3(gd::kBlock), 0, st>>>(
-            e->chunk, (uint32_t)io->rows, chunks, e->order);
+        const uint32_t ranks = (uint32_t)((io->rows + gd::kSortThreads - 1) / gd::kSortThreads);
+        gd::k_embed_rank<<<dim3(ranks + gd::fill_blocks(rest, e->dim)), dim3(gd::kSortThreads), 0, st>>>(
+            e->chunk, (uint32_t)io->rows, chunks, e->order, ranks, io->dweight + (uint64_t)first * io->dweight_stride, rest, e->dim,
+            io->dweight_stride);
         if (hipGetLastError() != hipSuccess) return GD_ERR_HIP;
     }
     const uint32_t unit = gd::unit_rows(io->rows), units = (uint32_t)gd::unit_count(io->rows);

@@ -73,9 +73,9 @@ def test_over_sizes(kind, index, rows, vocab, dim):
         check_backward(dw, dy, tokens, vocab, 1.5, rows, f"{kind} {rows} {vocab} {dim} {how}")
 
 
-# units of 16, 32 and 64 rows, several chunks of 2,048, the last one full or of one row; runs over many units
+# units of 8, 32 and 64 rows, one chunk of 4,096 and several, the last one full or of one row; runs over many units
 @pytest.mark.parametrize("how", ["text", "one", "each", "pairs", "padded"])
-@pytest.mark.parametrize("rows,dim", [(15, 20), (16, 20), (17, 300), (2048, 24), (2049, 24), (4096, 12), (4097, 12), (6144, 260),
+@pytest.mark.parametrize("rows,dim", [(7, 20), (8, 20), (9, 20), (15, 20), (16, 20), (17, 300), (2048, 24), (2049, 24), (4096, 12), (4097, 12), (6144, 260), (8192, 8),
                                       (16384, 5), (16385, 5), (30001, 9)])
 def test_backward_over_rows(how, rows, dim):
     vocab = max(rows, 700) if how in ("each", "pairs") else 700
