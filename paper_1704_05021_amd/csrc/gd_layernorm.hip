@@ -181,6 +181,34 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_layernorm(gd_lay
     }
 }
 
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+template <typename T>
+__device__ __forceinline__ uint32_t bits_of(T v) {
+    uint16_t b;
+    __builtin_memcpy(&b, &v, 2);
+    return b;
+}
+template <typename T>
+__device__ __forceinline__ float value_of_bits(uint32_t b) {
+    T v;
+    __builtin_memcpy(&v, &b, sizeof v);
+    return (float)v;
+}
+// Eight elements as they came from memory.  Kept as words: of elements the compiler makes eight values, which it takes apart
+// right behind the load, and so waits for the next row before it works on this one.
+template <typename T>
+struct Words {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    words w[sizeof(T) / 2];
+    __device__ __forceinline__ Words() {}
+    __device__ __forceinline__ Words(const Pack<T, 8>& p) { __builtin_memcpy(w, &p, sizeof p); }
+    __device__ __forceinline__ operator Pack<T, 8>() const {
+        Pack<T, 8> p;
+        __builtin_memcpy(&p, w, sizeof p);
+        return p;
+    }
+};
+
 // A block takes several rows, and loads each while it works on the one before;
 // its share of the sums over rows goes to part[blockIdx.x]: dweight's, then dbias's.
 template <typename T, int WAVES, int V, int ENDS>
@@ -192,15 +220,15 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads, 4) void k_layernorm_bac
     const uint64_t turn = (uint64_t)gridDim.x * S::kRows;
     const bool add = io.dsum != nullptr;
     struct Row {
-        Pack<T, 8> x[V], dy[V], dsum[V];
-        T first;
+        Words<T> x[V], dy[V], dsum[V];
+        uint32_t first;  // its bits
     };
     const auto place = [&](int i) { return Place<ENDS>((t + i * S::kRow) * 8, dim); };
     const auto load = [&](Row& r, uint64_t first) {
         const uint64_t row = min(first + threadIdx.x / S::kRow, io.rows - 1);
         const T *x = (const T*)io.x + row * io.x_stride, *dy = (const T*)io.dy + row * io.dy_stride;
         const T* dsum = add ? (const T*)io.dsum + row * io.dsum_stride : dy;
-        r.first = *x;
+        r.first = bits_of(*x);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             r.x[i] = place(i).load(x);
@@ -227,13 +255,14 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads, 4) void k_layernorm_bac
         if (!kAhead) load(next, first);
         const Row r = next;
         if (kAhead && first + turn < io.rows) load(next, first + turn);
-        const double from_here = (float)r.first;
+        const float x0 = value_of_bits<T>(r.first);
+        const double from_here = x0;
         double s[4] = {0.0, 0.0, 0.0, 0.0};  // of d, d^2, a, a d: d and a are 0 past the row's end
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float x[8], g[8];
-            place(i).get(x, r.x[i], (float)r.first);
-            place(i).get(g, r.dy[i], 0.0f);
+            place(i).template get<T>(x, r.x[i], x0);
+            place(i).template get<T>(g, r.dy[i], 0.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const double d = (double)x[j] - from_here, a = g[j] * w(i, j);
@@ -252,8 +281,9 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads, 4) void k_layernorm_bac
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float x[8], g[8];
-            place(i).get(x, r.x[i], (float)r.first);
-            place(i).get(g, r.dy[i], 0.0f);
+            place(i).template get<T>(x, r.x[i], x0);
+            place(i).template get<T>(g, r.dy[i], 0.0f);
+            const Pack<T, 8> more = r.dsum[i];
             Pack<T, 8> d;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -261,7 +291,7 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads, 4) void k_layernorm_bac
                 dw[i][j] += S::kRows == 1 || on ? g[j] * xhat : 0.0f;
                 db[i][j] += S::kRows == 1 || on ? g[j] : 0.0f;
                 const float v = st.rstd * (g[j] * w(i, j) - mean_a - xhat * mean_ax);
-                d.v[j] = (T)(add ? v + (float)r.dsum[i].v[j] : v);
+                d.v[j] = (T)(add ? v + (float)more.v[j] : v);
             }
             place(i).store((T*)io.dx + row * io.dx_stride, d, on);
         }
