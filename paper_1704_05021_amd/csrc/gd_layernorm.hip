@@ -45,7 +45,8 @@ __device__ __forceinline__ RowStats row_stats(double pivot, double d, double dd,
 enum RowEnds {
     kShort = 0,  // dim is below 8: read element by element
     kRagged = 1, // the last vector is the one that ends with the row; what it shares with the one before is left out
-    kWhole = 2
+    kWhole = 2,
+    kFull = 3    // and every thread has one
 };
 
 // The vector of eight elements that a thread takes of a row: where it lies, and which of its elements are the thread's.
@@ -54,7 +55,9 @@ struct Place {
     uint32_t at, dim, mine;  // mine: a bit for each
     __device__ __forceinline__ Place(uint32_t e, uint32_t dim) : dim(dim) {
         at = ENDS == kShort ? 0 : min(e, dim - 8);
-        if (ENDS == kWhole)
+        if (ENDS == kFull)
+            at = e, mine = 0xFF;
+        else if (ENDS == kWhole)
             mine = e < dim ? 0xFF : 0;
         else if (ENDS == kRagged)
             mine = 0xFFu << min(e - at, 8u) & 0xFF;
@@ -78,9 +81,9 @@ struct Place {
     __device__ __forceinline__ void get(float (&v)[8], const Pack<T, 8>& raw, float rest) const {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (float)raw.v[j];
-        if (mine == 0xFF) return;
+        if (ENDS == kFull || mine == 0xFF) return;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = ENDS != kWhole && mine >> j & 1 ? v[j] : rest;
+        for (int j = 0; j < 8; ++j) v[j] = ENDS < kWhole && mine >> j & 1 ? v[j] : rest;
     }
     template <typename T>
     __device__ __forceinline__ void store(T* row, const Pack<T, 8>& r, bool on) const {
@@ -90,7 +93,7 @@ struct Place {
                 store_stream<8>(row + at, r, 8);
             else
                 store_pack<8>(row + at, r);
-        } else if (ENDS != kWhole) {
+        } else if (ENDS < kWhole) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (mine >> j & 1) row[at + j] = r.v[j];
@@ -390,8 +393,9 @@ hipError_t launch_layernorm_back(const gd_layernorm_grad& io, uint32_t dim, floa
     return hipGetLastError();
 }
 
-template <int WAVES, typename F>
+template <int WAVES, int V, typename F>
 hipError_t with_ends(uint32_t dim, F f) {
+    if (dim == WAVES * kWave * 8 * V) return f(std::integral_constant<int, kFull>());
     if constexpr (WAVES == 1)
         if (dim < 8) return f(std::integral_constant<int, kShort>());
     return dim % 8 ? f(std::integral_constant<int, kRagged>()) : f(std::integral_constant<int, kWhole>());
@@ -449,7 +453,7 @@ gd_status gd_layernorm_forward(gd_layernorm* n, const gd_layernorm_io* io, void*
     if (!guard.ok) return GD_ERR_HIP;
     const hipError_t e = gd::with_type(n->type, [&](auto zero) {
         return gd::with_shape(n->dim, false, [&](auto waves, auto v) {
-            return gd::with_ends<waves()>(n->dim, [&](auto ends) {
+            return gd::with_ends<waves(), v()>(n->dim, [&](auto ends) {
                 return gd::launch_layernorm<decltype(zero), waves(), v(), ends()>(*io, n->dim, (hipStream_t)stream);
             });
         });
@@ -466,7 +470,7 @@ gd_status gd_layernorm_backward(gd_layernorm* n, const gd_layernorm_grad* io, vo
     if (!guard.ok) return GD_ERR_HIP;
     const hipError_t e = gd::with_type(n->type, [&](auto zero) {
         return gd::with_shape(n->dim, true, [&](auto waves, auto v) {
-            return gd::with_ends<waves()>(n->dim, [&](auto ends) {
+            return gd::with_ends<waves(), v()>(n->dim, [&](auto ends) {
                 return gd::launch_layernorm_back<decltype(zero), waves(), v(), ends()>(*io, n->dim, n->part, (hipStream_t)stream);
             });
         });

@@ -95,30 +95,66 @@ __device__ __forceinline__ void row_sums(double& a, double& b, double* lds_a, do
     }
 }
 
-// Up to four such sums behind one barrier, each wave's shares joined by 16 lanes a sum (all of them read by every
-// thread would take 64 registers for four sums of eight waves).
+// a in the lower half of the lanes and b in the upper, each with what its other half holds added: two sums over 64 lanes
+// become one over 32.
+__device__ __forceinline__ double halves_joined(double a, double b) {
+    const uint64_t x = (uint64_t)__double_as_longlong(a), y = (uint64_t)__double_as_longlong(b);
+    const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)y, false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(x >> 32), (uint32_t)(y >> 32), false, false);
+    return __longlong_as_double((long long)((uint64_t)hi[0] << 32 | lo[0])) +
+           __longlong_as_double((long long)((uint64_t)hi[1] << 32 | lo[1]));
+}
+// The same by rows of 16 lanes: a in the even ones and b in the odd.
+__device__ __forceinline__ double rows_joined(double a, double b) {
+    const uint64_t x = (uint64_t)__double_as_longlong(a), y = (uint64_t)__double_as_longlong(b);
+    const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)y, false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(x >> 32), (uint32_t)(y >> 32), false, false);
+    return __longlong_as_double((long long)((uint64_t)hi[0] << 32 | lo[0])) +
+           __longlong_as_double((long long)((uint64_t)hi[1] << 32 | lo[1]));
+}
+
+// Two or four such sums behind one barrier.  The sums share the steps over a
+// wave's lanes, which end with one sum to 16 or 32 of them (four sums one by
+// one took a quarter of the layer norm's backward pass), and 16 lanes a sum join
+// the waves' shares (read by every thread they would take 64 registers).
 template <int WAVES, int N, int LDS>
 __device__ __forceinline__ void row_sums(double (&v)[N], double (&lds)[N][LDS]) {
-    static_assert(N <= 4 && WAVES <= 16);
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
-    if constexpr (WAVES > 1) {
-        const uint32_t w = wave_index(), k = lane_id() / 16, from = lane_id() % 16;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (lane_id() == 0) lds[i][w] = v[i];
-        __syncthreads();
-        double s = -0.0;
-        if (k < (uint32_t)N && from < (uint32_t)WAVES) s = lds[k][w / WAVES * WAVES + from];
-        s += dpp_f64<0x111, 0xF>(s);  // row_shr:1
-        s += dpp_f64<0x112, 0xF>(s);  // row_shr:2
-        s += dpp_f64<0x114, 0xF>(s);  // row_shr:4
-        s += dpp_f64<0x118, 0xF>(s);  // row_shr:8
-        const uint64_t bits = (uint64_t)__double_as_longlong(s);
+    static_assert((N == 2 || N == 4) && WAVES <= 16);
+    double s = N == 2 ? halves_joined(v[0], v[1]) : rows_joined(halves_joined(v[0], v[N / 2]), halves_joined(v[1], v[N - 1]));
+    s += dpp_f64<0x111, 0xF>(s);  // row_shr:1
+    s += dpp_f64<0x112, 0xF>(s);  // row_shr:2
+    s += dpp_f64<0x114, 0xF>(s);  // row_shr:4
+    s += dpp_f64<0x118, 0xF>(s);  // row_shr:8
+    if (N == 2) s += dpp_f64<0x142, 0xA>(s);  // row_bcast:15, rows 1 and 3
+    constexpr int kSpan = kWave / N;          // sum i is in the last lane of the i-th span
+    const auto spread = [&](double x, int span) {
+        const uint64_t bits = (uint64_t)__double_as_longlong(x);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint32_t lo = lane_value((uint32_t)bits, i * 16 + 15), hi = lane_value((uint32_t)(bits >> 32), i * 16 + 15);
-            v[i] = __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+            const int from = (i + 1) * span - 1;
+            const uint32_t lo = lane_value((uint32_t)bits, from), hi = lane_value((uint32_t)(bits >> 32), from);
+            v[i] = __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+        }
+    };
+    if constexpr (WAVES == 1) {
+        spread(s, kSpan);
+    } else {
+        const uint32_t w = wave_index(), lane = lane_id(), k = lane / 16, from = lane % 16;
+        if (lane % kSpan == kSpan - 1) lds[lane / kSpan][w] = s;
+        __syncthreads();
+        s = -0.0;
+        if (k < (uint32_t)N && from < (uint32_t)WAVES) s = lds[k][w / WAVES * WAVES + from];
+        s += dpp_f64<0x111, 0xF>(s);
+        s += dpp_f64<0x112, 0xF>(s);
+        if (WAVES > 4) s += dpp_f64<0x114, 0xF>(s);
+        if (WAVES > 8) s += dpp_f64<0x118, 0xF>(s);
+        // the shares lie in the first WAVES lanes of 16; their sum is in the last of those
+        const uint64_t bits = (uint64_t)__double_as_longlong(s);
+        constexpr int kLast = WAVES > 8 ? 15 : WAVES > 4 ? 7 : 3;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t lo = lane_value((uint32_t)bits, i * 16 + kLast), hi = lane_value((uint32_t)(bits >> 32), i * 16 + kLast);
+            v[i] = __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
         }
     }
 }
