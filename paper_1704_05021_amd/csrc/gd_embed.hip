@@ -3,13 +3,16 @@
 //
 //   y[i] = scale weight[t_i],   dweight[v] = scale sum over i with t_i = v of dy[i]
 //
-// Both are bound by memory.  The gradient is formed without atomics on values,
-// so that it is the same on every run: rows are sorted by (token, row), the
-// sorted order is cut into equal units, a wave adds up a unit's runs of equal
-// tokens, and runs that cross units are joined from their units' shares.  Cut
-// by units and not by tokens, the work is even however often a token occurs
-// (in text the commonest word is a twentieth of all).  All of dweight is
-// written with zeros in the launch that sorts, which hides the sort behind it.
+// Both are bound by memory (8,192 rows of 4096 in bfloat16 17 us, 7.8 TB/s with
+// the commonest words' rows in the caches).  The gradient is formed without
+// atomics on values, so that it is the same on every run, and in one of two
+// forms: few rows in one launch, where every row looks for its like; more
+// sorted by (token, row), the sorted order cut into equal units, of which a wave
+// each adds up the runs of equal tokens, and runs that cross units joined from
+// their units' shares.  Cut by units and not by tokens, the work is even however
+// often a token occurs (in text the commonest word is a twentieth of all).  All
+// of dweight is written, and the zeros beside what else there is to do: they are
+// most of the time.
 
 #include <cmath>
 #include <new>
@@ -68,6 +71,134 @@ __global__ __launch_bounds__(kBlock) void k_embed(gd_embed_io io, uint32_t vocab
         }
     }
 }
+
+// out = or += scale s, columns from c on, n of which exist.
+template <int N>
+__device__ __forceinline__ void put_gradient(float* out, const float (&s)[N], float scale, int n, bool accumulate) {
+    Pack<float, N> v;
+    if (accumulate) v = load_some<N>(out, n);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v.v[j] = accumulate ? v.v[j] + scale * s[j] : scale * s[j];
+    store_some<N>(out, v, n);
+}
+
+// ---- Few rows: all of it in one launch ----
+//
+// A block takes a row and looks through all tokens for its own: the first row
+// of a token finds all rows of it, in order, and writes their sum, the others
+// end.  Blocks between those write zeros, over rows of dweight that no token
+// names.  Looking costs rows^2 reads of tokens, from the caches, and stays
+// beside the zeros up to kFewRows: 3,000 rows of 500 in binary32 for 85,000
+// words take 32 us, sorted (below) 43; 500 of 512 for 8,000 7.6 and 17.  But a
+// token that occurs often is one block's work: 4,000 rows of 1024 in bfloat16 for
+// 1,000 words take 36 us, sorted 27, so up to kFewWork elements of dy.
+constexpr uint32_t kFewWork = 1u << 21;
+constexpr uint32_t kFewRows = 4096, kFewThreads = 512, kFewWaves = kFewThreads / kWave, kFewAtOnce = 8;
+constexpr uint32_t kFillFloats = 16384;  // of zeros that a block writes, about
+constexpr uint32_t kFewBlocks = 1u << 22;
+
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uint32_t vocab, uint32_t dim, bool wide,
+                                                           uint32_t fills, uint32_t per_fill) {
+    constexpr int E = 16 / sizeof(T), kSlice = kWave * E;
+    __shared__ uint64_t mask[kFewRows / kWave];
+    __shared__ uint16_t list[kFewRows];
+    __shared__ float shares[kFewWaves][kSlice];
+    const uint32_t rows = (uint32_t)io.rows, wave = wave_index(), lane = lane_id();
+    // rows' blocks are spread evenly among those of zeros: the ones wait, the others write
+    const uint64_t all = (uint64_t)rows + fills, at = blockIdx.x;
+    const uint32_t i = (uint32_t)(at * rows / all);
+    if ((at + 1) * rows / all == i) {
+        uint32_t* named = (uint32_t*)list;  // a bit for each row of the block
+        static_assert(sizeof(list) * 8 >= kFillFloats);
+        const uint32_t first = (uint32_t)(at - i) * per_fill, n = min(per_fill, vocab - first);
+        for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += kFewThreads) named[w] = 0;
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < rows; j += kFewThreads) {
+            const uint32_t t = token_at(io.tokens, wide, j, vocab) - first;
+            if (t < n) atomicOr(&named[t / 32], 1u << t % 32);
+        }
+        __syncthreads();
+        const uint32_t per_row = (dim + 3) / 4;
+        const uint64_t vectors = (uint64_t)n * per_row;
+        for (uint64_t v = threadIdx.x; v < vectors; v += kFewThreads) {
+            const uint32_t row = n == 1 ? 0 : (uint32_t)v / per_row;
+            const uint32_t e = (uint32_t)(v - (uint64_t)row * per_row) * 4;
+            if (!(named[row / 32] >> row % 32 & 1))
+                store_stream<4>(io.dweight + (uint64_t)(first + row) * io.dweight_stride + e, Pack<float, 4>{}, (int)(dim - e));
+        }
+        return;
+    }
+    const uint32_t token = token_at(io.tokens, wide, i, vocab);
+    if (token == kNoToken) return;
+    uint32_t others[kFewRows / kFewThreads];
+#pragma unroll
+    for (uint32_t k = 0; k < kFewRows / kFewThreads; ++k)  // past the last row that one again
+        others[k] = token_at(io.tokens, wide, min(k * kFewThreads + threadIdx.x, rows - 1), vocab);
+#pragma unroll
+    for (uint32_t k = 0; k < kFewRows / kFewThreads; ++k) {
+        const uint64_t m = ballot(others[k] == token && k * kFewThreads + threadIdx.x < rows);
+        if (lane == 0) mask[k * kFewWaves + wave] = m;
+    }
+    __syncthreads();
+    uint64_t mine = mask[lane];
+    static_assert(kFewRows == kWave * kWave);
+    const uint64_t before = lane < i / kWave ? mine : lane == i / kWave ? mine & ((1ull << i % kWave) - 1) : 0;
+    if (ballot(before != 0)) return;  // an earlier row's block writes it
+    const uint32_t incl = wave_incl_scan(popc64(mine)), count = lane_value(incl, kWave - 1);
+    if (wave == 0)
+        for (uint32_t place = incl - popc64(mine); mine; mine &= mine - 1, ++place)
+            list[place] = (uint16_t)(lane * kWave + (uint32_t)__ffsll((unsigned long long)mine) - 1);
+    __syncthreads();
+    float* out = io.dweight + (uint64_t)token * io.dweight_stride;
+    // rows first to first + kFewAtOnce of the list, columns c on, n of which exist
+    const auto add = [&](uint32_t first, uint32_t c, int n, float (&sum)[E]) {
+        Pack<T, E> d[kFewAtOnce];
+#pragma unroll
+        for (uint32_t k = 0; k < kFewAtOnce; ++k)
+            d[k] = load_some<E>((const T*)io.dy + (uint64_t)list[min(first + k, count - 1)] * io.dy_stride + c, first + k < count ? n : 0);
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] = 0.0f;
+#pragma unroll
+        for (uint32_t k = 0; k < kFewAtOnce; ++k)
+#pragma unroll
+            for (int j = 0; j < E; ++j) sum[j] += (float)d[k].v[j];
+    };
+    if (count <= kFewAtOnce) {  // a wave takes a slice of the columns
+        for (uint32_t s = wave * kSlice; s < dim; s += kFewWaves * kSlice) {
+            const uint32_t c = min(s + lane * E, dim);
+            float sum[E];
+            add(0, c, (int)(dim - c), sum);
+            put_gradient<E>(out + c, sum, io.scale, (int)(dim - c), io.accumulate != 0);
+        }
+        return;
+    }
+    for (uint32_t s = 0; s < dim; s += kSlice) {  // the waves share the rows
+        const uint32_t c = min(s + lane * E, dim);
+        double total[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) total[j] = 0.0;
+        for (uint32_t first = wave * kFewAtOnce; first < count; first += kFewWaves * kFewAtOnce) {
+            float sum[E];
+            add(first, c, (int)(dim - c), sum);
+#pragma unroll
+            for (int j = 0; j < E; ++j) total[j] += sum[j];
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) shares[wave][lane * E + j] = (float)total[j];
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < (uint32_t)kSlice && s + j < dim; j += kFewThreads) {
+            double v = 0.0;
+#pragma unroll
+            for (uint32_t w = 0; w < kFewWaves; ++w) v += shares[w][j];
+            const float sum[1] = {(float)v};
+            put_gradient<1>(out + s + j, sum, io.scale, 1, io.accumulate != 0);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- More rows ----
 
 // Zeros over [rows][dim] at `stride`, shared by `blocks` blocks of kSortThreads, a 16-byte vector a thread and turn.  There are
 // as many blocks as such turns, up to kFillBlocks: 85,000 x 500 take 26 us so, 34 with 512 blocks that go round.
@@ -165,16 +296,6 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_rank(const uint64_t* chu
         for (int k = 0; k < kAtOnce; ++k) rank += at[k];
     }
     order[rank] = key;
-}
-
-// out = or += scale s, columns from c on, n of which exist.
-template <int N>
-__device__ __forceinline__ void put_gradient(float* out, const float (&s)[N], float scale, int n, bool accumulate) {
-    Pack<float, N> v;
-    if (accumulate) v = load_some<N>(out, n);
-#pragma unroll
-    for (int j = 0; j < N; ++j) v.v[j] = accumulate ? v.v[j] + scale * s[j] : scale * s[j];
-    store_some<N>(out, v, n);
 }
 
 // A wave adds up one unit of the sorted rows, a slice of 64 vectors of columns:
@@ -375,6 +496,16 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
     gd::DeviceGuard guard(e->device);
     if (!guard.ok) return GD_ERR_HIP;
     const hipStream_t st = (hipStream_t)stream;
+    const uint32_t per_fill = std::max(gd::kFillFloats / e->dim, 1u);
+    const uint64_t fills = io->accumulate ? 0 : ((uint64_t)e->vocab + per_fill - 1) / per_fill;
+    if (io->rows <= gd::kFewRows && io->rows * e->dim <= gd::kFewWork && fills <= gd::kFewBlocks) {
+        const hipError_t r = gd::with_type(e->type, [&](auto zero) {
+            gd::k_embed_few<decltype(zero)><<<dim3((uint32_t)(io->rows + fills)), dim3(gd::kFewThreads), 0, st>>>(
+                *io, e->vocab, e->dim, wide == GD_I64, (uint32_t)fills, per_fill);
+            return hipGetLastError();
+        });
+        return r == hipSuccess ? GD_OK : GD_ERR_HIP;
+    }
     const uint32_t chunks = (uint32_t)((io->rows + gd::kSortChunk - 1) / gd::kSortChunk);
     // The zeros are written beside the sort, and where its chunks are joined most of them beside that: each of the two
     // launches waits on memory for some microseconds, of which the zeros need not be waited for.

@@ -73,9 +73,10 @@ def test_over_sizes(kind, index, rows, vocab, dim):
         check_backward(dw, dy, tokens, vocab, 1.5, rows, f"{kind} {rows} {vocab} {dim} {how}")
 
 
-# units of 8, 32 and 64 rows, one chunk of 4,096 and several, the last one full or of one row; runs over many units
+# one launch up to 4,096 rows; sorted: units of 8, 32 and 64 rows (8 where rows are long), one chunk of 4,096 and several,
+# the last one full or of one row; runs over many units
 @pytest.mark.parametrize("how", ["text", "one", "each", "pairs", "padded"])
-@pytest.mark.parametrize("rows,dim", [(7, 20), (8, 20), (9, 20), (15, 20), (16, 20), (17, 300), (2048, 24), (2049, 24), (4096, 12), (4097, 12), (6144, 260), (8192, 8),
+@pytest.mark.parametrize("rows,dim", [(7, 20), (8, 20), (9, 20), (15, 20), (16, 20), (17, 300), (2048, 24), (2049, 24), (4096, 12), (4097, 12), (6144, 260), (257, 8200), (2049, 1040), (4096, 520), (8192, 8),
                                       (16384, 5), (16385, 5), (30001, 9)])
 def test_backward_over_rows(how, rows, dim):
     vocab = max(rows, 700) if how in ("each", "pairs") else 700
@@ -86,17 +87,29 @@ def test_backward_over_rows(how, rows, dim):
     assert torch.equal(op.backward(dy, tokens), dw)  # the same bits again
 
 
+@pytest.mark.parametrize("rows", [7, 8, 9, 16, 17, 25])
+@pytest.mark.parametrize("how", ["text", "one", "pairs", "padded"])
+def test_backward_of_few_long_rows(how, rows):
+    """Sorted, in one unit, one and a row, and several."""
+    vocab, dim = 12, (1 << 21) // rows + 1
+    tokens, dy = words(5, rows, vocab, how), draw(6, rows, dim)
+    dw = gd.Embedding(vocab, dim, torch.float32, max_rows=rows).backward(dy, tokens)
+    check_backward(dw, dy, tokens, vocab, 1.0, rows, f"{how} {rows}")
+
+
 def test_a_plan_of_just_these_rows():
     """Scratch for max_rows holds the most units that any smaller number of rows makes."""
     for most in (1, 16, 17, 4000, 4096, 5000, 8191, 9000, 16384, 16385, 33000):
-        op = gd.Embedding(64, 33, torch.float32, max_rows=most)
+        dim = 529 if 3900 < most < 8000 else 33
+        op = gd.Embedding(64, dim, torch.float32, max_rows=most)
         for rows in {most, min(most, 4096), min(most, 16384)}:
-            dy, tokens = draw(1, rows, 33), words(2, rows, 64, "text")
+            dy, tokens = draw(1, rows, dim), words(2, rows, 64, "text")
             check_backward(op.backward(dy, tokens), dy, tokens, 64, 1.0, rows, f"{rows} of {most}")
 
 
-def test_whole_numbers_are_summed_exactly():
-    rows, vocab, dim = 5000, 30, 70
+@pytest.mark.parametrize("rows", [1, 8, 9, 64, 65, 700, 3000, 4096, 5000])
+def test_whole_numbers_are_summed_exactly(rows):
+    vocab, dim = 30, 70
     dy = torch.randint(-8, 9, (rows, dim), generator=torch.Generator().manual_seed(1)).float().cuda()
     tokens = words(2, rows, vocab)
     dw = gd.Embedding(vocab, dim, torch.float32, scale=-2.0).backward(dy, tokens)

@@ -62,10 +62,14 @@ for ty in (0, 1, 2):
         f = dict(rows=2**50, tokens=P, weight=P, y=P, weight_stride=dim, y_stride=dim, scale=1.0, index=1)
         assert call("gd_embed_forward", e, io(gd._EmbedIO, **f)) == (0, 1)  # the grid goes round
         assert Dim.in_dll(S, "g_grid").x <= 2**20
-        for rows, launches in ((1, 2), (8, 2), (9, 3), (4096, 3), (4097, 4), (2**24, 4)):
+        for rows, accumulate in ((1, 1), (1, 0), (8, 1), (9, 1), (4096, 1), (4096, 0), (4097, 1), (4097, 0), (2**24, 1), (2**24, 0)):
             if rows > 64 and dim > 4096: continue
-            b = dict(rows=rows, tokens=P, dy=P, dweight=P, dy_stride=dim, dweight_stride=dim, scale=1.0, index=0)
+            # in one launch where rows are few and short; zeros of more blocks than a launch holds go round in the sorted form
+            few = rows <= 4096 and rows * dim <= 2**21 and (accumulate or -(-(2**31 - 1) // max(16384 // dim, 1)) <= 2**22)
+            launches = 1 if few else 1 + (rows > 4096) + 1 + (rows > 8)
+            b = dict(rows=rows, tokens=P, dy=P, dweight=P, dy_stride=dim, dweight_stride=dim, scale=1.0, index=0, accumulate=accumulate)
             assert call("gd_embed_backward", e, io(gd._EmbedGrad, **b)) == (0, launches), (dim, rows)
+            assert Dim.in_dll(S, "g_grid").x * 1024 < 2**32
         G.gd_embed_destroy(e)
 e = made("embed", 100, 8, 1, 50)
 f = dict(rows=60, tokens=P, weight=P, y=P, weight_stride=8, y_stride=8, scale=2.0, index=0)
@@ -75,7 +79,7 @@ for bad in (dict(tokens=None), dict(weight=None), dict(y=None), dict(weight_stri
             dict(index=2), dict(index=-1)):
     assert call("gd_embed_forward", e, io(gd._EmbedIO, **but(f, **bad)))[0] == 1, bad
 b = dict(rows=50, tokens=P, dy=P, dweight=P, dy_stride=8, dweight_stride=8, scale=1.0, index=1)
-assert call("gd_embed_backward", e, io(gd._EmbedGrad, **b)) == (0, 3)
+assert call("gd_embed_backward", e, io(gd._EmbedGrad, **b)) == (0, 1)
 assert call("gd_embed_backward", e, io(gd._EmbedGrad, **but(b, rows=0, tokens=None, dy=None))) == (0, 1)  # zeros
 assert call("gd_embed_backward", e, io(gd._EmbedGrad, **but(b, rows=0, accumulate=1))) == (0, 0)
 for bad in (dict(rows=51), dict(tokens=None), dict(dy=None), dict(dweight=None), dict(dy_stride=7), dict(dweight_stride=7),
