@@ -115,3 +115,33 @@ def test_the_step_in_a_graph(words):
         logp, loss = step(grads[0])
         torch.cuda.synchronize()
         assert torch.equal(grads[0], grads[1]) and torch.equal(logp, held[0]) and torch.equal(loss, held[1])
+
+
+def test_readme_language_model():
+    """The README's example runs, and its table's gradient is that of its loss in 64 bits, at bfloat16's precision."""
+    import re
+
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    blocks = re.findall(r"```py\n(.*?)```", open(os.path.join(ROOT, "README.md")).read(), re.S)
+    assert len(blocks) == 1
+    env = {}
+    torch.manual_seed(0)
+    exec(compile(blocks[0], "README.md", "exec"), env)
+    torch.cuda.synchronize()
+    table, up, down, head = (d(env[k]).requires_grad_() for k in ("table", "up", "down", "head"))
+    tokens, following = env["tokens"].cpu(), env["following"].cpu()
+    h0 = table[tokens] * env["width"] ** 0.5
+    c = h0 - h0.mean(1, keepdim=True)
+    z = c / torch.sqrt((c * c).mean(1, keepdim=True) + 1e-5) @ up.t()
+    gate, u = z.chunk(2, 1)
+    logits = (gate / (1 + torch.exp(-gate)) * u @ down.t() + h0) @ head.t()
+    lp = torch.log_softmax(logits, 1)
+    seen = following >= 0
+    loss = -lp[seen].gather(1, following[seen][:, None]).sum() / 290
+    loss.backward()
+    # each of some ten results along the way is rounded to bfloat16, half a step of 2^-8, at random: together within 2^-5
+    assert abs(float(env["loss"]) - float(loss.detach())) < 2.0 ** -8 * float(loss.detach())
+    for k, want in (("dtable", table), ("dup", up), ("ddown", down), ("dhead", head)):
+        assert float((d(env[k]) - want.grad).norm()) < 2.0 ** -5 * float(want.grad.norm()), k
+    assert env["best"].top_ids.shape == (1, 5) and bool(env["apart"].isfinite().all())
