@@ -19,7 +19,8 @@
 // Top alternatives: a row's 64 groups of threads know their largest logits, the
 // K-th largest of those is a bound that at least K elements reach, and few more:
 // a second look at the row lists what reaches it, and each listed one counts
-// those before it.
+// those before it.  Where a mask makes very many equal to the bound, a third look
+// lists what is above it.
 
 #include <cmath>
 #include <new>
@@ -298,10 +299,15 @@ struct Alternatives {
                                          Put put) {
         const uint32_t t = threadIdx.x % S::kRow, r = threadIdx.x / S::kRow;
         const uint32_t wave = wave_index(), wave0 = wave / WAVES * WAVES;
+        const auto row_sync = [] {  // a row's threads, whose paths may part from other rows' of the block
+            if constexpr (WAVES > 1)
+                __syncthreads();
+            else
+                wave_lds_sync();
+        };
         // the bound: the K-th largest of 64 groups of threads
         group[wave][lane_id()] = order_of(largest);
-        if (t == 0) n[r] = 0;
-        __syncthreads();
+        row_sync();
         if (t < (uint32_t)kWave) {
             uint32_t mine = 0, before = 0;
 #pragma unroll
@@ -313,51 +319,70 @@ struct Alternatives {
             }
             if (before == K - 1) bound[r] = mine;
         }
-        __syncthreads();
+        row_sync();
         const float least = value_of(bound[r]);
         const Turns<T, S::kRow> turns(x, t, len);
-        // one look a vector: hardly any holds an element that reaches the bound
-        const auto look = [&](const Pack<T, 8>& raw, uint32_t at, uint32_t mine) {
-            float v[8], top = -INFINITY;
+        // Lists what is above the bound, and with `equal` what equals it; how many there are.
+        const auto look = [&](bool equal) {
+            if (t == 0) n[r] = 0;
+            row_sync();
+            // one look a vector: hardly any holds an element to list
+            const auto at_vector = [&](const Pack<T, 8>& raw, uint32_t at, uint32_t mine) {
+                float v[8], top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (float)raw.v[j];
+                for (int j = 0; j < 8; ++j) v[j] = (float)raw.v[j];
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) top = max_of(top, v[j], v[j + 1]);
-            if (!(top >= least)) return;
+                for (int j = 0; j < 8; j += 2) top = max_of(top, v[j], v[j + 1]);
+                if (!(equal ? top >= least : top > least)) return;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (v[j] >= least && mine >> j & 1) {
-                    const uint32_t place = atomicAdd(&n[r], 1u);
-                    if (place < kListRoom) list[r][place] = key_of_element(order_of(v[j]), begin + at + j);
-                }
-        };
-        if (on && !odd) {
+                for (int j = 0; j < 8; ++j)
+                    if ((equal ? v[j] >= least : v[j] > least) && mine >> j & 1) {
+                        const uint32_t place = atomicAdd(&n[r], 1u);
+                        if (place < kListRoom) list[r][place] = key_of_element(order_of(v[j]), begin + at + j);
+                    }
+            };
             turns.walk(0, [&](const typename Turns<T, S::kRow>::Turn& raw, uint32_t turn) {
 #pragma unroll
-                for (int k = 0; k < kScoreDeep; ++k) look(raw[k], turns.vector(turn, k) * 8, 0xFF);
+                for (int k = 0; k < kScoreDeep; ++k) at_vector(raw[k], turns.vector(turn, k) * 8, 0xFF);
             });
             if (turns.left()) {
                 typename Turns<T, S::kRow>::Turn raw;
                 turns.load_left(raw);
 #pragma unroll
-                for (int k = 0; k < kScoreDeep; ++k) look(raw[k], turns.left_vec(k).at, turns.left_vec(k).mine);
+                for (int k = 0; k < kScoreDeep; ++k) at_vector(raw[k], turns.left_vec(k).at, turns.left_vec(k).mine);
+            }
+            row_sync();
+            const uint32_t listed = n[r];
+            row_sync();
+            return listed;
+        };
+        if (!on) return;
+        if (!odd) {
+            uint32_t listed = look(true);
+            // very many equal the bound (what a mask puts in its places): those above it, and behind them its first ones
+            const bool many = listed > kListRoom;
+            if (many) listed = look(false);
+            if (listed <= kListRoom) {
+                for (uint32_t i = t; i < listed; i += S::kRow) {
+                    const uint64_t key = list[r][i];
+                    uint32_t rank = 0;
+                    for (uint32_t k = 0; k < listed; ++k) rank += list[r][k] > key;
+                    if (rank < K) put(rank, key);
+                }
+                if (many && t < (uint32_t)kWave)  // in order of their ids, 64 elements at a time
+                    for (uint32_t e = 0, found = listed; e < len && found < K; e += kWave) {
+                        const bool here = e + t < len && (float)x[min(e + t, len - 1)] == least;
+                        const uint64_t m = ballot(here);
+                        const uint32_t rank = found + lanes_below(m);
+                        if (here && rank < K) put(rank, key_of_element(order_of(least), begin + e + t));
+                        found += popc64(m);
+                    }
+                if (!many)
+                    for (uint32_t k = len + t; k < K; k += S::kRow) put(k, 0);  // a piece of fewer elements than K
+                return;
             }
         }
-        __syncthreads();
-        const uint32_t listed = n[r];
-        if (!odd && listed <= kListRoom) {
-            if (!on) return;
-            for (uint32_t i = t; i < listed; i += S::kRow) {
-                const uint64_t key = list[r][i];
-                uint32_t rank = 0;
-                for (uint32_t k = 0; k < listed; ++k) rank += list[r][k] > key;
-                if (rank < K) put(rank, key);
-            }
-            for (uint32_t k = len + t; k < K; k += S::kRow) put(k, 0);  // a piece of fewer elements than K
-            return;
-        }
-        // more elements reach the bound than the list holds (a row of equal ones), or not all are in order: the next
-        // largest, K times
+        // Very many are above the bound (all of a few groups'), or not all are in order: the next largest, K times.
         uint64_t last = ~0ull;
         for (uint32_t k = 0; k < K; ++k) {
             uint64_t most = 0;

@@ -172,6 +172,20 @@ def test_masks(kind, rows, vocab):
             assert not bool(dx[0].any() or again[0].any())
 
 
+@pytest.mark.parametrize("rows,vocab", [(3, 500), (3, 2048), (1030, 2100), (2, 5000), (2, 8191), (300, 9000), (2, 40_000), (300, 110_000)])
+@pytest.mark.parametrize("value", [-math.inf, torch.finfo(torch.bfloat16).min, -3.0])
+@pytest.mark.parametrize("left", [0, 1, 5, 70, 300])
+def test_few_words_that_a_mask_leaves(rows, vocab, value, left):
+    """Most of a row equal: the alternatives are what is above, then the first of the others."""
+    x = torch.full((rows, vocab), value)
+    g = torch.Generator().manual_seed(left)
+    for row in range(rows):
+        x[row, torch.randperm(vocab, generator=g)[:left] if row % 3 else torch.arange(left) + vocab - left] = torch.randn(left, generator=g)
+    x, tokens = x.bfloat16().cuda(), ids_of(1, vocab, rows)
+    for top in (1, 4, 64):
+        check_scores(gd.TokenLogProbs(vocab, max_rows=rows).forward(x, tokens, top=top), x, tokens, 1.0, top, "few")
+
+
 @pytest.mark.parametrize("rows,vocab", [(3, 30), (3, 2048), (2, 5000), (300, 9000), (2, 40_000)])
 def test_ties_go_to_the_lower_id(rows, vocab):
     """Rows of equal logits, of zeros of both signs, of few values: more elements at the bound than a list holds."""
