@@ -74,8 +74,8 @@ __global__ __launch_bounds__(WAVES* kWave) void k_gated_slope(gd_gated_grad io, 
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             zg.v[j] = (T)dg[j];
-            // a unit that ReLU turns off passes nothing, a gradient that is not finite neither
-            zu.v[j] = (T)(act == GD_ACT_RELU && !(g[j] > 0.0f) ? 0.0f : (float)dy.v[j] * a[j]);
+            // a unit that ReLU turns off passes nothing, a gradient that is not finite neither; NaN is not turned off
+            zu.v[j] = (T)(act == GD_ACT_RELU && g[j] <= 0.0f ? 0.0f : (float)dy.v[j] * a[j]);
             sum_g[j] += (float)zg.v[j];
             sum_u[j] += (float)zu.v[j];
         }

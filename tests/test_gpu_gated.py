@@ -268,6 +268,20 @@ def test_relu_turns_units_off():
 
 
 @gpu
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+def test_a_gate_that_is_nan_passes_nan(act, kind):
+    """dz of what is gated is dy act(NaN), in the place of the NaN alone."""
+    op = gd.GatedLinear(2, 11, kind, act, max_rows=2)
+    pre, dy = draw(1, 2, 22, dtype=kind), draw(2, 2, 11, dtype=kind)
+    pre[1, 9] = math.nan
+    dz = op.backward(dy, draw(3, 2, 2, dtype=kind), draw(4, 22, 2, dtype=kind), pre)[3]
+    gated = torch.zeros(2, 11, dtype=torch.bool, device="cuda")
+    gated[1, 9] = True
+    assert torch.equal(dz[:, 11:].isnan(), gated) and not bool((dz[:, :11].isnan() & ~gated).any())
+
+
+@gpu
 def test_no_rows_another_stream_and_graph_replays():
     rows, k, n = 300, 256, 192
     t = torch.bfloat16
