@@ -1265,6 +1265,8 @@ class TokenLogProbs(_Scores):
                 out: Optional[LogProbs] = None, stream=None):
         """LogProbs; ``top`` up to 64 alternatives, of equal logits the lower id first; ``keep_stats`` for backward.
         ``out``: one of an earlier call of the same shape and wishes, to write again."""
+        if not 0 <= top < 1 << 32:
+            raise GDError(1, "gd_logprob_forward")
         io = _LogProbIO()
         rows = self._logits(io, logits)
         io.tokens, io.index = _ids_on(self.device.index, tokens, "tokens", rows)

@@ -456,3 +456,10 @@ def test_refusals():
                 lambda: op.forward_backward(x.clone().requires_grad_(), tokens, g)):
         with pytest.raises(RuntimeError):
             bad()
+
+
+@pytest.mark.parametrize("top", [-1, 1 << 32, (1 << 32) + 1])
+def test_refuses_a_number_of_alternatives_past_its_type(top):
+    op = gd.TokenLogProbs(50, torch.float32, max_rows=2)
+    with pytest.raises(gd.GDError):
+        op.forward(draw(1, 2, 50), ids_of(2, 50, 2), top=top)
