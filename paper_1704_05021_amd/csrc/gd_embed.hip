@@ -82,6 +82,50 @@ __device__ __forceinline__ void put_gradient(float* out, const float (&s)[N], fl
     store_some<N>(out, v, n);
 }
 
+// The columns of a row from c on that a lane takes, a 16-byte vector of dy.  Where the row ends inside it, the vector is
+// the one that ends with the row, and what it shares with the lane before is left out.  So every load is made, by every
+// lane: loads behind conditions wait for one another (14,003 rows of 237 in float16 took
+// 26 us so, now 18).
+template <typename T, bool SHORT>  // SHORT: dim is below a vector, and read element by element
+struct Columns {
+    static constexpr int E = 16 / sizeof(T);
+    uint32_t at, dim, skip;  // skip: elements of the vector that are not the lane's
+    __device__ __forceinline__ Columns(uint32_t c, uint32_t dim) : dim(dim) {
+        at = SHORT ? 0 : min(c, dim - E);
+        skip = min(c - at, (uint32_t)E);
+    }
+    __device__ __forceinline__ u4 load(const T* row) const {
+        Pack<T, E> r;
+        if constexpr (SHORT) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) r.v[j] = row[min((uint32_t)j, dim - 1)];
+        } else {
+            r = load_pack<E>(row + at);
+        }
+        u4 w;  // as words: elements would be taken apart behind the load, and waited for
+        __builtin_memcpy(&w, &r, sizeof w);
+        return w;
+    }
+    static __device__ __forceinline__ void add(float (&sum)[E], const u4& w) {
+        Pack<T, E> r;
+        __builtin_memcpy(&r, &w, sizeof w);
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] += (float)r.v[j];
+    }
+    __device__ __forceinline__ void put(float* row, const float (&s)[E], float scale, bool accumulate) const {
+        if (!SHORT && skip == 0) {
+            put_gradient<E>(row + at, s, scale, E, accumulate);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if ((uint32_t)j >= skip && (!SHORT || (uint32_t)j < dim)) {
+                float* const to = row + at + j;
+                *to = accumulate ? *to + scale * s[j] : scale * s[j];
+            }
+    }
+};
+
 // ---- Few rows: all of it in one launch ----
 //
 // A block takes a row and looks through all tokens for its own: the first row
@@ -97,7 +141,7 @@ constexpr uint32_t kFewRows = 4096, kFewThreads = 512, kFewWaves = kFewThreads /
 constexpr uint32_t kFillFloats = 16384;  // of zeros that a block writes, about
 constexpr uint32_t kFewBlocks = 1u << 22;
 
-template <typename T>
+template <typename T, bool SHORT>
 __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uint32_t vocab, uint32_t dim, bool wide,
                                                            uint32_t fills, uint32_t per_fill) {
     constexpr int E = 16 / sizeof(T), kSlice = kWave * E;
@@ -151,48 +195,52 @@ __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uin
             list[place] = (uint16_t)(lane * kWave + (uint32_t)__ffsll((unsigned long long)mine) - 1);
     __syncthreads();
     float* out = io.dweight + (uint64_t)token * io.dweight_stride;
-    // rows first to first + kFewAtOnce of the list, columns c on, n of which exist
-    const auto add = [&](uint32_t first, uint32_t c, int n, float (&sum)[E]) {
-        Pack<T, E> d[kFewAtOnce];
+    typedef Columns<T, SHORT> Cols;
+    // the sum of rows first to first + kFewAtOnce of the list
+    const auto add = [&](uint32_t first, const Cols& cols, float (&sum)[E]) {
+        u4 d[kFewAtOnce];
 #pragma unroll
         for (uint32_t k = 0; k < kFewAtOnce; ++k)
-            d[k] = load_some<E>((const T*)io.dy + (uint64_t)list[min(first + k, count - 1)] * io.dy_stride + c, first + k < count ? n : 0);
+            d[k] = cols.load((const T*)io.dy + (uint64_t)list[min(first + k, count - 1)] * io.dy_stride);
 #pragma unroll
         for (int j = 0; j < E; ++j) sum[j] = 0.0f;
 #pragma unroll
         for (uint32_t k = 0; k < kFewAtOnce; ++k)
-#pragma unroll
-            for (int j = 0; j < E; ++j) sum[j] += (float)d[k].v[j];
+            if (first + k < count) Cols::add(sum, d[k]);
     };
     if (count <= kFewAtOnce) {  // a wave takes a slice of the columns
         for (uint32_t s = wave * kSlice; s < dim; s += kFewWaves * kSlice) {
-            const uint32_t c = min(s + lane * E, dim);
+            const Cols cols(s + lane * E, dim);
             float sum[E];
-            add(0, c, (int)(dim - c), sum);
-            put_gradient<E>(out + c, sum, io.scale, (int)(dim - c), io.accumulate != 0);
+            add(0, cols, sum);
+            cols.put(out, sum, io.scale, io.accumulate != 0);
         }
         return;
     }
     for (uint32_t s = 0; s < dim; s += kSlice) {  // the waves share the rows
-        const uint32_t c = min(s + lane * E, dim);
+        const Cols cols(s + lane * E, dim);
         double total[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) total[j] = 0.0;
         for (uint32_t first = wave * kFewAtOnce; first < count; first += kFewWaves * kFewAtOnce) {
             float sum[E];
-            add(first, c, (int)(dim - c), sum);
+            add(first, cols, sum);
 #pragma unroll
             for (int j = 0; j < E; ++j) total[j] += sum[j];
         }
 #pragma unroll
-        for (int j = 0; j < E; ++j) shares[wave][lane * E + j] = (float)total[j];
+        for (int j = 0; j < E; ++j) shares[wave][j * kWave + lane] = (float)total[j];
         __syncthreads();
-        for (uint32_t j = threadIdx.x; j < (uint32_t)kSlice && s + j < dim; j += kFewThreads) {
-            double v = 0.0;
+        if (wave == 0) {
+            float sum[E];
 #pragma unroll
-            for (uint32_t w = 0; w < kFewWaves; ++w) v += shares[w][j];
-            const float sum[1] = {(float)v};
-            put_gradient<1>(out + s + j, sum, io.scale, 1, io.accumulate != 0);
+            for (int j = 0; j < E; ++j) {
+                double v = 0.0;
+#pragma unroll
+                for (uint32_t w = 0; w < kFewWaves; ++w) v += shares[w][j * kWave + lane];
+                sum[j] = (float)v;
+            }
+            cols.put(out, sum, io.scale, io.accumulate != 0);
         }
         __syncthreads();
     }
@@ -200,15 +248,15 @@ __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uin
 
 // ---- More rows ----
 
-// Zeros over [rows][dim] at `stride`, shared by `blocks` blocks of kSortThreads, a 16-byte vector a thread and turn.  There are
+// Zeros over [rows][dim] at `stride`, shared by `blocks` blocks, a 16-byte vector a thread and turn.  There are
 // as many blocks as such turns, up to kFillBlocks: 85,000 x 500 take 26 us so, 34 with 512 blocks that go round.
 constexpr uint32_t kFillBlocks = 1u << 20;
 __device__ __forceinline__ void fill_zeros(float* out, uint32_t rows, uint32_t dim, uint64_t stride, uint32_t block, uint32_t blocks) {
     const Pack<float, 4> zeros = {};
-    const uint32_t per_row = (dim + 3) / 4;
+    const uint32_t per_row = (dim + 3) / 4, threads = blockDim.x;
     const bool one_run = stride == dim;
     const uint64_t all = one_run ? (uint64_t)rows * dim : (uint64_t)rows * per_row;
-    for (uint64_t v = (uint64_t)block * kSortThreads + threadIdx.x; one_run ? v * 4 < all : v < all; v += (uint64_t)blocks * kSortThreads) {
+    for (uint64_t v = (uint64_t)block * threads + threadIdx.x; one_run ? v * 4 < all : v < all; v += (uint64_t)blocks * threads) {
         if (one_run) {
             store_stream<4>(out + v * 4, zeros, (int)min(all - v * 4, (uint64_t)4));
         } else {
@@ -218,8 +266,8 @@ __device__ __forceinline__ void fill_zeros(float* out, uint32_t rows, uint32_t d
         }
     }
 }
-uint32_t fill_blocks(uint32_t rows, uint32_t dim) {
-    return (uint32_t)std::min<uint64_t>(((uint64_t)rows * ((dim + 3ull) / 4) + kSortThreads - 1) / kSortThreads, kFillBlocks);
+uint32_t fill_blocks(uint32_t rows, uint32_t dim, uint32_t threads) {
+    return (uint32_t)std::min<uint64_t>(((uint64_t)rows * ((dim + 3ull) / 4) + threads - 1) / threads, kFillBlocks);
 }
 
 // Sorts chunks of 4,096 rows by (token, row): an element's place is the number
@@ -270,13 +318,14 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(gd_embed_grad io, u
 // The sorted chunks in one order: an element's place is the number of smaller
 // ones, a binary search in each other chunk, four of them at a time.  Blocks
 // from `ranks` on write zeros over `fill` rows.
-__global__ __launch_bounds__(kSortThreads) void k_embed_rank(const uint64_t* chunk, uint32_t rows, uint32_t chunks, uint64_t* order,
+constexpr uint32_t kRankThreads = 256;
+__global__ __launch_bounds__(kRankThreads) void k_embed_rank(const uint64_t* chunk, uint32_t rows, uint32_t chunks, uint64_t* order,
                                                        uint32_t ranks, float* out, uint32_t fill, uint32_t dim, uint64_t stride) {
     if (blockIdx.x >= ranks) {
         fill_zeros(out, fill, dim, stride, blockIdx.x - ranks, gridDim.x - ranks);
         return;
     }
-    const uint32_t i = blockIdx.x * kSortThreads + threadIdx.x;
+    const uint32_t i = blockIdx.x * kRankThreads + threadIdx.x;
     if (i >= rows) return;
     const uint64_t key = chunk[i];
     const uint32_t own = i / kSortChunk;
@@ -301,63 +350,57 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_rank(const uint64_t* chu
 // A wave adds up one unit of the sorted rows, a slice of 64 vectors of columns:
 // a run of equal tokens that lies within the unit goes to dweight, one that
 // began before it to part[2 unit], one that begins in it and goes on behind it
-// to part[2 unit + 1].
+// to part[2 unit + 1].  A lane reads the key of one row, and the rows' loads,
+// each group's while the one before is added up, take it from there.
 constexpr int kSumWaves = 4, kSumAtOnce = 8;
-template <typename T>
+template <typename T, bool SHORT>
 __global__ __launch_bounds__(kSumWaves* kWave) void k_embed_sum(gd_embed_grad io, const uint64_t* order, uint32_t unit,
                                                                 uint32_t units, uint32_t dim, float* part) {
-    constexpr int E = 16 / sizeof(T);
+    typedef Columns<T, SHORT> Cols;
+    constexpr int E = Cols::E;
     const uint32_t u = blockIdx.x * kSumWaves + wave_index();
     if (u >= units) return;
-    const uint32_t c = min(blockIdx.y * (kWave * E) + (uint32_t)lane_id() * E, dim);
-    const int n = (int)(dim - c);
-    const uint64_t begin = (uint64_t)u * unit, end = min(begin + unit, io.rows);
-    const auto token = [&](uint64_t i) { return (uint32_t)(order[i] >> 32); };
-    const bool joins = begin && token(begin - 1) == token(begin);        // the first run began before the unit
-    const bool goes_on = end < io.rows && token(end) == token(end - 1);  // the last run goes on behind it
+    const uint32_t begin = u * unit, rows = (uint32_t)io.rows, n = min(unit, rows - begin);
+    const uint64_t key = order[begin + min((uint32_t)lane_id(), n - 1)];
+    const uint32_t key_token = (uint32_t)(key >> 32), key_row = (uint32_t)key;
+    const uint32_t ahead = (uint32_t)(order[begin - (begin != 0)] >> 32), behind = (uint32_t)(order[min(begin + n, rows - 1)] >> 32);
+    const Cols cols(blockIdx.y * (kWave * E) + (uint32_t)lane_id() * E, dim);
+    const auto load = [&](u4 (&d)[kSumAtOnce], uint32_t i) {
+#pragma unroll
+        for (int k = 0; k < kSumAtOnce; ++k)
+            d[k] = cols.load((const T*)io.dy + (uint64_t)lane_value(key_row, (int)min(i + k, n - 1)) * io.dy_stride);
+    };
+    u4 next[kSumAtOnce];
+    load(next, 0);
+    uint32_t run = lane_value(key_token, 0);
+    const bool joins = begin && ahead == run;                                                       // the first run began before
+    const bool goes_on = begin + n < rows && behind == lane_value(key_token, (int)n - 1);  // the last run goes on behind
     float sum[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) sum[j] = 0.0f;
-    uint32_t run = token(begin);
     bool first = true;
     const auto flush = [&](bool last) {
         if (run == kNoToken) return;
-        float* shares = part + (uint64_t)u * 2 * dim + c;
-        if (first && joins) {
-            Pack<float, E> v;
-#pragma unroll
-            for (int j = 0; j < E; ++j) v.v[j] = sum[j];
-            store_some<E>(shares, v, n);
-        } else if (last && goes_on) {
-            Pack<float, E> v;
-#pragma unroll
-            for (int j = 0; j < E; ++j) v.v[j] = sum[j];
-            store_some<E>(shares + dim, v, n);
-        } else {
-            put_gradient<E>(io.dweight + (uint64_t)run * io.dweight_stride + c, sum, io.scale, n, io.accumulate != 0);
-        }
+        const bool share = first && joins, open = !share && last && goes_on;
+        float* const to = share || open ? part + ((uint64_t)u * 2 + open) * dim : io.dweight + (uint64_t)run * io.dweight_stride;
+        cols.put(to, sum, share || open ? 1.0f : io.scale, !(share || open) && io.accumulate != 0);
     };
-    for (uint64_t i = begin; i < end; i += kSumAtOnce) {
-        uint32_t t[kSumAtOnce];
-        Pack<T, E> d[kSumAtOnce];
+    for (uint32_t i = 0; i < n; i += kSumAtOnce) {
+        u4 d[kSumAtOnce];
+#pragma unroll
+        for (int k = 0; k < kSumAtOnce; ++k) d[k] = next[k];
+        if (i + kSumAtOnce < n) load(next, i + kSumAtOnce);
 #pragma unroll
         for (int k = 0; k < kSumAtOnce; ++k) {
-            const uint64_t key = order[min(i + k, end - 1)];
-            t[k] = (uint32_t)(key >> 32);
-            d[k] = load_some<E>((const T*)io.dy + (uint64_t)(uint32_t)key * io.dy_stride + c,
-                                i + k < end && t[k] != kNoToken ? n : 0);
-        }
-#pragma unroll
-        for (int k = 0; k < kSumAtOnce; ++k) {
-            if (i + k >= end) break;
-            if (t[k] != run) {
+            if (i + k >= n) break;
+            const uint32_t t = lane_value(key_token, (int)(i + k));
+            if (t != run) {
                 flush(false);
-                run = t[k], first = false;
+                run = t, first = false;
 #pragma unroll
                 for (int j = 0; j < E; ++j) sum[j] = 0.0f;
             }
-#pragma unroll
-            for (int j = 0; j < E; ++j) sum[j] += (float)d[k].v[j];
+            Cols::add(sum, d[k]);
         }
     }
     flush(true);
@@ -374,11 +417,12 @@ __global__ __launch_bounds__(kRunWaves* kWave) void k_embed_join(gd_embed_grad i
     const uint32_t run = token((uint64_t)u * unit + unit - 1);
     if (run == kNoToken || token((uint64_t)(u + 1) * unit) != run) return;       // it ends with the unit
     if (u && token((uint64_t)u * unit - 1) == run) return;                       // it began before
-    uint32_t last = u + 1, past = units;                                          // the last unit that it reaches
+    uint32_t last = u + 1, past = units;  // the last unit that it reaches, 64 looked at in turn
     while (past - last > 1) {
-        const uint32_t mid = last + (past - last) / 2;
-        if (token((uint64_t)mid * unit) == run) last = mid;
-        else past = mid;
+        const uint32_t step = (past - last - 1 + kWave - 1) / kWave, mid = last + (lane_id() + 1) * step;
+        const uint64_t within = ballot(mid < past && token((uint64_t)min(mid, past - 1) * unit) == run);
+        last += popc64(within) * step;
+        past = min(past, last + step);
     }
     const uint32_t c = min(blockIdx.y * (kWave * 4) + (uint32_t)lane_id() * 4, dim);
     const int n = (int)(dim - c);
@@ -500,8 +544,10 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
     const uint64_t fills = io->accumulate ? 0 : ((uint64_t)e->vocab + per_fill - 1) / per_fill;
     if (io->rows <= gd::kFewRows && io->rows * e->dim <= gd::kFewWork && fills <= gd::kFewBlocks) {
         const hipError_t r = gd::with_type(e->type, [&](auto zero) {
-            gd::k_embed_few<decltype(zero)><<<dim3((uint32_t)(io->rows + fills)), dim3(gd::kFewThreads), 0, st>>>(
-                *io, e->vocab, e->dim, wide == GD_I64, (uint32_t)fills, per_fill);
+            using T = decltype(zero);
+            const auto kernel = e->dim * sizeof(T) < 16 ? gd::k_embed_few<T, true> : gd::k_embed_few<T, false>;
+            kernel<<<dim3((uint32_t)(io->rows + fills)), dim3(gd::kFewThreads), 0, st>>>(*io, e->vocab, e->dim, wide == GD_I64,
+                                                                                          (uint32_t)fills, per_fill);
             return hipGetLastError();
         });
         return r == hipSuccess ? GD_OK : GD_ERR_HIP;
@@ -511,14 +557,14 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
     // launches waits on memory for some microseconds, of which the zeros need not be waited for.
     const uint32_t first = io->accumulate ? 0 : chunks > 1 ? e->vocab / 4 : e->vocab, rest = io->accumulate ? 0 : e->vocab - first;
     const uint32_t sorts = chunks * gd::kChunkBlocks;
-    gd::k_embed_sort<<<dim3(sorts + gd::fill_blocks(first, e->dim)), dim3(gd::kSortThreads), 0, st>>>(
+    gd::k_embed_sort<<<dim3(sorts + gd::fill_blocks(first, e->dim, gd::kSortThreads)), dim3(gd::kSortThreads), 0, st>>>(
         *io, e->vocab, e->dim, wide == GD_I64, sorts, chunks > 1 ? e->chunk : e->order, first);
     hipError_t r = hipGetLastError();
     if (r != hipSuccess) return GD_ERR_HIP;
     if (!io->rows) return GD_OK;
     if (chunks > 1) {
-        const uint32_t ranks = (uint32_t)((io->rows + gd::kSortThreads - 1) / gd::kSortThreads);
-        gd::k_embed_rank<<<dim3(ranks + gd::fill_blocks(rest, e->dim)), dim3(gd::kSortThreads), 0, st>>>(
+        const uint32_t ranks = (uint32_t)((io->rows + gd::kRankThreads - 1) / gd::kRankThreads);
+        gd::k_embed_rank<<<dim3(ranks + gd::fill_blocks(rest, e->dim, gd::kRankThreads)), dim3(gd::kRankThreads), 0, st>>>(
             e->chunk, (uint32_t)io->rows, chunks, e->order, ranks, io->dweight + (uint64_t)first * io->dweight_stride, rest, e->dim,
             io->dweight_stride);
         if (hipGetLastError() != hipSuccess) return GD_ERR_HIP;
@@ -527,8 +573,9 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
     r = gd::with_type(e->type, [&](auto zero) {
         using T = decltype(zero);
         constexpr uint32_t kColumns = gd::kWave * 16 / sizeof(T);
-        gd::k_embed_sum<T><<<dim3((units + gd::kSumWaves - 1) / gd::kSumWaves, (e->dim + kColumns - 1) / kColumns),
-                             dim3(gd::kSumWaves * gd::kWave), 0, st>>>(*io, e->order, unit, units, e->dim, e->part);
+        const auto kernel = e->dim * sizeof(T) < 16 ? gd::k_embed_sum<T, true> : gd::k_embed_sum<T, false>;
+        kernel<<<dim3((units + gd::kSumWaves - 1) / gd::kSumWaves, (e->dim + kColumns - 1) / kColumns),
+                 dim3(gd::kSumWaves * gd::kWave), 0, st>>>(*io, e->order, unit, units, e->dim, e->part);
         return hipGetLastError();
     });
     if (r != hipSuccess) return GD_ERR_HIP;
