@@ -331,11 +331,11 @@ typedef enum {
  * A token outside [0, vocab) is padding: its row of y is zeros, and its row of
  * dy is not read.  dweight is written whole, rows of tokens that do not occur
  * with zeros.  A token's rows are summed in their order, in binary32 within
- * 8 to 64 of them and in 64 bits across those.
+ * 8 to 32 of them and in 64 bits across those.
  * gd_embed_create plans a vocabulary (1..2^31 - 1) of rows of dim (1..2^20)
  * elements in `type` on the current device, for backward calls of at most
  * max_rows (up to 2^24) rows, and allocates 16 bytes per row of those and
- * 8 dim bytes per 64 of them (per 8 up to the 4,096th) as scratch.  The
+ * 8 dim bytes per 32 of them (per 8 up to some 6 MB) as scratch.  The
  * forward call takes any number of rows.
  */
 typedef struct gd_embed gd_embed;

@@ -29,19 +29,45 @@ constexpr uint32_t kPadding = 0x7FFFFFFFu;  // what stands for it where tokens a
 constexpr uint32_t kSortChunk = 4096, kSortThreads = 1024;
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-// Sorted rows a unit holds, by the number of rows: few rows make many small units for the sake of parallel work, many
-// make larger ones, of which fewer partial sums are written (3,000 rows of 500 in binary32 for 85,000 words, sorted: units
-// of 8 took 5 us less than units of 16).
-__host__ __device__ constexpr uint32_t unit_rows(uint64_t rows) { return rows <= 4096 ? 8 : rows <= 16384 ? 32 : 64; }
-constexpr uint64_t unit_count(uint64_t rows) { return (rows + unit_rows(rows) - 1) / unit_rows(rows); }
-// The most units that any number of rows up to this one makes.
-constexpr uint64_t most_units(uint64_t rows) { return std::max<uint64_t>(std::min<uint64_t>((rows + 7) / 8, 512), (rows + 63) / 64); }
-static_assert(unit_count(4096) == 512 && unit_count(16384) == 512 && unit_count(16385) == 257);
+// Sorted rows a unit holds: as many, up to 32, as leave three waves a compute unit, each with a slice of 64 vectors of a
+// unit's columns.  Few short rows make many small units for the sake of parallel work (14,003 rows of 237 in float16 with
+// units of 16 and 32: 40 and 46 us), many or long ones larger, of which fewer partial sums are written (16,384 of 1024 in
+// bfloat16: 54 and 51; with 64 8,192 of 4096 take 120 us in place of 118, and 200,000 of 256 301 in place of 310).
+constexpr uint64_t kUnitWaves = 768;
+constexpr uint32_t slice_count(uint32_t dim, int type) {
+    const uint32_t columns = kWave * 16 / (type == GD_F32 ? 4 : 2);
+    return (dim + columns - 1) / columns;
+}
+constexpr uint32_t unit_rows(uint64_t rows, uint32_t slices) {
+    uint32_t unit = 32;
+    while (unit > 8 && (rows + unit - 1) / unit * slices < kUnitWaves) unit /= 2;
+    return unit;
+}
+// No number of rows up to this one makes more units: where units are below 32, twice their rows made fewer than kUnitWaves waves.
+constexpr uint64_t most_units(uint64_t rows, uint32_t slices) {
+    return std::max<uint64_t>(std::min<uint64_t>((rows + 7) / 8, 2 * kUnitWaves / slices), (rows + 31) / 32);
+}
 
 // The token of row i: kNoToken for ids outside the vocabulary.
 __device__ __forceinline__ uint32_t token_at(const void* tokens, bool wide, uint64_t i, uint32_t vocab) {
     const int64_t t = wide ? ((const int64_t*)tokens)[i] : (int64_t)((const int32_t*)tokens)[i];
     return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : kNoToken;
+}
+
+// The tokens of rows i, i + step and so on, past the last row that one again.  All loads before the first use.
+template <int N>
+__device__ __forceinline__ void tokens_at(const void* tokens, bool wide, uint64_t i, uint64_t step, uint64_t rows, uint32_t vocab,
+                                          uint32_t (&out)[N]) {
+    int64_t t[N];
+    if (wide) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) t[k] = ((const int64_t*)tokens)[min(i + k * step, rows - 1)];
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) t[k] = ((const int32_t*)tokens)[min(i + k * step, rows - 1)];
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) out[k] = t[k] >= 0 && t[k] < (int64_t)vocab ? (uint32_t)t[k] : kNoToken;
 }
 
 // y[i] = scale weight[t_i]: LANES lanes a row, VECS 16-byte vectors a lane at a time.
@@ -176,9 +202,7 @@ __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uin
     const uint32_t token = token_at(io.tokens, wide, i, vocab);
     if (token == kNoToken) return;
     uint32_t others[kFewRows / kFewThreads];
-#pragma unroll
-    for (uint32_t k = 0; k < kFewRows / kFewThreads; ++k)  // past the last row that one again
-        others[k] = token_at(io.tokens, wide, min(k * kFewThreads + threadIdx.x, rows - 1), vocab);
+    tokens_at(io.tokens, wide, threadIdx.x, kFewThreads, rows, vocab, others);
 #pragma unroll
     for (uint32_t k = 0; k < kFewRows / kFewThreads; ++k) {
         const uint64_t m = ballot(others[k] == token && k * kFewThreads + threadIdx.x < rows);
@@ -286,8 +310,13 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(gd_embed_grad io, u
     __shared__ uint32_t counts[kSortWaves][kWave];
     const uint64_t first = (uint64_t)(blockIdx.x / kChunkBlocks) * kSortChunk;
     const uint32_t n = (uint32_t)min(io.rows - first, (uint64_t)kSortChunk), padded = (n + kWave - 1) / kWave * kWave;
-    for (uint32_t i = threadIdx.x; i < padded; i += kSortThreads)
-        lds[i] = i < n ? min(token_at(io.tokens, wide, first + i, vocab), kPadding) : 0xFFFFFFFFu;
+    uint32_t tokens[kSortChunk / kSortThreads];
+    tokens_at(io.tokens, wide, first + threadIdx.x, kSortThreads, io.rows, vocab, tokens);
+#pragma unroll
+    for (uint32_t k = 0; k < kSortChunk / kSortThreads; ++k) {
+        const uint32_t i = k * kSortThreads + threadIdx.x;
+        lds[i] = i < n ? min(tokens[k], kPadding) : 0xFFFFFFFFu;
+    }
     __syncthreads();
     const uint32_t i0 = blockIdx.x % kChunkBlocks * kWave, i = i0 + lane_id();
     if (i0 >= n) return;
@@ -316,8 +345,8 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(gd_embed_grad io, u
 }
 
 // The sorted chunks in one order: an element's place is the number of smaller
-// ones, a binary search in each other chunk, four of them at a time.  Blocks
-// from `ranks` on write zeros over `fill` rows.
+// ones, a search in each other chunk, four chunks at a time and eight places in
+// each (by halves 14,003 rows took 4 us more).  Blocks from `ranks` on write zeros over `fill` rows.
 constexpr uint32_t kRankThreads = 256;
 __global__ __launch_bounds__(kRankThreads) void k_embed_rank(const uint64_t* chunk, uint32_t rows, uint32_t chunks, uint64_t* order,
                                                        uint32_t ranks, float* out, uint32_t fill, uint32_t dim, uint64_t stride) {
@@ -330,17 +359,30 @@ __global__ __launch_bounds__(kRankThreads) void k_embed_rank(const uint64_t* chu
     const uint64_t key = chunk[i];
     const uint32_t own = i / kSortChunk;
     uint32_t rank = i % kSortChunk;
-    constexpr int kAtOnce = 4;
+    constexpr int kAtOnce = 4, kWays = 8;
     for (uint32_t c = 0; c < chunks; c += kAtOnce) {
         uint32_t at[kAtOnce] = {}, len[kAtOnce];
+        const uint64_t* in[kAtOnce];
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k)
+        for (int k = 0; k < kAtOnce; ++k) {
             len[k] = c + k < chunks && c + k != own ? min(rows - (c + k) * kSortChunk, kSortChunk) : 0;
+            in[k] = len[k] ? chunk + (c + k) * kSortChunk : chunk;
+        }
 #pragma unroll
-        for (uint32_t step = kSortChunk; step; step /= 2)
+        for (uint32_t step = kSortChunk / kWays; step; step /= kWays) {
+            uint64_t other[kAtOnce][kWays];
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k)
-                if (at[k] + step <= len[k] && chunk[(c + k) * kSortChunk + at[k] + step - 1] < key) at[k] += step;
+#pragma unroll
+                for (uint32_t w = 0; w < kWays; ++w) other[k][w] = in[k][min(at[k] + (w + 1) * step, max(len[k], 1u)) - 1];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                uint32_t before = 0;
+#pragma unroll
+                for (uint32_t w = 0; w < kWays; ++w) before += (at[k] + (w + 1) * step <= len[k]) & (other[k][w] < key);
+                at[k] += before * step;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) rank += at[k];
     }
@@ -360,10 +402,12 @@ __global__ __launch_bounds__(kSumWaves* kWave) void k_embed_sum(gd_embed_grad io
     constexpr int E = Cols::E;
     const uint32_t u = blockIdx.x * kSumWaves + wave_index();
     if (u >= units) return;
-    const uint32_t begin = u * unit, rows = (uint32_t)io.rows, n = min(unit, rows - begin);
-    const uint64_t key = order[begin + min((uint32_t)lane_id(), n - 1)];
+    const uint32_t begin = u * unit, rows = (uint32_t)io.rows, all = min(unit, rows - begin);
+    const uint64_t key = order[begin + min((uint32_t)lane_id(), all - 1)];
     const uint32_t key_token = (uint32_t)(key >> 32), key_row = (uint32_t)key;
-    const uint32_t ahead = (uint32_t)(order[begin - (begin != 0)] >> 32), behind = (uint32_t)(order[min(begin + n, rows - 1)] >> 32);
+    const uint32_t ahead = (uint32_t)(order[begin - (begin != 0)] >> 32), behind = (uint32_t)(order[min(begin + all, rows - 1)] >> 32);
+    const uint32_t n = min((uint32_t)popc64(ballot(key_token != kNoToken)), all);  // padding is behind all others
+    if (n == 0) return;
     const Cols cols(blockIdx.y * (kWave * E) + (uint32_t)lane_id() * E, dim);
     const auto load = [&](u4 (&d)[kSumAtOnce], uint32_t i) {
 #pragma unroll
@@ -373,14 +417,13 @@ __global__ __launch_bounds__(kSumWaves* kWave) void k_embed_sum(gd_embed_grad io
     u4 next[kSumAtOnce];
     load(next, 0);
     uint32_t run = lane_value(key_token, 0);
-    const bool joins = begin && ahead == run;                                                       // the first run began before
-    const bool goes_on = begin + n < rows && behind == lane_value(key_token, (int)n - 1);  // the last run goes on behind
+    const bool joins = begin && ahead == run;  // the first run began before
+    const bool goes_on = n == all && begin + n < rows && behind == lane_value(key_token, (int)n - 1);  // the last run goes on
     float sum[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) sum[j] = 0.0f;
     bool first = true;
     const auto flush = [&](bool last) {
-        if (run == kNoToken) return;
         const bool share = first && joins, open = !share && last && goes_on;
         float* const to = share || open ? part + ((uint64_t)u * 2 + open) * dim : io.dweight + (uint64_t)run * io.dweight_stride;
         cols.put(to, sum, share || open ? 1.0f : io.scale, !(share || open) && io.accumulate != 0);
@@ -414,9 +457,9 @@ __global__ __launch_bounds__(kRunWaves* kWave) void k_embed_join(gd_embed_grad i
     __shared__ double lds[kRunWaves][kWave * 4];
     const uint32_t u = blockIdx.x;
     const auto token = [&](uint64_t i) { return (uint32_t)(order[i] >> 32); };
-    const uint32_t run = token((uint64_t)u * unit + unit - 1);
-    if (run == kNoToken || token((uint64_t)(u + 1) * unit) != run) return;       // it ends with the unit
-    if (u && token((uint64_t)u * unit - 1) == run) return;                       // it began before
+    const uint64_t begin = (uint64_t)u * unit;
+    const uint32_t run = token(begin + unit - 1), behind = token(begin + unit), ahead = token(begin - (u != 0));
+    if (run == kNoToken || behind != run || (u && ahead == run)) return;  // it ends with the unit, or began before it
     uint32_t last = u + 1, past = units;  // the last unit that it reaches, 64 looked at in turn
     while (past - last > 1) {
         const uint32_t step = (past - last - 1 + kWave - 1) / kWave, mid = last + (lane_id() + 1) * step;
@@ -498,7 +541,7 @@ gd_status gd_embed_create(gd_embed** out, uint32_t vocab, uint32_t dim, gd_dtype
     try {
         if (hipGetDevice(&e->device) != hipSuccess) st = GD_ERR_HIP;
         else if (!e->mem.alloc(&e->chunk, max_rows) || !e->mem.alloc(&e->order, max_rows) ||
-                 !e->mem.alloc(&e->part, gd::most_units(max_rows) * 2 * dim))
+                 !e->mem.alloc(&e->part, gd::most_units(max_rows, gd::slice_count(dim, ty)) * 2 * dim))
             st = GD_ERR_OOM;
     } catch (const std::bad_alloc&) {
         st = GD_ERR_OOM;
@@ -569,12 +612,12 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
             io->dweight_stride);
         if (hipGetLastError() != hipSuccess) return GD_ERR_HIP;
     }
-    const uint32_t unit = gd::unit_rows(io->rows), units = (uint32_t)gd::unit_count(io->rows);
+    const uint32_t slices = gd::slice_count(e->dim, e->type), unit = gd::unit_rows(io->rows, slices);
+    const uint32_t units = (uint32_t)((io->rows + unit - 1) / unit);
     r = gd::with_type(e->type, [&](auto zero) {
         using T = decltype(zero);
-        constexpr uint32_t kColumns = gd::kWave * 16 / sizeof(T);
         const auto kernel = e->dim * sizeof(T) < 16 ? gd::k_embed_sum<T, true> : gd::k_embed_sum<T, false>;
-        kernel<<<dim3((units + gd::kSumWaves - 1) / gd::kSumWaves, (e->dim + kColumns - 1) / kColumns),
+        kernel<<<dim3((units + gd::kSumWaves - 1) / gd::kSumWaves, slices),
                  dim3(gd::kSumWaves * gd::kWave), 0, st>>>(*io, e->order, unit, units, e->dim, e->part);
         return hipGetLastError();
     });

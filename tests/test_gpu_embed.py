@@ -73,8 +73,8 @@ def test_over_sizes(kind, index, rows, vocab, dim):
         check_backward(dw, dy, tokens, vocab, 1.5, rows, f"{kind} {rows} {vocab} {dim} {how}")
 
 
-# one launch up to 4,096 rows; sorted: units of 8, 32 and 64 rows (8 where rows are long), one chunk of 4,096 and several,
-# the last one full or of one row; runs over many units
+# one launch up to 4,096 rows; sorted: units of 8 to 32 rows, one chunk of 4,096 and several, the last one full or of one
+# row; runs over many units
 @pytest.mark.parametrize("how", ["text", "one", "each", "pairs", "padded"])
 @pytest.mark.parametrize("rows,dim", [(7, 20), (8, 20), (9, 20), (15, 20), (16, 20), (17, 300), (2048, 24), (2049, 24), (4096, 12), (4097, 12), (6144, 260), (257, 8200), (2049, 1040), (4096, 520), (8192, 8),
                                       (16384, 5), (16385, 5), (30001, 9)])
@@ -95,6 +95,28 @@ def test_backward_of_few_long_rows(how, rows):
     tokens, dy = words(5, rows, vocab, how), draw(6, rows, dim)
     dw = gd.Embedding(vocab, dim, torch.float32, max_rows=rows).backward(dy, tokens)
     check_backward(dw, dy, tokens, vocab, 1.0, rows, f"{how} {rows}")
+
+
+@pytest.mark.parametrize("how", ["text", "one", "padded"])
+@pytest.mark.parametrize("dim", [3, 8, 261])
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+def test_runs_over_very_many_units(kind, dim, how):
+    """More units than 64 times 64, which the search for a run's end takes in steps of."""
+    rows, vocab, t = 140_001, 300, TYPES[kind]
+    tokens, dy = words(5, rows, vocab, how), draw(6, rows, dim, dtype=t)
+    dw = gd.Embedding(vocab, dim, t, max_rows=rows).backward(dy, tokens)
+    check_backward(dw, dy, tokens, vocab, 1.0, rows, f"{kind} {dim} {how}")
+
+
+@pytest.mark.parametrize("rows", [3000, 9000])
+@pytest.mark.parametrize("dim", [5, 520])
+def test_rows_that_no_token_names_do_not_matter(rows, dim):
+    """NaN in the rows of padding, most of the batch; words of few rows and of many."""
+    tokens, dy = words(5, rows, 40, "text"), draw(6, rows, dim)
+    tokens[torch.arange(rows) % 5 != 0] = -1
+    dy[tokens < 0] = math.nan
+    dw = gd.Embedding(40, dim, torch.float32, max_rows=rows).backward(dy, tokens)
+    check_backward(dw, dy, tokens, 40, 1.0, rows, f"{rows} {dim}")
 
 
 def test_a_plan_of_just_these_rows():

@@ -66,7 +66,9 @@ for ty in (0, 1, 2):
             if rows > 64 and dim > 4096: continue
             # in one launch where rows are few and short; zeros of more blocks than a launch holds go round in the sorted form
             few = rows <= 4096 and rows * dim <= 2**21 and (accumulate or -(-(2**31 - 1) // max(16384 // dim, 1)) <= 2**22)
-            launches = 1 if few else 1 + (rows > 4096) + 1 + (rows > 8)
+            slices = -(-dim // (256 if ty == 0 else 512))
+            unit = next((u for u in (32, 16) if -(-rows // u) * slices >= 768), 8)
+            launches = 1 if few else 1 + (rows > 4096) + 1 + (rows > unit)
             b = dict(rows=rows, tokens=P, dy=P, dweight=P, dy_stride=dim, dweight_stride=dim, scale=1.0, index=0, accumulate=accumulate)
             assert call("gd_embed_backward", e, io(gd._EmbedGrad, **b)) == (0, launches), (dim, rows)
             assert Dim.in_dll(S, "g_grid").x * 1024 < 2**32
@@ -89,6 +91,17 @@ assert G.gd_embed_forward(None, io(gd._EmbedIO), None) == 1 and G.gd_embed_backw
 frees = get("g_frees"); G.gd_embed_destroy(e); assert get("g_frees") == frees + 3
 G.gd_embed_destroy(None)
 """, tmp_path)
+
+
+def test_units_of_the_embedding_fit_the_scratch():
+    """No number of rows makes more units than a plan of this many rows or more has room for."""
+    for slices in (1, 2, 3, 5, 8, 33, 100, 767, 768, 1000, 4096):
+        def units(rows):
+            return -(-rows // next((u for u in (32, 16) if -(-rows // u) * slices >= 768), 8))
+        most = 0
+        for rows in [*range(1, 3000), *range(3000, 60_000, 37), 2**24 - 1, 2**24]:
+            most = max(most, units(rows))
+            assert most <= max(min(-(-rows // 8), 1536 // slices), -(-rows // 32)), (slices, rows)
 
 
 def test_gated_layer(tmp_path):
