@@ -331,7 +331,7 @@ typedef enum {
  * A token outside [0, vocab) is padding: its row of y is zeros, and its row of
  * dy is not read.  dweight is written whole, rows of tokens that do not occur
  * with zeros.  A token's rows are summed in their order, in binary32 within
- * 8 to 32 of them and in 64 bits across those.
+ * groups of up to 32 of them and in 64 bits across those.
  * gd_embed_create plans a vocabulary (1..2^31 - 1) of rows of dim (1..2^20)
  * elements in `type` on the current device, for backward calls of at most
  * max_rows (up to 2^24) rows, and allocates 16 bytes per row of those and

@@ -156,24 +156,31 @@ struct Columns {
 //
 // A block takes a row and looks through all tokens for its own: the first row
 // of a token finds all rows of it, in order, and writes their sum, the others
-// end.  Blocks between those write zeros, over rows of dweight that no token
-// names.  Looking costs rows^2 reads of tokens, from the caches, and stays
-// beside the zeros up to kFewRows: 3,000 rows of 500 in binary32 for 85,000
-// words take 32 us, sorted (below) 43; 500 of 512 for 8,000 7.6 and 17.  But a
-// token that occurs often is one block's work: 4,000 rows of 1024 in bfloat16 for
-// 1,000 words take 36 us, sorted 27, so up to kFewWork elements of dy.
-constexpr uint32_t kFewWork = 1u << 21;
+// end.  Of a token with many rows the first few rows' blocks take a share of the
+// columns each, so that the commonest word is no block's work alone (4,096 rows
+// of 512 in bfloat16, one word: 25 us, by one block 66).  Blocks between those
+// write zeros, over rows of dweight that no token names.  Looking costs rows^2
+// reads of tokens, from the caches, and stays beside the zeros up to kFewRows:
+// 3,000 rows of 500 in binary32 for 85,000 words take 31 us, sorted (below) 38;
+// 4,000 of 1024 in bfloat16 for 1,000 words 15 and 22, 4,096 of 8192 26 and 41.
+// Longer rows, whose slices a block would take in turn, are sorted (64 rows of
+// 65,536: 49 us, sorted 15).
+constexpr uint32_t kFewSlices = 16;
 constexpr uint32_t kFewRows = 4096, kFewThreads = 512, kFewWaves = kFewThreads / kWave, kFewAtOnce = 8;
+constexpr uint32_t kFewTogether = 32;  // rows of a token that a wave adds up alone: 1,000 rows of 1024 8.4 us, with 16 12.2
+constexpr uint32_t kRunLanes = 16, kRunAtOnce = 4, kRunShare = 16;  // where a token has more: lanes a row, rows at a time and a block
 constexpr uint32_t kFillFloats = 16384;  // of zeros that a block writes, about
 constexpr uint32_t kFewBlocks = 1u << 22;
 
 template <typename T, bool SHORT>
 __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uint32_t vocab, uint32_t dim, bool wide,
                                                            uint32_t fills, uint32_t per_fill) {
-    constexpr int E = 16 / sizeof(T), kSlice = kWave * E;
+    typedef Columns<T, SHORT> Cols;
+    constexpr int E = Cols::E;
+    constexpr uint32_t kSlice = kWave * E, kRunSlice = kRunLanes * E, kRunGroups = kFewThreads / kRunLanes;
     __shared__ uint64_t mask[kFewRows / kWave];
     __shared__ uint16_t list[kFewRows];
-    __shared__ float shares[kFewWaves][kSlice];
+    __shared__ float shares[kRunGroups][kRunSlice];
     const uint32_t rows = (uint32_t)io.rows, wave = wave_index(), lane = lane_id();
     // rows' blocks are spread evenly among those of zeros: the ones wait, the others write
     const uint64_t all = (uint64_t)rows + fills, at = blockIdx.x;
@@ -212,59 +219,60 @@ __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uin
     uint64_t mine = mask[lane];
     static_assert(kFewRows == kWave * kWave);
     const uint64_t before = lane < i / kWave ? mine : lane == i / kWave ? mine & ((1ull << i % kWave) - 1) : 0;
-    if (ballot(before != 0)) return;  // an earlier row's block writes it
-    const uint32_t incl = wave_incl_scan(popc64(mine)), count = lane_value(incl, kWave - 1);
+    // the token's first row's block writes the sum, of many rows its first rows' blocks a share of the columns each: the
+    // more the more rows, and no block more than four (4,096 rows of 8192: 26 us, by rows alone 51)
+    const uint32_t scan = wave_incl_scan((uint32_t)popc64(before) << 16 | (uint32_t)popc64(mine)), ends = lane_value(scan, kWave - 1);
+    const uint32_t place = ends >> 16, incl = scan & 0xFFFF, count = ends & 0xFFFF;
+    const uint32_t shares_of_row = (dim + kRunSlice - 1) / kRunSlice;
+    const uint32_t blocks = count <= kFewTogether ? 1 : min(max(count / kRunShare, (shares_of_row + 3) / 4), min(count, shares_of_row));
+    if (place >= blocks) return;
     if (wave == 0)
-        for (uint32_t place = incl - popc64(mine); mine; mine &= mine - 1, ++place)
-            list[place] = (uint16_t)(lane * kWave + (uint32_t)__ffsll((unsigned long long)mine) - 1);
+        for (uint32_t to = incl - popc64(mine); mine; mine &= mine - 1, ++to)
+            list[to] = (uint16_t)(lane * kWave + (uint32_t)__ffsll((unsigned long long)mine) - 1);
     __syncthreads();
     float* out = io.dweight + (uint64_t)token * io.dweight_stride;
-    typedef Columns<T, SHORT> Cols;
-    // the sum of rows first to first + kFewAtOnce of the list
-    const auto add = [&](uint32_t first, const Cols& cols, float (&sum)[E]) {
-        u4 d[kFewAtOnce];
+    // adds rows first to first + N of the list
+    const auto add = [&](auto at_once, uint32_t first, const Cols& cols, float (&sum)[E]) {
+        constexpr uint32_t N = at_once();
+        u4 d[N];
 #pragma unroll
-        for (uint32_t k = 0; k < kFewAtOnce; ++k)
-            d[k] = cols.load((const T*)io.dy + (uint64_t)list[min(first + k, count - 1)] * io.dy_stride);
+        for (uint32_t k = 0; k < N; ++k) d[k] = cols.load((const T*)io.dy + (uint64_t)list[min(first + k, count - 1)] * io.dy_stride);
 #pragma unroll
-        for (int j = 0; j < E; ++j) sum[j] = 0.0f;
-#pragma unroll
-        for (uint32_t k = 0; k < kFewAtOnce; ++k)
+        for (uint32_t k = 0; k < N; ++k)
             if (first + k < count) Cols::add(sum, d[k]);
     };
-    if (count <= kFewAtOnce) {  // a wave takes a slice of the columns
+    if (count <= kFewTogether) {  // a wave takes a slice of the columns
         for (uint32_t s = wave * kSlice; s < dim; s += kFewWaves * kSlice) {
             const Cols cols(s + lane * E, dim);
-            float sum[E];
-            add(0, cols, sum);
+            float sum[E] = {};
+            for (uint32_t first = 0; first < count; first += kFewAtOnce)
+                add(std::integral_constant<uint32_t, kFewAtOnce>(), first, cols, sum);
             cols.put(out, sum, io.scale, io.accumulate != 0);
         }
         return;
     }
-    for (uint32_t s = 0; s < dim; s += kSlice) {  // the waves share the rows
-        const Cols cols(s + lane * E, dim);
+    const uint32_t group = threadIdx.x / kRunLanes, l = threadIdx.x % kRunLanes;
+    for (uint32_t s = place * kRunSlice; s < dim; s += blocks * kRunSlice) {  // groups of lanes share the rows
+        const Cols cols(s + l * E, dim);
         double total[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) total[j] = 0.0;
-        for (uint32_t first = wave * kFewAtOnce; first < count; first += kFewWaves * kFewAtOnce) {
-            float sum[E];
-            add(first, cols, sum);
+        for (uint32_t first = group * kRunAtOnce; first < count; first += kRunGroups * kRunAtOnce) {
+            float sum[E] = {};
+            add(std::integral_constant<uint32_t, kRunAtOnce>(), first, cols, sum);
 #pragma unroll
             for (int j = 0; j < E; ++j) total[j] += sum[j];
         }
 #pragma unroll
-        for (int j = 0; j < E; ++j) shares[wave][j * kWave + lane] = (float)total[j];
+        for (int j = 0; j < E; ++j) shares[group][j * kRunLanes + l] = (float)total[j];
         __syncthreads();
-        if (wave == 0) {
-            float sum[E];
+        if (threadIdx.x < kRunSlice) {
+            double v = 0.0;
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                double v = 0.0;
-#pragma unroll
-                for (uint32_t w = 0; w < kFewWaves; ++w) v += shares[w][j * kWave + lane];
-                sum[j] = (float)v;
-            }
-            cols.put(out, sum, io.scale, io.accumulate != 0);
+            for (uint32_t g = 0; g < kRunGroups; ++g) v += shares[g][threadIdx.x];
+            const uint32_t j = threadIdx.x / kRunLanes;  // of the lane's vector
+            const float sum[1] = {(float)v};
+            if (j >= cols.skip && (!SHORT || j < dim)) put_gradient<1>(out + cols.at + j, sum, io.scale, 1, io.accumulate != 0);
         }
         __syncthreads();
     }
@@ -585,7 +593,8 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
     const hipStream_t st = (hipStream_t)stream;
     const uint32_t per_fill = std::max(gd::kFillFloats / e->dim, 1u);
     const uint64_t fills = io->accumulate ? 0 : ((uint64_t)e->vocab + per_fill - 1) / per_fill;
-    if (io->rows <= gd::kFewRows && io->rows * e->dim <= gd::kFewWork && fills <= gd::kFewBlocks) {
+    const uint32_t slices = gd::slice_count(e->dim, e->type);
+    if (io->rows <= gd::kFewRows && slices <= gd::kFewSlices && fills <= gd::kFewBlocks) {
         const hipError_t r = gd::with_type(e->type, [&](auto zero) {
             using T = decltype(zero);
             const auto kernel = e->dim * sizeof(T) < 16 ? gd::k_embed_few<T, true> : gd::k_embed_few<T, false>;
@@ -612,7 +621,7 @@ gd_status gd_embed_backward(gd_embed* e, const gd_embed_grad* io, void* stream) 
             io->dweight_stride);
         if (hipGetLastError() != hipSuccess) return GD_ERR_HIP;
     }
-    const uint32_t slices = gd::slice_count(e->dim, e->type), unit = gd::unit_rows(io->rows, slices);
+    const uint32_t unit = gd::unit_rows(io->rows, slices);
     const uint32_t units = (uint32_t)((io->rows + unit - 1) / unit);
     r = gd::with_type(e->type, [&](auto zero) {
         using T = decltype(zero);

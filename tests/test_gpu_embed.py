@@ -76,7 +76,7 @@ def test_over_sizes(kind, index, rows, vocab, dim):
 # one launch up to 4,096 rows; sorted: units of 8 to 32 rows, one chunk of 4,096 and several, the last one full or of one
 # row; runs over many units
 @pytest.mark.parametrize("how", ["text", "one", "each", "pairs", "padded"])
-@pytest.mark.parametrize("rows,dim", [(7, 20), (8, 20), (9, 20), (15, 20), (16, 20), (17, 300), (2048, 24), (2049, 24), (4096, 12), (4097, 12), (6144, 260), (257, 8200), (2049, 1040), (4096, 520), (8192, 8),
+@pytest.mark.parametrize("rows,dim", [(7, 20), (8, 20), (9, 20), (15, 20), (16, 20), (17, 300), (2048, 24), (2049, 24), (4096, 12), (4097, 12), (6144, 260), (257, 8200), (2049, 1040), (4096, 520), (300, 8192), (1500, 8200), (8192, 8),
                                       (16384, 5), (16385, 5), (30001, 9)])
 def test_backward_over_rows(how, rows, dim):
     vocab = max(rows, 700) if how in ("each", "pairs") else 700

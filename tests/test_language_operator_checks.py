@@ -65,7 +65,7 @@ for ty in (0, 1, 2):
         for rows, accumulate in ((1, 1), (1, 0), (8, 1), (9, 1), (4096, 1), (4096, 0), (4097, 1), (4097, 0), (2**24, 1), (2**24, 0)):
             if rows > 64 and dim > 4096: continue
             # in one launch where rows are few and short; zeros of more blocks than a launch holds go round in the sorted form
-            few = rows <= 4096 and rows * dim <= 2**21 and (accumulate or -(-(2**31 - 1) // max(16384 // dim, 1)) <= 2**22)
+            few = rows <= 4096 and -(-dim // (256 if ty == 0 else 512)) <= 16 and (accumulate or -(-(2**31 - 1) // max(16384 // dim, 1)) <= 2**22)
             slices = -(-dim // (256 if ty == 0 else 512))
             unit = next((u for u in (32, 16) if -(-rows // u) * slices >= 768), 8)
             launches = 1 if few else 1 + (rows > 4096) + 1 + (rows > unit)
