@@ -119,6 +119,22 @@ def test_rows_that_no_token_names_do_not_matter(rows, dim):
     check_backward(dw, dy, tokens, 40, 1.0, rows, f"{rows} {dim}")
 
 
+@pytest.mark.parametrize("dim", [1, 3, 7, 9, 130, 1000, 5001])
+@pytest.mark.parametrize("how", ["text", "one"])
+def test_words_of_many_rows_added_to_what_is_there(dim, how):
+    """A word's columns shared by blocks: rows below a vector, ends inside one, rows of dweight that lie apart."""
+    rows, vocab = 1800, 20
+    tokens, dy = words(5, rows, vocab, how), draw(6, rows, dim, dtype=torch.bfloat16)
+    op = gd.Embedding(vocab, dim, max_rows=rows)
+    check_backward(op.backward(dy, tokens), dy, tokens, vocab, 1.0, rows, f"{dim} {how}")
+    wide = torch.full((vocab, dim + 3), 2.0, device="cuda")
+    op.backward(dy, tokens, dweight=wide[:, :dim], accumulate=True)
+    size = torch.zeros(vocab, dim, dtype=torch.float64).index_add_(0, tokens.cpu(), d(dy).abs())
+    want = torch.zeros(vocab, dim, dtype=torch.float64).index_add_(0, tokens.cpu(), d(dy)) + 2.0
+    close(wide[:, :dim], want, 67 * E * (size + 2.0), f"{dim} {how}")
+    assert bool((wide[:, dim:] == 2.0).all())
+
+
 def test_a_plan_of_just_these_rows():
     """Scratch for max_rows holds the most units that any smaller number of rows makes."""
     for most in (1, 16, 17, 4000, 4096, 5000, 8191, 9000, 16384, 16385, 33000):
