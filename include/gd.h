@@ -649,7 +649,10 @@ gd_status gd_gated_backward(gd_gated* layer, const gd_gated_grad* io, void* stre
  * its logp is 0, whatever dlogp is there passes no gradient; the row's entropy and
  * alternatives are as every row's.  A row with plus infinity or a NaN has NaN,
  * and where no gradient comes down to a row (padding, or dlogp of 0, and
- * dentropy of 0) its gradient is 0 whatever it holds.
+ * dentropy of 0) its gradient is 0 whatever it holds.  Finite logits are
+ * numbers of any size, also where scale takes them past binary32: a row of the
+ * lowest value is uniform.  What counts is scale times the distance from the
+ * row's largest (a distance past binary32 is infinite).
  * gd_logprob_create plans rows of vocab (1..2^31 - 1) logits in `type` for
  * calls of at most max_rows (up to 2^31 - 1) rows on the current device, and
  * allocates 300 KB of scratch.
@@ -664,8 +667,9 @@ typedef struct {
     const void* tokens;       /* [rows] of `index` */
     float* logp;              /* [rows], or NULL */
     float* entropy;           /* [rows], or NULL */
-    float* stats;             /* [rows][2] receives the largest z and the log of the sum of exp(z - largest), whose sum
-                                 is lse, for a backward call; or NULL */
+    float* stats;             /* [rows][2] receives two numbers for a backward call, whose sum is lse: the largest z and
+                                 the log of the sum of exp(z - largest).  A row whose largest z is past 2^24 and not
+                                 a binary32 number has others, whose sum is nothing.  Or NULL */
     float* top_logp;          /* [rows][top] receives the log probabilities of the likeliest tokens, in falling order */
     int64_t* top_id;          /* [rows][top] and their ids: of equal logits the lower id first, a NaN before all numbers */
     uint64_t stride;          /* at least vocab */

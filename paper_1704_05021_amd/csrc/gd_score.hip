@@ -9,12 +9,16 @@
 //     loss = sum_j w_j (log w_j - (z_id_j - lse)),  dz_v = dloss (p_v sum_j w_j - sum over j with id_j = v of w_j)
 //   dlogits = scale dz
 //
-// One pass over a row gives its largest z, the sum of exp(z - largest) and the
-// sum of exp(z - largest) (z - largest), each thread with a running maximum of
-// its own, joined at the end; from these come lse = largest + log s and
+// One pass over a row gives its largest logit, the sum of exp(d) and the sum of
+// exp(d) d, where d = scale (logit - largest), each thread with a running
+// maximum of its own, joined at the end; from these come log p = d - log s and
 // H = log s - t / s.  The gradient takes a second pass.  Both are bound by
 // memory.  Few long rows are cut into pieces, a block each, whose sums a second
 // launch joins.
+//
+// The largest is taken off before the scale is put on: the difference of equal
+// logits is 0 whatever their size and the scale's.  (z - largest z, with either
+// product rounded, is 1e30 for the lowest value of binary32 at a scale of 0.7.)
 //
 // Top alternatives: a row's 64 groups of threads know their largest logits, the
 // K-th largest of those is a bound that at least K elements reach, and few more:
@@ -22,6 +26,7 @@
 // those before it.  Where a mask makes very many equal to the bound, a third look
 // lists what is above it.
 
+#include <cfloat>
 #include <cmath>
 #include <new>
 
@@ -39,14 +44,19 @@ constexpr uint32_t kScoreTopRoom = 1024;     // alternatives that a row's pieces
 constexpr uint32_t kListRoom = 1024;         // elements that a row's list holds; a row of more is looked through K times
 constexpr int kScoreDeep = 2;                // vectors of a thread in a turn; the next turn's are on their way meanwhile
 
-// A share of a row: the largest z, and relative to it the sums of exp(z) and of exp(z) z.
+// A share of a row: the largest logit, and the sums of 2^d and of 2^d d, d = rate (logit - largest), rate = scale log2 e.
 struct Soft {
     float m, s, t;
 };
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m; }
-// exp of this and of all below is 0 in binary32: farther terms are held there, as 0 times infinity is not 0.
+// 2 to the power of this and of all below is 0 in binary32, and exp of it: farther terms are held there, as 0 times
+// infinity is not 0.
 constexpr float kFar = -200.0f;
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+// The hardware's exponential in every type: scale and log2 e are put on with two roundings, whose share in exp(x) is up to
+// |x| 2^-23, 4e-6 where exp(x) is 1e-15 (the library's errs by 1e-7 there).  What counts in sums is near x = 0.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float exp_fast(float x) { return exp2_fast(x * kLog2E); }
 
 // The largest of three, NaN left out.  (Of fmaxf the compiler makes three instructions for a pair: it quiets both first.)
 __device__ __forceinline__ float max_of(float a, float b, float c) {
@@ -76,24 +86,24 @@ __device__ __forceinline__ float wave_max_f32(float v) {
 __device__ __forceinline__ float wave_sum_f32(float v) {
     return wave_join(v, -0.0f, [](float a, float b) { return a + b; });
 }
-__device__ __forceinline__ Soft wave_soft(Soft a) {
+__device__ __forceinline__ Soft wave_soft(Soft a, float rate) {
     Soft r;
     r.m = wave_max_f32(a.m);
-    const float to = reference(r.m), f = exp_fast(a.m - to);
-    r.t = wave_sum_f32(f * (a.t + a.s * fmaxf(reference(a.m) - to, kFar)));
+    const float gap = (a.m - reference(r.m)) * rate, f = exp2_fast(gap);
+    r.t = wave_sum_f32(f * (a.t + a.s * fmaxf(gap, kFar)));
     r.s = wave_sum_f32(f * a.s);
     return r;
 }
 // Over the threads of a row; a barrier lies between this and the next use of lds.
 template <int WAVES>
-__device__ __forceinline__ Soft row_soft(Soft a, Soft* lds) {
-    a = wave_soft(a);
+__device__ __forceinline__ Soft row_soft(Soft a, float rate, Soft* lds) {
+    a = wave_soft(a, rate);
     if constexpr (WAVES > 1) {
         if (lane_id() == 0) lds[wave_index()] = a;
         __syncthreads();
         a = Soft{-INFINITY, 0.0f, 0.0f};
         if (lane_id() < WAVES) a = lds[wave_index() / WAVES * WAVES + lane_id()];
-        a = wave_soft(a);
+        a = wave_soft(a, rate);
     }
     return a;
 }
@@ -109,17 +119,46 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ uint64_t key_of_element(uint32_t order, uint32_t id) { return (uint64_t)order << 32 | ~id; }
 
-// What is named in a row or a piece of it: of a token z and 1; of a teacher the sum of w (log w - z), and of w.
+// What is named in a row or a piece of it, relative to a logit of it: of a token 0, 1 and its own logit; of a teacher the
+// sum of w (log w - scale (logit - of)), that of w, and the largest logit that it names.  (Relative to 0, terms of the
+// lowest value's size would leave nothing of the logs.)
 struct Sight {
     double at, w;
+    float of;
+    // at, relative to the logit `to`.
+    __device__ __forceinline__ double from(float to, float scale) const {
+        return w == 0.0 ? at : at + w * (((double)to - (double)of) * (double)scale);
+    }
 };
+
+// What a row's elements are measured from: log p = scale (logit - ref) - log_s.
+struct Level {
+    float ref, log_s;
+};
+// The two numbers that a gradient's call takes it from, of the largest logit and the log of the sum.  As long as they can
+// be they are the largest z, rounded, and the log with what that rounding left, so that their sum is lse.  Where
+// what it leaves is of any size, they are the logit itself and the log less than -1, which no log of the others is.
+__device__ __forceinline__ void put_stats(float* to, float most, float log_s, float scale) {
+    const float z = most * scale, rest = isinf(most) ? 0.0f : fmaf(most, scale, -z);
+    const bool adds = fabsf(z) < 0x1p24f || rest == 0.0f;  // rest is at most 1/2, or none
+    to[0] = adds ? z : most;
+    to[1] = adds ? log_s + rest : -1.0f - log_s;
+}
+__device__ __forceinline__ Level get_stats(const float* from, float scale) {
+    const float z = from[0], log_s = from[1];
+    if (log_s <= -1.0f && log_s != -INFINITY) return {z, -1.0f - log_s};
+    if (isinf(z)) return {z, log_s};
+    // where z is past 2^24 it is exact, and so is this quotient
+    const float ref = fminf(fmaxf(__fdiv_rn(z, scale), -FLT_MAX), FLT_MAX);
+    return {ref, log_s - fmaf(ref, scale, -z)};
+}
 
 struct ScoreArgs {
     uint64_t rows;
     uint32_t vocab, pieces, piece;   // pieces of a row and the elements of one
     const void* logits;
     uint64_t stride;
-    float scale;
+    float scale, rate;               // rate: scale log2 e
     const void* ids;                 // [rows][count]
     uint64_t ids_stride;
     uint32_t count;
@@ -200,10 +239,11 @@ struct Turns {
 
 // What the gradient at an element takes: dz = p (c + e (log p + H)), both with the scale in them.
 struct Slope {
-    float m, log_s, c, e, entropy, c_s;  // c_s: c over the sum of exp(z - m)
-    __device__ __forceinline__ float plain(float x, float scale) const { return exp_fast(fmaf(x, scale, -m)) * c_s; }
+    Level level;
+    float c, e, entropy, c_s;  // c_s: c over the sum
+    __device__ __forceinline__ float plain(float x, float rate) const { return exp2_fast((x - level.ref) * rate) * c_s; }
     __device__ __forceinline__ float at(float x, float scale) const {
-        const float lp = fmaf(x, scale, -m) - log_s;  // log p
+        const float lp = fmaf(x - level.ref, scale, -level.log_s);  // log p
         return exp_fast(lp) * fmaf(e, fmaxf(lp, kFar) + entropy, c);
     }
 };
@@ -243,47 +283,52 @@ __device__ __forceinline__ void name_teacher(const ScoreArgs& a, uint64_t row, u
         if (i * kWave >= (int)a.count) continue;
         const int64_t v = j < a.count ? id_at(a, row, j) : -1;
         if (v >= 0) {
-            w[i] = teacher_at(a, row, j) * a.scale;
+            w[i] = teacher_at(a, row, j);
             if ((uint64_t)v - begin < n) here[i] = (uint32_t)v - begin;
         }
         most = fmaxf(most, w[i]);
     }
     most = reference(wave_max_f32(most));
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += expf(w[i] - most);
+    for (int i = 0; i < kEach; ++i) w[i] = (w[i] - most) * a.scale, sum += expf(w[i]);
     sum = wave_sum_f32(sum);
     const float log_sum = logf(sum);
-    Sight sight{0.0, 0.0};
+    float weight[kEach], v[kEach], of = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        weight[i] = sum == 0.0f ? 0.0f : expf(w[i]) / sum;
+        v[i] = here[i] != kNotHere ? (float)x[here[i]] : 0.0f;
+        if (here[i] != kNotHere && weight[i] != 0.0f) of = fmaxf(of, v[i]);
+    }
+    of = reference(wave_max_f32(of));
+    Sight sight{0.0, 0.0, of};
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const uint32_t j = i * kWave + lane;
         if (j >= a.count) continue;
-        const float log_w = w[i] - most - log_sum, weight = sum == 0.0f ? 0.0f : expf(w[i] - most) / sum;
-        const float v = here[i] != kNotHere ? (float)x[here[i]] : 0.0f;
-        if (here[i] != kNotHere && weight != 0.0f) {
-            sight.at += (double)weight * ((double)log_w - (double)v * (double)a.scale);
-            sight.w += (double)weight;
+        if (here[i] != kNotHere && weight[i] != 0.0f) {
+            sight.at += (double)weight[i] * ((double)(w[i] - log_sum) - ((double)v[i] - (double)of) * (double)a.scale);
+            sight.w += (double)weight[i];
         }
-        to.w[j] = weight, to.x[j] = v, to.id[j] = here[i];
+        to.w[j] = weight[i], to.x[j] = v[i], to.id[j] = here[i];
     }
     sight.at = wave_sum(sight.at);
     sight.w = wave_sum(sight.w);
     if (lane == 0) to.sight = sight, to.held = sum > 0.0f ? 1.0f : sum;
 }
 
-// What a row comes to: the token's log probability or the teacher's loss, its entropy and its sums.
+// What a row comes to: the token's log probability or the teacher's loss, its entropy and its sums.  at and w: of what is
+// named, relative to the largest logit; weights as rounded, whose sum is not quite 1.
 template <bool TEACHER>
-__device__ __forceinline__ void put_row(const ScoreArgs& a, uint64_t row, const Soft& soft, const Sight& sight, bool held) {
+__device__ __forceinline__ void put_row(const ScoreArgs& a, uint64_t row, const Soft& soft, double at, double w, bool held) {
     const float log_s = logf(soft.s);
     const bool none = soft.m == -INFINITY && soft.s == 0.0f;  // every logit is minus infinity
     if (a.out) {
-        // the largest first, which may be so far from 0 that the log vanishes beside it; weights as rounded, whose sum is not quite 1
-        const double v = TEACHER ? (sight.at + sight.w * (double)soft.m) + sight.w * (double)log_s
-                                 : (sight.at - (double)soft.m) - (double)log_s;
+        const double v = TEACHER ? at + w * (double)log_s : -at - (double)log_s;
         a.out[row] = !held ? 0.0f : none ? (TEACHER ? INFINITY : -INFINITY) : (float)v;
     }
-    if (a.entropy) a.entropy[row] = none ? 0.0f : log_s - soft.t / soft.s;
-    if (a.stats) a.stats[row * 2] = soft.m, a.stats[row * 2 + 1] = log_s;
+    if (a.entropy) a.entropy[row] = none ? 0.0f : log_s - soft.t / soft.s * kLn2;
+    if (a.stats) put_stats(a.stats + row * 2, soft.m, log_s, a.scale);
 }
 
 // The alternatives of a row or a piece, from the largest element of every thread.
@@ -420,7 +465,7 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
     const uint32_t piece = unit % a.pieces, begin = piece * a.piece, n = min(a.vocab - begin, a.piece), vecs = (n + 7) / 8;
     const uint64_t row = unit / a.pieces;
     const T* x = (const T*)a.logits + row * a.stride + begin;
-    const float scale = a.scale;
+    const float scale = a.scale, rate = a.rate;
     constexpr bool GRAD = KIND >= kGrad;
 
     // the token and its logit, read before anything is written over it; a teacher's by the row's first wave
@@ -459,23 +504,22 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
             for (int k = 0; k < kScoreDeep; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) most = max_of(most, z[k][j], z[k][j + 1]);
-            const float big = most * scale;
-            const float to = reference(big), f = exp_fast(soft.m - to);
+            const float to = reference(most), gap = (soft.m - to) * rate, f = exp2_fast(gap);
             float p[kScoreDeep] = {}, tt[kScoreDeep] = {};  // sums of a few, side by side
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int k = 0; k < kScoreDeep; ++k) {
-                    const float d = fmaf(z[k][j], scale, -to), e = exp_fast(d);
+                    const float d = (z[k][j] - to) * rate, e = exp2_fast(d);
                     p[k] += e;
                     if (entropy) tt[k] = fmaf(e, fmaxf(d, kFar), tt[k]);
                 }
             float ps = 0.0f, ts = 0.0f;
 #pragma unroll
             for (int k = 0; k < kScoreDeep; ++k) ps += p[k], ts += tt[k];
-            if (entropy) soft.t = f * (soft.t + soft.s * fmaxf(reference(soft.m) - to, kFar)) + ts;
+            if (entropy) soft.t = f * (soft.t + soft.s * fmaxf(gap, kFar)) + ts;
             soft.s = fmaf(f, soft.s, ps);
-            soft.m = big;
+            soft.m = most;
         };
         const auto add_whole = [&](const Turn& raw, uint32_t) {
             float z[kScoreDeep][8];
@@ -500,22 +544,22 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
             add(z);
         }
     }
-    if (stats) soft = row_soft<WAVES>(soft, lds_soft);
+    if (stats) soft = row_soft<WAVES>(soft, rate, lds_soft);
     if (TEACHER || GRAD) __syncthreads();
 
-    Sight sight{0.0, 0.0};
+    Sight sight{0.0, 0.0, 0.0f};
     float held = 0.0f;
     if constexpr (TEACHER) {
         sight = named[r].sight, held = named[r].held;
     } else if (token >= 0) {
         held = 1.0f;
-        if ((uint64_t)token - begin < n) sight = {(double)token_x * (double)scale, 1.0};
+        if ((uint64_t)token - begin < n) sight = {0.0, 1.0, token_x};
     }
     if (stats && t == 0 && on) {
         if (a.pieces > 1)
             a.part[unit] = soft, a.part_sight[unit] = sight;
         else
-            put_row<TEACHER>(a, row, soft, sight, held != 0.0f);
+            put_row<TEACHER>(a, row, soft, sight.from(soft.m, scale), sight.w, held != 0.0f);
     }
 
     if constexpr (KIND == kTop) {
@@ -526,7 +570,7 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
             if (a.pieces > 1) {
                 a.part_key[(uint64_t)unit * K + rank] = key;
             } else {
-                const float lp = fmaf(value_of((uint32_t)(key >> 32)), scale, -soft.m) - log_s;
+                const float lp = fmaf(value_of((uint32_t)(key >> 32)) - soft.m, scale, -log_s);
                 a.top_logp[row * K + rank] = soft.m == -INFINITY && log_s == -INFINITY ? -INFINITY : lp;
                 a.top_id[row * K + rank] = (int64_t)(uint32_t)~(uint32_t)key;
             }
@@ -534,15 +578,14 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
     }
     if constexpr (GRAD) {
         Slope sl;
-        sl.m = stats ? soft.m : a.given[row * 2];
-        sl.log_s = stats ? logf(soft.s) : a.given[row * 2 + 1];
-        sl.entropy = stats ? sl.log_s - soft.t / soft.s : a.given_entropy ? a.given_entropy[row] : 0.0f;
+        sl.level = stats ? Level{soft.m, logf(soft.s)} : get_stats(a.given + row * 2, scale);
+        sl.entropy = stats ? sl.level.log_s - soft.t / soft.s * kLn2 : a.given_entropy ? a.given_entropy[row] : 0.0f;
         sl.c = held == 0.0f ? 0.0f : (TEACHER ? g : -g) * held * scale;
         sl.e = e;
-        sl.c_s = sl.c / (stats ? soft.s : expf(sl.log_s));
+        sl.c_s = sl.c / (stats ? soft.s : expf(sl.level.log_s));
         T* d = (T*)a.dlogits + row * a.dstride + begin;
         // a row that no gradient comes down to has none, whatever it holds, nor has one of which every logit is minus infinity
-        const bool zeros = (sl.c == 0.0f && sl.e == 0.0f) || (sl.m == -INFINITY && sl.log_s == -INFINITY);
+        const bool zeros = (sl.c == 0.0f && sl.e == 0.0f) || (sl.level.ref == -INFINITY && sl.level.log_s == -INFINITY);
         const auto write = [&](auto value) {  // of an element
             const auto of = [&](const Pack<T, 8>& raw) {
                 Pack<T, 8> y;
@@ -577,7 +620,7 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
             if constexpr (KIND == kGradEntropy)
                 write([&](float v) { return sl.at(v, scale); });
             else
-                write([&](float v) { return sl.plain(v, scale); });
+                write([&](float v) { return sl.plain(v, rate); });
         }
         // the elements that are named are written anew, with their weights in them and rounded once, behind the others
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -595,10 +638,10 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
                         first = first && k >= j;
                         w += q.w[k];
                     }
-                if (first) d[id] = (T)(sl.plain(q.x[j], scale) - g * w * scale);
+                if (first) d[id] = (T)(sl.plain(q.x[j], rate) - g * w * scale);
             }
         } else if (t == 0 && token >= 0 && (uint64_t)token - begin < n) {
-            d[(uint64_t)token - begin] = (T)((KIND == kGradEntropy ? sl.at(token_x, scale) : sl.plain(token_x, scale)) + g * scale);
+            d[(uint64_t)token - begin] = (T)((KIND == kGradEntropy ? sl.at(token_x, scale) : sl.plain(token_x, rate)) + g * scale);
         }
     }
 }
@@ -611,16 +654,15 @@ __global__ __launch_bounds__(kScoreJoinThreads) void k_score_join(ScoreArgs a) {
     const uint64_t row = blockIdx.x;
     const uint32_t lane = lane_id();
     Soft soft{-INFINITY, 0.0f, 0.0f};
-    Sight sight{0.0, 0.0};
+    Sight sight{0.0, 0.0, 0.0f};
     if (lane < a.pieces) soft = a.part[row * a.pieces + lane], sight = a.part_sight[row * a.pieces + lane];
     bool held = false;  // whether a token is there, or a teacher's logit above minus infinity (NaN is one)
     for (uint32_t j = lane; j < a.count; j += kWave)
         held = held || (id_at(a, row, j) >= 0 && (!TEACHER || !(teacher_at(a, row, j) == -INFINITY)));
     held = ballot(held) != 0;
-    soft = wave_soft(soft);
-    sight.at = wave_sum(sight.at);
-    sight.w = wave_sum(sight.w);
-    if (threadIdx.x == 0) put_row<TEACHER>(a, row, soft, sight, held);
+    soft = wave_soft(soft, a.rate);
+    const double at = wave_sum(sight.from(soft.m, a.scale)), w = wave_sum(sight.w);
+    if (threadIdx.x == 0) put_row<TEACHER>(a, row, soft, at, w, held);
     if (!a.top) return;
     const float log_s = logf(soft.s);
     const uint32_t all = a.pieces * a.top;
@@ -631,7 +673,7 @@ __global__ __launch_bounds__(kScoreJoinThreads) void k_score_join(ScoreArgs a) {
         uint32_t rank = 0;
         for (uint32_t k = 0; k < all; ++k) rank += keys[k] > key;
         if (rank >= a.top || key == 0) continue;
-        const float lp = fmaf(value_of((uint32_t)(key >> 32)), a.scale, -soft.m) - log_s;
+        const float lp = fmaf(value_of((uint32_t)(key >> 32)) - soft.m, a.scale, -log_s);
         a.top_logp[row * a.top + rank] = soft.m == -INFINITY && log_s == -INFINITY ? -INFINITY : lp;
         a.top_id[row * a.top + rank] = (int64_t)(uint32_t)~(uint32_t)key;
     }
@@ -724,9 +766,11 @@ struct ScorePlan {
                         mem.alloc(&stats, kScoreBlocks) && mem.alloc(&entropy, kScoreBlocks / 2);
         return ok ? GD_OK : GD_ERR_OOM;
     }
-    ScoreArgs args() const {
+    ScoreArgs args(float scale) const {
         ScoreArgs a{};
         a.vocab = vocab;
+        a.scale = scale;
+        a.rate = std::min(scale * kLog2E, FLT_MAX);  // not infinity: 0 times that is not 0
         a.part = part, a.part_sight = part_sight, a.part_key = part_key;
         return a;
     }
@@ -809,11 +853,10 @@ gd_status distill_args(const gd_distill* l, const IO* io, gd::ScoreArgs& a) {
     if (io->rows && (!io->logits || !io->ids || !io->teacher || io->stride < l->plan.vocab || io->ids_stride < io->top ||
                      io->teacher_stride < io->top))
         return GD_ERR_ARG;
-    a = l->plan.args();
+    a = l->plan.args(io->scale);
     a.rows = io->rows;
     a.logits = io->logits;
     a.stride = io->stride;
-    a.scale = io->scale;
     a.ids = io->ids;
     a.ids_stride = io->ids_stride;
     a.count = io->top;
@@ -844,11 +887,10 @@ gd_status gd_logprob_forward(gd_logprob* l, const gd_logprob_io* io, void* strea
         return GD_ERR_ARG;
     gd::DeviceGuard guard(l->plan.device);
     if (!guard.ok) return GD_ERR_HIP;
-    gd::ScoreArgs a = l->plan.args();
+    gd::ScoreArgs a = l->plan.args(io->scale);
     a.rows = io->rows;
     a.logits = io->logits;
     a.stride = io->stride;
-    a.scale = io->scale;
     a.ids = io->tokens;
     a.ids_stride = a.count = 1;
     a.wide = wide == GD_I64;
@@ -872,11 +914,10 @@ gd_status gd_logprob_backward(gd_logprob* l, const gd_logprob_grad* io, void* st
         return GD_ERR_ARG;
     gd::DeviceGuard guard(l->plan.device);
     if (!guard.ok) return GD_ERR_HIP;
-    gd::ScoreArgs a = l->plan.args();
+    gd::ScoreArgs a = l->plan.args(io->scale);
     a.rows = io->rows;
     a.logits = io->logits;
     a.stride = io->stride;
-    a.scale = io->scale;
     a.ids = io->tokens;
     a.ids_stride = a.count = 1;
     a.wide = wide == GD_I64;

@@ -1217,7 +1217,7 @@ class LogProbs:
 
     logp: torch.Tensor  # of the given token
     entropy: Optional[torch.Tensor] = None
-    stats: Optional[torch.Tensor] = None  # [..., 2]: the largest scaled logit, the log of the sum of exp relative to it
+    stats: Optional[torch.Tensor] = None  # [..., 2] for backward, their sum the log of the sum of exp (see gd.h)
     top_logp: Optional[torch.Tensor] = None  # [..., top], falling
     top_ids: Optional[torch.Tensor] = None  # [..., top] int64
 
