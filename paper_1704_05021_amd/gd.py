@@ -1284,6 +1284,11 @@ class TokenLogProbs(_Scores):
                     self._tensor(getattr(out, name), "out." + name, torch.float32, n)
             if top:
                 self._tensor(out.top_ids, "out.top_ids", torch.int64, rows * top)
+            if rows:
+                self._outputs_apart(io, logits, tokens, {"out.logp": out.logp, "out.entropy": out.entropy if entropy else None,
+                                                         "out.stats": out.stats if keep_stats else None,
+                                                         "out.top_logp": out.top_logp if top else None,
+                                                         "out.top_ids": out.top_ids if top else None})
         io.logp = out.logp.data_ptr()
         if entropy:
             io.entropy = out.entropy.data_ptr()
@@ -1298,6 +1303,17 @@ class TokenLogProbs(_Scores):
         if st != 0:
             raise GDError(st, "gd_logprob_forward")
         return out
+
+    def _outputs_apart(self, io, logits, tokens, outputs) -> None:
+        """Given outputs lie apart from what the call reads, and from one another, of whatever types they are."""
+        size = self.dtype.itemsize
+        others = {"logits": (io.logits, io.rows, io.stride * size, self.vocab * size),
+                  "tokens": (io.tokens, 1, tokens.nbytes, tokens.nbytes)}
+        for name, t in outputs.items():
+            if t is not None:
+                span = (t.data_ptr(), 1, t.nbytes, t.nbytes)
+                _apart(1, name, span, others)
+                others[name] = span
 
     def backward(self, logits, tokens, dlogp, dentropy=None, scores: Optional[LogProbs] = None, out=None, stream=None):
         """dlogits, from the gradients of the log probabilities and (or None) of the entropies, float32.  ``scores``:
