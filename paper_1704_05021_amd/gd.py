@@ -1264,7 +1264,8 @@ class TokenLogProbs(_Scores):
     def forward(self, logits, tokens, top: int = 0, entropy: bool = True, keep_stats: bool = False,
                 out: Optional[LogProbs] = None, stream=None):
         """LogProbs; ``top`` up to 64 alternatives, of equal logits the lower id first; ``keep_stats`` for backward.
-        ``out``: one of an earlier call of the same shape and wishes, to write again."""
+        ``out``: one of an earlier call of the same shape and wishes, to write again; what it holds beyond these wishes would
+        stay that call's, and is refused."""
         if not 0 <= top < 1 << 32:
             raise GDError(1, "gd_logprob_forward")
         io = _LogProbIO()
@@ -1284,6 +1285,9 @@ class TokenLogProbs(_Scores):
                     self._tensor(getattr(out, name), "out." + name, torch.float32, n)
             if top:
                 self._tensor(out.top_ids, "out.top_ids", torch.int64, rows * top)
+            for name, wish in (("entropy", entropy), ("stats", keep_stats), ("top_logp", top), ("top_ids", top)):
+                if not wish and getattr(out, name) is not None:
+                    raise ValueError(f"out.{name} is of another call, and not asked for in this one")
             if rows:
                 self._outputs_apart(io, logits, tokens, {"out.logp": out.logp, "out.entropy": out.entropy if entropy else None,
                                                          "out.stats": out.stats if keep_stats else None,

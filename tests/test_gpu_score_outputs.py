@@ -70,3 +70,14 @@ def test_outputs_side_by_side_and_between_rows_are_taken():
     for name in NAMES:
         assert torch.equal(getattr(got, name), getattr(r, name)), name
     assert torch.equal(between.logp, r.logp) and torch.equal(wide[:, :vocab], x)
+
+
+@pytest.mark.parametrize("wishes", [dict(top=4, entropy=False, keep_stats=True), dict(top=4), dict(keep_stats=True)])
+def test_outputs_that_the_call_would_leave_as_they_were_are_refused(wishes):
+    """Stats of other logits, taken for these ones' by a backward call, would give a wrong gradient."""
+    op, x, tokens, r = made(8, 96)
+    with pytest.raises(ValueError, match="not asked for"):
+        op.forward(x, tokens, out=r, **wishes)
+    for keep in (False, True):
+        r = op.forward(x, tokens, keep_stats=keep)
+        assert op.forward(x, tokens, keep_stats=keep, out=r) is r
