@@ -627,7 +627,8 @@ typedef struct {
     const void* pre;          /* [rows][2 out] pre of the forward call: g and u */
     void* dz;                 /* [rows][2 out] receives dy u act'(g) and dy act(g), rounded to the type, the gradient of
                                  both sums that the products below are taken with; may be pre.  Under GD_ACT_RELU both
-                                 are 0 where g is not above 0, whatever dy is there. */
+                                 are 0 where g is 0 or below, whatever dy is there; where g is NaN the first is 0 and
+                                 the second NaN. */
     void* dx;                 /* [rows][in] receives dz weight, or NULL */
     float* dweight;           /* [2 out][in] in binary32, rows at dweight_stride: dz^T x, or NULL */
     float* dbias;             /* [2 out] in binary32: sum over rows of dz, or NULL */
