@@ -330,8 +330,9 @@ typedef enum {
  *   y[i] = scale * weight[t_i];  dweight[v] = scale * sum over i with t_i = v of dy[i]
  * A token outside [0, vocab) is padding: its row of y is zeros, and its row of
  * dy is not read.  dweight is written whole, rows of tokens that do not occur
- * with zeros.  A token's rows are summed in their order, in binary32 within
- * groups of up to 32 of them and in 64 bits across those.
+ * with zeros.  A token's rows are summed in binary32 within groups of up to 32
+ * of them and in 64 bits across those, in an order that is the same on every
+ * run.
  * gd_embed_create plans a vocabulary (1..2^31 - 1) of rows of dim (1..2^20)
  * elements in `type` on the current device, for backward calls of at most
  * max_rows (up to 2^24) rows, and allocates 16 bytes per row of those and
