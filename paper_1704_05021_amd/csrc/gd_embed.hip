@@ -179,15 +179,17 @@ __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uin
     constexpr int E = Cols::E;
     constexpr uint32_t kSlice = kWave * E, kRunSlice = kRunLanes * E, kRunGroups = kFewThreads / kRunLanes;
     __shared__ uint64_t mask[kFewRows / kWave];
-    __shared__ uint16_t list[kFewRows];
+    __shared__ union {
+        uint16_t list[kFewRows];                    // of a token's rows
+        uint32_t named[(kFillFloats + 31) / 32];    // a bit for each row that a block of zeros looks after
+    } lds;
     __shared__ float shares[kRunGroups][kRunSlice];
     const uint32_t rows = (uint32_t)io.rows, wave = wave_index(), lane = lane_id();
     // rows' blocks are spread evenly among those of zeros: the ones wait, the others write
     const uint64_t all = (uint64_t)rows + fills, at = blockIdx.x;
     const uint32_t i = (uint32_t)(at * rows / all);
     if ((at + 1) * rows / all == i) {
-        uint32_t* named = (uint32_t*)list;  // a bit for each row of the block
-        static_assert(sizeof(list) * 8 >= kFillFloats);
+        auto& named = lds.named;
         const uint32_t first = (uint32_t)(at - i) * per_fill, n = min(per_fill, vocab - first);
         for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += kFewThreads) named[w] = 0;
         __syncthreads();
@@ -208,6 +210,7 @@ __global__ __launch_bounds__(kFewThreads) void k_embed_few(gd_embed_grad io, uin
     }
     const uint32_t token = token_at(io.tokens, wide, i, vocab);
     if (token == kNoToken) return;
+    auto& list = lds.list;
     uint32_t others[kFewRows / kFewThreads];
     tokens_at(io.tokens, wide, threadIdx.x, kFewThreads, rows, vocab, others);
 #pragma unroll
