@@ -1280,19 +1280,17 @@ class TokenLogProbs(_Scores):
                 out.top_logp = _fresh(stream, logits, (*shape, top), f32)
                 out.top_ids = _fresh(stream, logits, (*shape, top), torch.int64)
         else:
-            for name, n in (("logp", rows), ("entropy", rows * entropy), ("stats", 2 * rows * keep_stats), ("top_logp", rows * top)):
+            spans = []
+            for name, n, size in (("logp", rows, 4), ("entropy", rows * entropy, 4), ("stats", 2 * rows * keep_stats, 4),
+                                  ("top_logp", rows * top, 4), ("top_ids", rows * top, 8)):
+                t, name = getattr(out, name), "out." + name
                 if n:
-                    self._tensor(getattr(out, name), "out." + name, torch.float32, n)
-            if top:
-                self._tensor(out.top_ids, "out.top_ids", torch.int64, rows * top)
-            for name, wish in (("entropy", entropy), ("stats", keep_stats), ("top_logp", top), ("top_ids", top)):
-                if not wish and getattr(out, name) is not None:
-                    raise ValueError(f"out.{name} is of another call, and not asked for in this one")
+                    at = self._tensor(t, name, torch.float32 if size == 4 else torch.int64, n)
+                    spans.append((at, at + n * size, name))
+                elif rows and t is not None:
+                    raise ValueError(f"{name} is of another call, and not asked for in this one")
             if rows:
-                self._outputs_apart(io, logits, tokens, {"out.logp": out.logp, "out.entropy": out.entropy if entropy else None,
-                                                         "out.stats": out.stats if keep_stats else None,
-                                                         "out.top_logp": out.top_logp if top else None,
-                                                         "out.top_ids": out.top_ids if top else None})
+                self._outputs_apart(io, tokens, spans)
         io.logp = out.logp.data_ptr()
         if entropy:
             io.entropy = out.entropy.data_ptr()
@@ -1308,16 +1306,24 @@ class TokenLogProbs(_Scores):
             raise GDError(st, "gd_logprob_forward")
         return out
 
-    def _outputs_apart(self, io, logits, tokens, outputs) -> None:
-        """Given outputs lie apart from what the call reads, and from one another, of whatever types they are."""
-        size = self.dtype.itemsize
+    def _outputs_apart(self, io, tokens, spans) -> None:
+        """Given outputs (first byte, past the last, name) lie apart from what the call reads, and from one another, of
+        whatever types they are."""
+        size, token_bytes = self.dtype.itemsize, tokens.nbytes
+        past = 0
+        for at, to, _ in sorted([*spans, (io.tokens, io.tokens + token_bytes, ""),
+                                 (io.logits, io.logits + ((io.rows - 1) * io.stride + self.vocab) * size, "")]):
+            if at < past:
+                break
+            past = to
+        else:
+            return
         others = {"logits": (io.logits, io.rows, io.stride * size, self.vocab * size),
-                  "tokens": (io.tokens, 1, tokens.nbytes, tokens.nbytes)}
-        for name, t in outputs.items():
-            if t is not None:
-                span = (t.data_ptr(), 1, t.nbytes, t.nbytes)
-                _apart(1, name, span, others)
-                others[name] = span
+                  "tokens": (io.tokens, 1, token_bytes, token_bytes)}
+        for at, to, name in spans:  # an output may lie between the logits' rows
+            span = (at, 1, to - at, to - at)
+            _apart(1, name, span, others)
+            others[name] = span
 
     def backward(self, logits, tokens, dlogp, dentropy=None, scores: Optional[LogProbs] = None, out=None, stream=None):
         """dlogits, from the gradients of the log probabilities and (or None) of the entropies, float32.  ``scores``:
