@@ -121,3 +121,21 @@ def test_stats_of_ordinary_rows_add_up(kind):
         rel, lse, p, *_ = tokens64(x, ids_of(2, vocab, rows), scale32)
         # the log's error, and its rounding beside the rest of the largest product, which is below 1
         close(d(r.stats).sum(1), lse[:, 0], sum_error(p, rel)[:, 0] + 14 * E, f"{kind} {scale}")
+
+
+@pytest.mark.parametrize("rows,vocab", [(5, 300), (300, 9000), (2, 30_000)])
+@pytest.mark.parametrize("scale", [1e30, 1e-30])
+def test_scales_of_any_size(rows, vocab, scale):
+    """Ordinary logits: one of them is certain, or all are as likely as one another."""
+    x, tokens, g, h = draw(1, rows, vocab, scale=3.0), ids_of(2, vocab, rows), draw(3, rows), draw(4, rows)
+    ids, teacher = ids_of(5, vocab, rows, 3), draw(6, rows, 3)
+    scale32 = float(torch.tensor(scale, dtype=torch.float32))
+    op, ds = (kind(vocab, torch.float32, scale=scale, max_rows=rows) for kind in (gd.TokenLogProbs, gd.Distill))
+    r = op.forward(x, tokens, keep_stats=True)
+    rel, _, p, _, logp, *_ = tokens64(x, tokens, scale32)
+    close(r.logp, logp, sum_error(p, rel)[:, 0] + 2 * E * logp.abs(), "logp")
+    for dh in (None, h):
+        check_gradient(op.backward(x, tokens, g, dh, scores=r), x, tokens, g, dh, scale32, "given")
+        check_gradient(op.forward_backward(x, tokens, g, dh)[1], x, tokens, g, dh, scale32, "in one")
+    loss, dx = ds.forward_backward(x, ids, teacher, g)
+    check_distill(loss, dx, x, ids, teacher, g, scale32, "teacher")
