@@ -718,7 +718,11 @@ hipError_t launch_gradient(const ScoreArgs& a, hipStream_t st) {
 // barrier stands between its passes (gradient of 20,000 x 4,000 in bfloat16: 79 us, with four waves 186; of 9,000 x
 // 8,000 63 and 75; of 5,000 x 16,000 80 and 69), where there are rows enough to fill the chip so.  Turns held spare a
 // second reading but leave room for fewer waves: 3,000 x 85,000 take 220 us with six turns of four waves, 241 with two;
-// 5,000 x 16,000 take 83 and 69; four waves in place of eight 248 and 262.
+// 2,400 x 42,000 73 and 83, but 2,400 x 30,000 52 and 58 and 2,400 x 38,000 64 and 75: of bfloat16 the border could lie
+// lower, between those and 5,000 x 16,000 (83 and 69).  Of 2,400 rows in binary32, 15,000 take 56 and 59, 25,000 101 and
+// 109.  Four waves in place of eight take 248 and 262.
+// The sums alone by four waves and by eight: 600 x 70,000 in bfloat16 20 and 22 us, 600 x 90,000 25 and 27, 600 x 110,000 29
+// and 31, 600 x 200,000 47 and 48; in binary32 600 x 45,000 21 and 21, 600 x 60,000 26 and 26.
 template <typename T>
 hipError_t launch_score_type(const ScoreArgs& a, bool grad, hipStream_t st) {
     const uint32_t n = std::min(a.vocab, a.piece);

@@ -639,7 +639,8 @@ class _Handle:
     """A library handle on one device, freed with the object.
 
     Outputs in the layer's type that the caller gives are checked to lie apart from the call's inputs and its other
-    outputs in that type, but where a call says that they may be the same rows.  Autograd does not follow the calls: a
+    outputs in that type, but where a call says that they may be the same rows; gradients of parameters, which are in
+    float32 whatever the type, are the caller's to keep apart.  Autograd does not follow the calls: a
     layer's forward refuses tensors that require gradients while autograd records, and its backward gives the gradients.
     """
 
