@@ -672,8 +672,8 @@ typedef struct {
     float* logp;              /* [rows], or NULL */
     float* entropy;           /* [rows], or NULL */
     float* stats;             /* [rows][2] receives two numbers for a backward call, whose sum is lse: the largest z and
-                                 the log of the sum of exp(z - largest).  A row whose largest z is past 2^24 and not
-                                 a binary32 number has others, whose sum is nothing.  Or NULL */
+                                 the log of the sum of exp(z - largest).  Where the largest z is past 2^24 and no
+                                 binary32 number they are two others, whose sum has no meaning.  Or NULL */
     float* top_logp;          /* [rows][top] receives the log probabilities of the likeliest tokens, in falling order */
     int64_t* top_id;          /* [rows][top] and their ids: of equal logits the lower id first, a NaN before all numbers */
     uint64_t stride;          /* at least vocab */
