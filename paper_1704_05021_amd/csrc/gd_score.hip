@@ -261,7 +261,8 @@ __device__ __forceinline__ float teacher_at(const ScoreArgs& a, uint64_t row, ui
 }
 
 // A teacher's row, by one wave: the ids that lie in this piece, the logits there and the weights; `held` is the sum of
-// all weights, 1, or 0 where the teacher names nothing.
+// all weights, 1, or 0 where the teacher names nothing.  What is seen of them is formed where it is asked for: not where the
+// row's sums are given.
 struct Named {
     float w[kScoreMaxTeacher], x[kScoreMaxTeacher];
     uint32_t id[kScoreMaxTeacher];  // within the piece, or kNotHere
@@ -270,7 +271,7 @@ struct Named {
 };
 constexpr uint32_t kNotHere = 0xFFFFFFFFu;
 template <typename T>
-__device__ __forceinline__ void name_teacher(const ScoreArgs& a, uint64_t row, uint32_t begin, uint32_t n, const T* x, Named& to) {
+__device__ __forceinline__ void name_teacher(const ScoreArgs& a, uint64_t row, uint32_t begin, uint32_t n, const T* x, bool seen, Named& to) {
     constexpr int kEach = kScoreMaxTeacher / kWave;
     const uint32_t lane = lane_id();
     float w[kEach], most = -INFINITY, sum = 0.0f;
@@ -300,21 +301,24 @@ __device__ __forceinline__ void name_teacher(const ScoreArgs& a, uint64_t row, u
         v[i] = here[i] != kNotHere ? (float)x[here[i]] : 0.0f;
         if (here[i] != kNotHere && weight[i] != 0.0f) of = fmaxf(of, v[i]);
     }
-    of = reference(wave_max_f32(of));
-    Sight sight{0.0, 0.0, of};
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const uint32_t j = i * kWave + lane;
-        if (j >= a.count) continue;
+        if (j < a.count) to.w[j] = weight[i], to.x[j] = v[i], to.id[j] = here[i];
+    }
+    if (lane == 0) to.held = sum > 0.0f ? 1.0f : sum;
+    if (!seen) return;
+    of = reference(wave_max_f32(of));
+    Sight sight{0.0, 0.0, of};
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
         if (here[i] != kNotHere && weight[i] != 0.0f) {
             sight.at += (double)weight[i] * ((double)(w[i] - log_sum) - ((double)v[i] - (double)of) * (double)a.scale);
             sight.w += (double)weight[i];
         }
-        to.w[j] = weight[i], to.x[j] = v[i], to.id[j] = here[i];
-    }
     sight.at = wave_sum(sight.at);
     sight.w = wave_sum(sight.w);
-    if (lane == 0) to.sight = sight, to.held = sum > 0.0f ? 1.0f : sum;
+    if (lane == 0) to.sight = sight;
 }
 
 // What a row comes to: the token's log probability or the teacher's loss, its entropy and its sums.  at and w: of what is
@@ -467,18 +471,19 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
     const T* x = (const T*)a.logits + row * a.stride + begin;
     const float scale = a.scale, rate = a.rate;
     constexpr bool GRAD = KIND >= kGrad;
+    const bool stats = !GRAD || !a.given;  // the row's sums are formed here
 
     // the token and its logit, read before anything is written over it; a teacher's by the row's first wave
     int64_t token = -1;
     float token_x = 0.0f;
     if constexpr (TEACHER) {
-        if (t < (uint32_t)kWave) name_teacher(a, row, begin, n, x, named[r]);
+        if (t < (uint32_t)kWave) name_teacher(a, row, begin, n, x, stats, named[r]);
     } else {
         token = id_at(a, row, 0);
         if (token >= 0) token_x = (float)((const T*)a.logits + row * a.stride)[token];
     }
     const float g = GRAD ? a.g[row] : 0.0f, e = KIND == kGradEntropy && a.h ? -a.h[row] * scale : 0.0f;
-    const bool stats = !GRAD || !a.given, entropy = KIND == kGradEntropy || (!GRAD && a.entropy);
+    const bool entropy = KIND == kGradEntropy || (!GRAD && a.entropy);
     // padding with nothing to say of it: its logits are not read
     const bool skip = GRAD && !TEACHER && token < 0 && e == 0.0f && !a.entropy;
 
@@ -550,7 +555,8 @@ __global__ __launch_bounds__(NormShape<WAVES>::kThreads) void k_score(ScoreArgs 
     Sight sight{0.0, 0.0, 0.0f};
     float held = 0.0f;
     if constexpr (TEACHER) {
-        sight = named[r].sight, held = named[r].held;
+        held = named[r].held;
+        if (stats) sight = named[r].sight;
     } else if (token >= 0) {
         held = 1.0f;
         if ((uint64_t)token - begin < n) sight = {0.0, 1.0, token_x};
